@@ -230,7 +230,7 @@ def _store_plain(x, codes, scale, slots, query_start):
     most = torch.zeros_like(scale).scatter_reduce(0, page[:, None].expand_as(top), top, "amax")
     begin = torch.full((pages,), P, device=x.device).scatter_reduce(0, page, torch.where(live, place, P), "amin")
     fresh, touched = (begin == 0)[:, None], (begin < P)[:, None]
-    want = (most / 127.0).clamp(min=FLOOR)
+    want = (most / torch.full_like(most, 127.0)).clamp(min=FLOOR)                                # a tensor: by a number, torch multiplies by 1 / 127
     after = torch.where(touched, torch.where(fresh, want, torch.maximum(scale, want)), scale)
     # the page in which each request goes on: codes in front of its first new token
     lead = query_start[:-1].long().clamp(max=slots.numel() - 1)
