@@ -256,6 +256,93 @@ double tsq_model_outage(double rate, double bandwidth, double snr);
 double tsq_model_latency(double bits, double rate, double bandwidth, double snr, double epsilon);
 double tsq_model_best_rate(double rate_lo, double rate_hi, double bandwidth, double snr);
 
+/*
+ * The paged 8-bit key/value cache.  (The paper counts the bits of a KV cache held at Q^a bits per element, Eq. "bkv", and the machine that takes a
+ * request over goes on from it; how it is held there is this library's own.)  Keys and values are whole numbers in [-127, 127] with one scale
+ * for each page of tokens and head: Eq. "Proposed" on signed values with zero-point 0, the range taken over the page instead of the token.
+ *
+ * A cache is described by a HOST struct that the caller fills in; the library keeps nothing of it.
+ *   dtype        type of the 16-bit rows that are stored, loaded and attended with
+ *   kv_heads     >= 1
+ *   head_dim     64 or 128 (else TSQ_ERR_UNSUPPORTED)
+ *   page_tokens  tokens of a page: 16, 32, 64 or 128 (else TSQ_ERR_UNSUPPORTED)
+ *   pages        >= 1; pages * page_tokens < 2^31
+ *   k_codes, v_codes  DEVICE, [pages][kv_heads][page_tokens][head_dim], 16-byte aligned
+ *   k_scale, v_scale  DEVICE, [pages][kv_heads], value = code * scale; >= 0
+ * A token's slot is page * page_tokens + its place in the page.  Rows of keys, values and queries are [tokens][heads][head_dim] with the heads of a
+ * token contiguous and a stride between tokens, in elements: a multiple of 8, at least heads * head_dim (so that a part of a wider
+ * tensor can be passed); their base addresses are 16-byte aligned.  Every call enqueues work on `cuda_stream`, whose device has to be current,
+ * and returns argument errors before anything is enqueued.  Nothing a caller leaves in the slots, tables and lengths makes a call read or write outside
+ * its arrays: a slot or a page outside the cache stands for "none".
+ */
+typedef struct {
+  tsq_dtype_t dtype;
+  int32_t kv_heads, head_dim, page_tokens;
+  int64_t pages;
+  int8_t *k_codes, *v_codes;
+  float *k_scale, *v_scale;
+} tsq_cache_t;
+
+/*
+ * What a step's other calls need, from the requests' lengths, built on the GPU.  Request i has held[i] tokens in the cache and brings added[i]
+ * (both int32, DEVICE, [requests]; negative counts as 0).  0 <= requests <= 8192, more are TSQ_ERR_UNSUPPORTED.
+ *   query_start  out [requests + 1]   exclusive prefix sum of added (their sum has to be below 2^31)
+ *   lengths      out [requests]       held + added
+ *   block_table  in/out [requests][table_pages]  entry e is the page of tokens e * page_tokens ... of the request.  The entries of the pages that
+ *                the step begins are written, in the order of the requests, with free_pages[0], free_pages[1], ...; -1 once the n_free are used up.
+ *                Entries in front are read, those behind left as they are; pages past table_pages are not recorded
+ *   slots        out [tokens]         slot of every new token, request after request; -1 where there is no page, and in the rows behind the last
+ *                request's (a batch padded to a fixed size)
+ *   taken        out [1]              pages that the step begins (more than n_free: the last ones got none)
+ * free_pages [n_free] DEVICE.  The call is one kernel launch, with the same arguments it gives the same results again.
+ */
+tsq_status_t tsq_cache_slots(int32_t page_tokens, const int32_t *held, const int32_t *added, int32_t requests,
+                             const int32_t *free_pages, int32_t n_free, int32_t *query_start, int32_t *lengths,
+                             int32_t *block_table, int32_t table_pages, int32_t *slots, int64_t tokens, int32_t *taken,
+                             void *cuda_stream);
+
+/*
+ * Quantise a step's keys and values (DEVICE, [tokens][kv_heads][head_dim], strides as above) into the cache at slots[0 .. tokens) (DEVICE; a slot
+ * outside the cache: the row is skipped).  Tokens of one page have to be neighbours at successive places, as tsq_cache_slots lays them out; a page that
+ * comes twice in a call is left with undefined codes and scale.  For a run at the places o, o + 1, ... of a page, for each head and for keys and
+ * values apart: a = largest |x| of the run, infinities and NaN left out; scale s = max(a / 127, 2^-40), and not below the scale that the page had if
+ * o > 0; codes at the places in front of o become rint(code * (s_had / s)); the run's codes are rint(x * (1 / s)), within +-127, 0 for NaN.  Places behind
+ * the run keep their codes.  The arithmetic is IEEE binary32, round-to-nearest-even.  One kernel launch.
+ */
+tsq_status_t tsq_cache_store(const tsq_cache_t *cache, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                             int64_t tokens, const int32_t *slots, void *cuda_stream);
+
+/*
+ * Read tokens back: row t of k and v (DEVICE, strides as above) becomes code * scale of slots[t], in binary32 and rounded once to the cache's
+ * dtype; 0 for a slot outside the cache.  Slots may come in any order and more than once.  (What a cache that is handed on to another machine goes through
+ * tsq_encode as.)  One kernel launch.
+ */
+tsq_status_t tsq_cache_load(const tsq_cache_t *cache, const int32_t *slots, int64_t tokens, void *k, int64_t k_stride,
+                            void *v, int64_t v_stride, void *cuda_stream);
+
+/*
+ * Attention of a step's queries over the cache.  q and out: [tokens][q_heads][head_dim] (DEVICE, strides as above), q_heads a multiple of kv_heads, at most
+ * 64 times; query head h reads key head h / (q_heads / kv_heads).  Request i owns the rows query_start[i] .. query_start[i + 1) and has lengths[i]
+ * tokens in the cache, its own of this step among them; its row j is the token at position lengths[i] - n_i + j and sees the positions up to its own:
+ *   out = sum_p softmax_p(scale * <q, k_p>) v_p
+ * Rows that see no key (n_i > lengths[i]) are written as zeros, rows behind the last request's are left as they were.  Scores, the softmax's
+ * sum and the accumulators are binary32; weights are rounded to binary16, relative to the largest of their row times its page's scale.
+ * A page outside the cache in block_table, and what lies past table_pages, is not seen.  Codes and scales behind a request's last token are not used, whatever they hold.
+ *   max_query    no request has more rows than this (>= 1); rows past it are left as they were
+ *   requests     0 .. 8192, more are TSQ_ERR_UNSUPPORTED
+ *   scale        finite; 1 / sqrt(head_dim) is the usual one
+ *   ws           DEVICE, of tsq_cache_workspace's size or larger, 16-byte aligned, initialised once by tsq_cache_workspace_init; one workspace
+ *                serves one call at a time.  Calls of a step whose sizes are not above those that the size was asked for may share it
+ * Offsets into the cache are 64-bit.  One kernel launch; the same inputs give the same bits.
+ */
+tsq_status_t tsq_cache_workspace(const tsq_cache_t *cache, int64_t tokens, int32_t q_heads, int32_t requests, int32_t max_query,
+                                 size_t *workspace_bytes);
+tsq_status_t tsq_cache_workspace_init(void *ws_dev, size_t ws_bytes, void *cuda_stream);
+tsq_status_t tsq_cache_attention(const tsq_cache_t *cache, const void *q, int64_t q_stride, int32_t q_heads, int64_t tokens,
+                                 const int32_t *query_start, const int32_t *lengths, int32_t requests, int32_t max_query,
+                                 const int32_t *block_table, int32_t table_pages, float scale, void *out,
+                                 int64_t out_stride, void *ws_dev, size_t ws_bytes, void *cuda_stream);
+
 /* Number of kernels the library has launched in this process (all plans, all streams). */
 uint64_t tsq_kernel_launch_count(void);
 

@@ -1,9 +1,9 @@
 """Thin binding of the tsq C ABI (include/tsq.h): argument marshalling only.
 
 Every step of encode and decode runs inside the CUDA library; torch is used for device
-memory and streams.  Function names mirror the C entry points.  The two calls of a decode step,
-encode and decode, go through the extension module built from csrc/tsq_torch.cpp (5 us less host
-time per call than ctypes); everything else goes through ctypes.
+memory and streams.  Function names mirror the C entry points.  The calls of a decode step,
+encode and decode and those of the paged cache, go through the extension module built from
+csrc/tsq_torch.cpp (5 us less host time per call than ctypes); everything else goes through ctypes.
 """
 from __future__ import annotations
 
@@ -24,6 +24,7 @@ EXPORTS = ["tsq_plan", "tsq_plan_variant", "tsq_plan_sizes", "tsq_workspace_init
            "tsq_blob_info",
            "tsq_workspace_status", "tsq_encode_host", "tsq_decode_host", "tsq_kernel_launch_count",
            "tsq_plan_destroy", "tsq_status_string",
+           "tsq_cache_slots", "tsq_cache_store", "tsq_cache_load", "tsq_cache_workspace", "tsq_cache_workspace_init", "tsq_cache_attention",
            "tsq_model_kv_bits", "tsq_model_io_bits", "tsq_model_outage", "tsq_model_latency", "tsq_model_best_rate"]
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtsq.so")
@@ -44,6 +45,11 @@ class _Sizes(C.Structure):
 class _Info(C.Structure):
     _fields_ = [("status", C.c_uint32), ("tokens", C.c_uint32), ("hidden", C.c_uint32), ("dtype", C.c_uint32),
                 ("total_words", C.c_uint64), ("total_outliers", C.c_uint64), ("payload_bytes", C.c_uint64)]
+
+
+class _CacheStruct(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_tokens", C.c_int32), ("pages", C.c_int64),
+                ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
 
 
 def lib() -> C.CDLL:
@@ -78,6 +84,15 @@ def lib() -> C.CDLL:
                  "tsq_workspace_status", "tsq_encode_host", "tsq_decode_host"):
         getattr(L, name).restype = C.c_int
     d, i32 = C.c_double, C.c_int32
+    cache, ip = C.POINTER(_CacheStruct), C.c_void_p
+    L.tsq_cache_slots.argtypes = [i32, ip, ip, i32, ip, i32, ip, ip, ip, i32, ip, i64, ip, vp]
+    L.tsq_cache_store.argtypes = [cache, vp, i64, vp, i64, i64, ip, vp]
+    L.tsq_cache_load.argtypes = [cache, ip, i64, vp, i64, vp, i64, vp]
+    L.tsq_cache_workspace.argtypes = [cache, i64, i32, i32, i32, C.POINTER(sz)]
+    L.tsq_cache_workspace_init.argtypes = [vp, sz, vp]
+    L.tsq_cache_attention.argtypes = [cache, vp, i64, i32, i64, ip, ip, i32, i32, ip, i32, C.c_float, vp, i64, vp, sz, vp]
+    for name in ("tsq_cache_slots", "tsq_cache_store", "tsq_cache_load", "tsq_cache_workspace", "tsq_cache_workspace_init", "tsq_cache_attention"):
+        getattr(L, name).restype = C.c_int
     L.tsq_model_kv_bits.argtypes = [i64, i32, i32, i32, i64, d, d]
     L.tsq_model_io_bits.argtypes = [i64, i32, i32, i32, i64, d, d, i32]
     L.tsq_model_outage.argtypes = [d, d, d]
@@ -216,6 +231,80 @@ class Plan:
                                    blob_dev.data_ptr(), y_dev.data_ptr(), ws.data_ptr(), ws.numel(),
                                    _stream(stream))
         _check(st, "tsq_decode_host")
+
+
+class Cache:
+    """The paged 8-bit key/value cache (tsq_cache_t) over four tensors of the caller's: codes int8 [pages, kv_heads, page_tokens, head_dim] and scales
+    float32 [pages, kv_heads], for keys and for values.  Methods are the C calls tsq_cache_* with pointers filled in; they run on the tensors' device,
+    on `stream` or that device's current one, and raise TsqError where the call refuses its arguments."""
+
+    def __init__(self, dtype: torch.dtype, k_codes: torch.Tensor, v_codes: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        lib()
+        for name, t in (("k_codes", k_codes), ("v_codes", v_codes)):
+            assert t.is_cuda and t.is_contiguous() and t.dtype == torch.int8 and t.dim() == 4 and t.shape == k_codes.shape and t.device == k_codes.device, \
+                "%s must be a contiguous int8 CUDA tensor [pages, kv_heads, page_tokens, head_dim]" % name
+        pages, kv_heads, page_tokens, head_dim = k_codes.shape
+        for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+            assert t.is_cuda and t.is_contiguous() and t.dtype == torch.float32 and tuple(t.shape) == (pages, kv_heads) and t.device == k_codes.device, \
+                "%s must be a contiguous float32 CUDA tensor [pages, kv_heads] on the codes' device" % name
+        self.dtype, self.pages, self.kv_heads, self.page_tokens, self.head_dim = dtype, pages, kv_heads, page_tokens, head_dim
+        self.k_codes, self.v_codes, self.k_scale, self.v_scale = k_codes, v_codes, k_scale, v_scale
+        self.device = k_codes.device.index
+        self._c = _CacheStruct(dtype_code(dtype), kv_heads, head_dim, page_tokens, pages, k_codes.data_ptr(), v_codes.data_ptr(),
+                               k_scale.data_ptr(), v_scale.data_ptr())
+        self._addr = C.addressof(self._c)
+        self._scale = head_dim ** -0.5 if head_dim else 1.0
+
+    @classmethod
+    def alloc(cls, dtype: torch.dtype, kv_heads: int, head_dim: int, pages: int, page_tokens: int = 64, device: int = 0) -> "Cache":
+        """A cache over tensors of its own, every code and scale 0."""
+        dev = torch.device("cuda", device)
+        codes = [torch.zeros((pages, kv_heads, page_tokens, head_dim), dtype=torch.int8, device=dev) for _ in range(2)]
+        scales = [torch.zeros((pages, kv_heads), dtype=torch.float32, device=dev) for _ in range(2)]
+        return cls(dtype, *codes, *scales)
+
+    def store(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
+        st = _calls.cache_store(self._addr, self.device, k, v, slots, stream)
+        if st != 0:
+            raise TsqError(st, "tsq_cache_store")
+
+    def load(self, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
+        st = _calls.cache_load(self._addr, self.device, slots, k, v, stream)
+        if st != 0:
+            raise TsqError(st, "tsq_cache_load")
+
+    def workspace_bytes(self, tokens: int, q_heads: int, requests: int, max_query: int) -> int:
+        out = C.c_size_t(0)
+        with torch.cuda.device(self.device):
+            _check(lib().tsq_cache_workspace(C.byref(self._c), tokens, q_heads, requests, max_query, C.byref(out)), "tsq_cache_workspace")
+        return int(out.value)
+
+    def workspace(self, tokens: int, q_heads: int, requests: int, max_query: int) -> torch.Tensor:
+        """Allocate a workspace for attention calls of up to these sizes with torch and initialise it on the current stream."""
+        ws = torch.empty(self.workspace_bytes(tokens, q_heads, requests, max_query), dtype=torch.uint8, device=torch.device("cuda", self.device))
+        self.workspace_init(ws)
+        return ws
+
+    def workspace_init(self, ws: torch.Tensor, stream=None) -> None:
+        with torch.cuda.device(self.device):
+            _check(lib().tsq_cache_workspace_init(ws.data_ptr(), ws.numel(), _stream(stream)), "tsq_cache_workspace_init")
+
+    def attention(self, q: torch.Tensor, query_start: torch.Tensor, lengths: torch.Tensor, block_table: torch.Tensor, out: torch.Tensor,
+                  ws: torch.Tensor, max_query: int, scale: Optional[float] = None, stream=None) -> None:
+        """scale: 1 / sqrt(head_dim) unless given."""
+        st = _calls.cache_attention(self._addr, self.device, q, query_start, lengths, block_table, out, ws, max_query,
+                                    self._scale if scale is None else scale, stream)
+        if st != 0:
+            raise TsqError(st, "tsq_cache_attention")
+
+
+def cache_slots(page_tokens: int, held: torch.Tensor, added: torch.Tensor, free_pages: torch.Tensor, query_start: torch.Tensor,
+                lengths: torch.Tensor, block_table: torch.Tensor, slots: torch.Tensor, taken: torch.Tensor, stream=None) -> None:
+    """tsq_cache_slots on int32 tensors of one device."""
+    lib()
+    st = _calls.cache_slots(page_tokens, held, added, free_pages, query_start, lengths, block_table, slots, taken, stream)
+    if st != 0:
+        raise TsqError(st, "tsq_cache_slots")
 
 
 def model_kv_bits(w, layer, n_layers, split_layer, hd, qa_front, qa_back) -> float:

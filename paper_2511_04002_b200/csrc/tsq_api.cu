@@ -7,6 +7,7 @@
 #include <mutex>
 #include <new>
 
+#include "tsq_cache.h"
 #include "tsq_internal.h"
 
 namespace tsq {
@@ -83,6 +84,9 @@ __global__ void workspace_init_kernel(WsControl* ws, uint32_t desc_capacity) { w
 __global__ void workspace_wait_limit_kernel(WsControl* ws, uint32_t polls) { ws->poll_limit = polls; }
 
 }  // namespace
+
+void count_launch() { g_launches.fetch_add(1); }
+
 }  // namespace tsq
 
 namespace tsq {

@@ -1,0 +1,565 @@
+// The paged 8-bit key/value cache: argument checks and launches of its calls, and the kernels that build block tables and slots, quantise keys
+// and values into the cache and read them back.  Attention: tsq_cache_rows.cu.
+
+#include <algorithm>
+#include <atomic>
+#include <cmath>
+#include <cstring>
+
+#include "tsq_cache.h"
+#include "tsq_device.cuh"
+#include "tsq_internal.h"
+
+namespace tsq {
+namespace {
+
+// ---- block tables and slots ----------------------------------------------------------------------
+
+constexpr int kSlotThreads = 256;
+constexpr int kSlotTokens = 4 * kSlotThreads;  // rows per CTA, as far as the grid goes by them
+
+struct SlotParams {
+  const int32_t *held, *added, *free_pages;
+  int32_t *query_start, *lengths, *table, *slots, *taken;
+  long long tokens;
+  int32_t requests, n_free, table_pages, page_shift;
+};
+
+__device__ __forceinline__ long long warp_scan(long long v) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const long long up = __shfl_up_sync(kFull, v, d);
+    if (lane >= d) v += up;
+  }
+  return v;
+}
+
+// Exclusive sums of tokens and new pages over the requests, by every CTA for itself: the lengths are a few kilobytes that come out of L2, and nothing has to
+// be waited for.  Then a thread per token: the request by bisection, the page from the table or, where the step begins it, from the free
+// list.  The token at a page's first place also writes the table's entry, so no entry is read that this call writes.
+// Bound by latency: two dependent reads and a scan (64 requests), and by the slots written (262144 tokens 1 MB).
+__global__ void __launch_bounds__(kSlotThreads) slots_kernel(const SlotParams p) {
+  extern __shared__ int32_t s_requests[];  // [requests + 1] first token, [requests] rank of the first new page
+  __shared__ long long s_tokens[kSlotThreads / 32], s_pages[kSlotThreads / 32];
+  launch_dependents();
+  wait_for_prior_grids();
+  int32_t* const s_start = s_requests;
+  int32_t* const s_rank = s_requests + p.requests + 1;
+  const int P = 1 << p.page_shift;
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  const int per = (p.requests + kSlotThreads - 1) / kSlotThreads;
+  const int i0 = min(tid * per, p.requests), i1 = min(i0 + per, p.requests);
+  long long n_tokens = 0, n_pages = 0;
+  for (int i = i0; i < i1; ++i) {
+    const long long held = max(p.held[i], 0), added = max(p.added[i], 0);
+    n_tokens += added;
+    n_pages += ((held + added + P - 1) >> p.page_shift) - ((held + P - 1) >> p.page_shift);
+  }
+  const long long in_tokens = warp_scan(n_tokens), in_pages = warp_scan(n_pages);
+  if (lane == 31) {
+    s_tokens[warp] = in_tokens;
+    s_pages[warp] = in_pages;
+  }
+  __syncthreads();
+  long long at = in_tokens - n_tokens, rank = in_pages - n_pages, all_tokens = 0, all_pages = 0;
+#pragma unroll
+  for (int w = 0; w < kSlotThreads / 32; ++w) {
+    if (w < warp) {
+      at += s_tokens[w];
+      rank += s_pages[w];
+    }
+    all_tokens += s_tokens[w];
+    all_pages += s_pages[w];
+  }
+  const long long most = 0x7fffffffll;
+  for (int i = i0; i < i1; ++i) {
+    const long long held = max(p.held[i], 0), added = max(p.added[i], 0);
+    s_start[i] = static_cast<int32_t>(min(at, most));
+    s_rank[i] = static_cast<int32_t>(min(rank, most));
+    if (blockIdx.x == 0) {
+      p.query_start[i] = static_cast<int32_t>(min(at, most));
+      p.lengths[i] = static_cast<int32_t>(min(held + added, most));
+    }
+    at += added;
+    rank += ((held + added + P - 1) >> p.page_shift) - ((held + P - 1) >> p.page_shift);
+  }
+  if (tid == 0) {
+    s_start[p.requests] = static_cast<int32_t>(min(all_tokens, most));
+    if (blockIdx.x == 0) {
+      p.query_start[p.requests] = static_cast<int32_t>(min(all_tokens, most));
+      *p.taken = static_cast<int32_t>(min(all_pages, most));
+    }
+  }
+  __syncthreads();
+  // every new token, with a row in slots or without one, and the rows behind the last request's
+  const long long total = s_start[p.requests], end = max(total, p.tokens);
+  for (long long t = static_cast<long long>(blockIdx.x) * kSlotThreads + tid; t < end; t += static_cast<long long>(gridDim.x) * kSlotThreads) {
+    int32_t slot = -1;
+    if (t < total) {
+      int lo = 0, hi = p.requests - 1;  // the last request that starts at or in front of t: the one that has it
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (s_start[mid] <= t) {
+          lo = mid;
+        } else {
+          hi = mid - 1;
+        }
+      }
+      const long long held = max(p.held[lo], 0);
+      const long long position = held + (t - s_start[lo]);
+      const long long entry = position >> p.page_shift, first = (held + P - 1) >> p.page_shift;
+      const int place = static_cast<int>(position & (P - 1));
+      int32_t page = -1;
+      if (entry < p.table_pages) {
+        int32_t* const cell = p.table + static_cast<long long>(lo) * p.table_pages + entry;
+        if (entry < first) {
+          page = *cell;
+        } else {
+          const long long r = s_rank[lo] + (entry - first);
+          page = r < p.n_free ? p.free_pages[r] : -1;
+          if (place == 0) *cell = page;
+        }
+      }
+      const long long at = (static_cast<long long>(page) << p.page_shift) + place;
+      if (page >= 0 && at <= most) slot = static_cast<int32_t>(at);
+    }
+    if (t < p.tokens) p.slots[t] = slot;
+  }
+}
+
+// ---- quantising into the cache -------------------------------------------------------------------
+
+constexpr int kStoreThreads = 128;
+constexpr int kStoreBlock = 64;           // most tokens whose runs one CTA looks after
+constexpr float kScaleFloor = 9.094947017729282e-13f;  // 2^-40
+
+struct StoreParams {
+  const uint16_t *k, *v;
+  int8_t *k_codes, *v_codes;
+  float *k_scale, *v_scale;
+  long long k_stride, v_stride, tokens;
+  const int32_t* slots;
+  int32_t heads, block;                   // tokens per CTA
+  uint32_t n_slots;                       // of the cache
+};
+
+// A code from x * (1 / s), rounded to nearest even: within +-127 whatever x is, 0 for NaN (the conversion's result).
+__device__ __forceinline__ uint32_t code_of(float x, float inverse) {
+  return static_cast<uint32_t>(min(max(__float2int_rn(x * inverse), -127), 127)) & 0xffu;
+}
+__device__ __forceinline__ int signed_byte(uint32_t w, int i) { return static_cast<int>(w << (24 - 8 * i)) >> 24; }
+
+// One CTA per head, keys or values, and block of tokens: for every run (tokens of one page) that begins in the block, the run's rows are read once into
+// registers, the largest finite |x| is reduced on the 15-bit patterns, and the codes are formed from the registers.  A page that was begun earlier has its codes
+// rescaled only when the scale grows.  Block: as many tokens as leave a few CTAs per SM, a page's run at most (store_block).
+template <bool BF16, int D, int P>
+__global__ void __launch_bounds__(kStoreThreads) store_kernel(const StoreParams p) {
+  constexpr int kRowChunks = D / 8;                                    // 16-byte chunks of a row
+  constexpr int kItems = (P * kRowChunks + kStoreThreads - 1) / kStoreThreads;
+  __shared__ int32_t s_slot[kStoreBlock + P + 1];
+  __shared__ uint32_t s_lead[kStoreThreads / 32], s_max[kStoreThreads / 32], s_ok[kStoreThreads / 32];
+  launch_dependents();
+  wait_for_prior_grids();
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  const int parts = 2 * p.heads;
+  const long long t0 = static_cast<long long>(blockIdx.x / parts) * p.block;
+  const int which = static_cast<int>(blockIdx.x % parts) / p.heads, head = static_cast<int>(blockIdx.x % parts) % p.heads;
+  const uint16_t* const x = which ? p.v : p.k;
+  const long long stride = which ? p.v_stride : p.k_stride;
+  int8_t* const codes = which ? p.v_codes : p.k_codes;
+  float* const scales = which ? p.v_scale : p.k_scale;
+  // s_slot[1 + i] is the slot of token t0 + i, s_slot[0] that of the token in front; -1: none
+  for (int i = tid; i < p.block + P + 1; i += kStoreThreads) {
+    const long long t = t0 + i - 1;
+    const int32_t slot = t >= 0 && t < p.tokens ? p.slots[t] : -1;
+    s_slot[i] = static_cast<uint32_t>(slot) < p.n_slots ? slot : -1;
+  }
+  __syncthreads();
+  bool leads = false;
+  if (tid < p.block) {
+    const int32_t slot = s_slot[1 + tid];
+    leads = slot >= 0 && (slot % P == 0 || s_slot[tid] != slot - 1);
+  }
+  const uint32_t mine = __ballot_sync(kFull, leads);
+  if (lane == 0) s_lead[warp] = mine;
+  __syncthreads();
+  for (int w = 0; w < kStoreBlock / 32; ++w) {
+    for (uint32_t left = s_lead[w]; left != 0; left &= left - 1) {
+      const int j = 32 * w + __ffs(static_cast<int>(left)) - 1;
+      const int32_t slot = s_slot[1 + j];
+      const int place = slot % P;
+      // length of the run
+      const bool on = tid < P && place + tid < P && s_slot[1 + j + (tid < P ? tid : 0)] == slot + tid;
+      const uint32_t ok = __ballot_sync(kFull, on);
+      if (lane == 0) s_ok[warp] = ok;
+      __syncthreads();
+      int n = 0;
+#pragma unroll
+      for (int v = 0; v < kStoreThreads / 32; ++v) {
+        if (n == 32 * v) n += s_ok[v] == kFull ? 32 : __ffs(static_cast<int>(~s_ok[v])) - 1;
+      }
+      const long long page_head = static_cast<long long>(slot / P) * p.heads + head;
+      const float had = place > 0 ? scales[page_head] : 0.0f;
+      uint4 v[kItems];
+      uint32_t top = 0u;
+#pragma unroll
+      for (int it = 0; it < kItems; ++it) {
+        const int item = it * kStoreThreads + tid, row = item / kRowChunks;
+        v[it] = make_uint4(0u, 0u, 0u, 0u);
+        if (row < n) v[it] = __ldcs(reinterpret_cast<const uint4*>(x + (t0 + j + row) * stride + head * D) + item % kRowChunks);
+      }
+#pragma unroll
+      for (int it = 0; it < kItems; ++it) {
+        const uint32_t words[4] = {v[it].x, v[it].y, v[it].z, v[it].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t lo = words[k] & 0x7fffu, hi = (words[k] >> 16) & 0x7fffu;
+          if (lo < Elem<BF16>::kInfPattern) top = max(top, lo);
+          if (hi < Elem<BF16>::kInfPattern) top = max(top, hi);
+        }
+      }
+      top = __reduce_max_sync(kFull, top);
+      if (lane == 0) s_max[warp] = top;
+      __syncthreads();
+#pragma unroll
+      for (int u = 0; u < kStoreThreads / 32; ++u) top = max(top, s_max[u]);
+      const float scale = fmaxf(fmaxf(Elem<BF16>::pattern_f32(top) / 127.0f, kScaleFloor), had);
+      const float inverse = 1.0f / scale;
+      int8_t* const page_codes = codes + page_head * (P * D);
+#pragma unroll
+      for (int it = 0; it < kItems; ++it) {
+        const int item = it * kStoreThreads + tid, row = item / kRowChunks;
+        if (row >= n) continue;
+        const uint32_t words[4] = {v[it].x, v[it].y, v[it].z, v[it].w};
+        uint32_t out[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t a = code_of(Elem<BF16>::lo_f32(words[2 * k]), inverse) | code_of(Elem<BF16>::hi_f32(words[2 * k]), inverse) << 8;
+          const uint32_t b = code_of(Elem<BF16>::lo_f32(words[2 * k + 1]), inverse) | code_of(Elem<BF16>::hi_f32(words[2 * k + 1]), inverse) << 8;
+          out[k] = a | b << 16;
+        }
+        *reinterpret_cast<uint2*>(page_codes + (place + row) * D + (item % kRowChunks) * 8) = make_uint2(out[0], out[1]);
+      }
+      if (place > 0 && scale != had) {
+        const float ratio = had / scale;
+        for (int item = tid; item < place * (D / 16); item += kStoreThreads) {
+          uint4* const at = reinterpret_cast<uint4*>(page_codes) + item;
+          uint4 c = *at;
+          uint32_t words[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            uint32_t w4 = 0u;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) w4 |= code_of(static_cast<float>(signed_byte(words[k], b)), ratio) << (8 * b);
+            words[k] = w4;
+          }
+          *at = make_uint4(words[0], words[1], words[2], words[3]);
+        }
+      }
+      if (tid == 0) scales[page_head] = scale;
+      __syncthreads();  // s_ok and s_max are free again
+    }
+  }
+}
+
+// ---- reading tokens back -------------------------------------------------------------------------
+
+constexpr int kLoadThreads = 256;
+
+struct LoadParams {
+  const int8_t *k_codes, *v_codes;
+  const float *k_scale, *v_scale;
+  uint16_t *k, *v;
+  long long k_stride, v_stride, tokens;
+  const int32_t* slots;
+  int32_t heads, page_shift, block;  // tokens per CTA
+  uint32_t n_slots;
+};
+
+// A thread per 16 codes: one 16-byte load, two 16-byte stores.  Bound by HBM.
+template <bool BF16, int D>
+__global__ void __launch_bounds__(kLoadThreads) load_kernel(const LoadParams p) {
+  launch_dependents();
+  wait_for_prior_grids();
+  const uint32_t row = static_cast<uint32_t>(p.heads) * (D / 16);          // chunks of a token's keys
+  const long long t0 = static_cast<long long>(blockIdx.x) * p.block;
+  const uint32_t rows = static_cast<uint32_t>(min(static_cast<long long>(p.block), p.tokens - t0));
+  for (uint32_t item = threadIdx.x; item < rows * row * 2u; item += kLoadThreads) {
+    const uint32_t which = item >= rows * row ? 1u : 0u, in = item - which * rows * row;
+    const uint32_t r = in / row, chunk = in - r * row, head = chunk / (D / 16), c = chunk % (D / 16);
+    const uint32_t slot = static_cast<uint32_t>(p.slots[t0 + r]);
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+    float scale = 0.0f;
+    if (slot < p.n_slots) {
+      const long long page_head = static_cast<long long>(slot >> p.page_shift) * p.heads + head;
+      const uint4 v = __ldcs(reinterpret_cast<const uint4*>((which ? p.v_codes : p.k_codes) + ((page_head << p.page_shift) + (slot & ((1u << p.page_shift) - 1u))) * D) + c);
+      scale = (which ? p.v_scale : p.k_scale)[page_head];
+      w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    }
+    uint32_t out[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      out[k] = Elem<BF16>::pack_rn(static_cast<float>(signed_byte(w[k / 2], (k & 1) * 2)) * scale,
+                                   static_cast<float>(signed_byte(w[k / 2], (k & 1) * 2 + 1)) * scale);
+    }
+    uint4* const to = reinterpret_cast<uint4*>((which ? p.v : p.k) + (t0 + r) * (which ? p.v_stride : p.k_stride) + head * D + c * 16);
+    __stcs(to, make_uint4(out[0], out[1], out[2], out[3]));
+    __stcs(to + 1, make_uint4(out[4], out[5], out[6], out[7]));
+  }
+}
+
+// ---- host side -----------------------------------------------------------------------------------
+
+constexpr int kMaxSlots = 0x7fffffff;
+
+bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+int page_shift(int32_t page_tokens) {
+  for (int s = 4; s <= 7; ++s) {
+    if (page_tokens == 1 << s) return s;
+  }
+  return -1;
+}
+
+tsq_status_t check_cache(const tsq_cache_t* c) {
+  if (!c || (c->dtype != TSQ_F16 && c->dtype != TSQ_BF16) || c->kv_heads < 1 || c->head_dim < 1 || c->page_tokens < 1 || c->pages < 1)
+    return TSQ_ERR_INVALID_ARG;
+  if (!c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale) return TSQ_ERR_INVALID_ARG;
+  if (!aligned(c->k_codes, 16) || !aligned(c->v_codes, 16) || !aligned(c->k_scale, 4) || !aligned(c->v_scale, 4)) return TSQ_ERR_INVALID_ARG;
+  if ((c->head_dim != 64 && c->head_dim != 128) || page_shift(c->page_tokens) < 0) return TSQ_ERR_UNSUPPORTED;
+  if (c->kv_heads > 1024) return TSQ_ERR_UNSUPPORTED;
+  if (c->pages > kMaxSlots / c->page_tokens) return TSQ_ERR_INVALID_ARG;
+  return TSQ_OK;
+}
+
+// Rows of `heads` heads with `stride` elements between tokens.
+bool rows_fit(const void* x, long long stride, long long tokens, long long heads, int head_dim) {
+  return tokens == 0 || (x && aligned(x, 16) && stride % 8 == 0 && stride >= heads * head_dim);
+}
+
+// SMs of the current device, asked for once per device.
+int current_sms() {
+  static std::atomic<int> known[kMaxDevices];
+  int device = 0;
+  if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= kMaxDevices) return 0;
+  int n = known[device].load(std::memory_order_relaxed);
+  if (n == 0) {
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return 0;
+    known[device].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
+// The result of a launch; a failed one leaves nothing behind for the caller's own error checks.
+tsq_status_t launched(cudaError_t e) {
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    return TSQ_ERR_CUDA;
+  }
+  count_launch();
+  return TSQ_OK;
+}
+
+template <bool BF16, int D>
+cudaError_t launch_store(const StoreParams& p, int shift, int grid, cudaStream_t stream) {
+  switch (shift) {
+    case 4: return launch_overlapped(store_kernel<BF16, D, 16>, grid, kStoreThreads, 0, stream, p);
+    case 5: return launch_overlapped(store_kernel<BF16, D, 32>, grid, kStoreThreads, 0, stream, p);
+    case 6: return launch_overlapped(store_kernel<BF16, D, 64>, grid, kStoreThreads, 0, stream, p);
+    default: return launch_overlapped(store_kernel<BF16, D, 128>, grid, kStoreThreads, 0, stream, p);
+  }
+}
+
+size_t workspace_counters(int sms) { return static_cast<size_t>(align16(4ull * kRowsCtasPerSm * sms)); }
+size_t workspace_size(int sms, int head_dim) {
+  return workspace_counters(sms) + static_cast<size_t>(align16(8ull * kRowsCtasPerSm * sms * rows_slot_floats(head_dim)));
+}
+
+}  // namespace
+}  // namespace tsq
+
+using namespace tsq;
+
+extern "C" {
+
+tsq_status_t tsq_cache_slots(int32_t page_tokens, const int32_t* held, const int32_t* added, int32_t requests, const int32_t* free_pages, int32_t n_free,
+                             int32_t* query_start, int32_t* lengths, int32_t* block_table, int32_t table_pages, int32_t* slots, int64_t tokens,
+                             int32_t* taken, void* cuda_stream) {
+  if (page_tokens < 1 || requests < 0 || n_free < 0 || table_pages < 0 || tokens < 0 || tokens > kMaxSlots || !query_start || !taken) return TSQ_ERR_INVALID_ARG;
+  if (page_shift(page_tokens) < 0 || requests > kMaxRequests) return TSQ_ERR_UNSUPPORTED;
+  if (requests > 0 && (!held || !added || !lengths || (table_pages > 0 && !block_table))) return TSQ_ERR_INVALID_ARG;
+  if ((n_free > 0 && !free_pages) || (tokens > 0 && !slots)) return TSQ_ERR_INVALID_ARG;
+  for (const void* a : {static_cast<const void*>(held), static_cast<const void*>(added), static_cast<const void*>(free_pages), static_cast<const void*>(query_start),
+                        static_cast<const void*>(lengths), static_cast<const void*>(block_table), static_cast<const void*>(slots), static_cast<const void*>(taken)}) {
+    if (!aligned(a, 4)) return TSQ_ERR_INVALID_ARG;
+  }
+  SlotParams p;
+  std::memset(&p, 0, sizeof p);
+  p.held = held;
+  p.added = added;
+  p.free_pages = free_pages;
+  p.query_start = query_start;
+  p.lengths = lengths;
+  p.table = block_table;
+  p.slots = slots;
+  p.taken = taken;
+  p.tokens = tokens;
+  p.requests = requests;
+  p.n_free = n_free;
+  p.table_pages = table_pages;
+  p.page_shift = page_shift(page_tokens);
+  const size_t smem = 4ull * (2ull * static_cast<size_t>(requests) + 1ull);
+  if (smem > 48 * 1024 && cudaFuncSetAttribute(slots_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
+    return launched(cudaErrorInvalidValue);
+  const int grid = tokens > 0 ? static_cast<int>((tokens + kSlotTokens - 1) / kSlotTokens) : 1;
+  return launched(launch_overlapped(slots_kernel, grid, kSlotThreads, smem, static_cast<cudaStream_t>(cuda_stream), p));
+}
+
+tsq_status_t tsq_cache_store(const tsq_cache_t* cache, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int64_t tokens, const int32_t* slots,
+                             void* cuda_stream) {
+  const tsq_status_t fine = check_cache(cache);
+  if (fine != TSQ_OK) return fine;
+  if (tokens < 0 || tokens > kMaxSlots || (tokens > 0 && (!slots || !aligned(slots, 4)))) return TSQ_ERR_INVALID_ARG;
+  if (!rows_fit(k, k_stride, tokens, cache->kv_heads, cache->head_dim) || !rows_fit(v, v_stride, tokens, cache->kv_heads, cache->head_dim)) return TSQ_ERR_INVALID_ARG;
+  if (tokens == 0) return TSQ_OK;
+  const int sms = current_sms();
+  if (sms < 1) return launched(cudaErrorInvalidDevice);
+  StoreParams p;
+  std::memset(&p, 0, sizeof p);
+  p.k = static_cast<const uint16_t*>(k);
+  p.v = static_cast<const uint16_t*>(v);
+  p.k_codes = cache->k_codes;
+  p.v_codes = cache->v_codes;
+  p.k_scale = cache->k_scale;
+  p.v_scale = cache->v_scale;
+  p.k_stride = k_stride;
+  p.v_stride = v_stride;
+  p.tokens = tokens;
+  p.slots = slots;
+  p.heads = cache->kv_heads;
+  p.n_slots = static_cast<uint32_t>(cache->pages * cache->page_tokens);
+  const long long parts = 2ll * cache->kv_heads;
+  int block = 1;
+  while (block < kStoreBlock && tokens * parts > 8ll * sms * block) block *= 2;
+  p.block = block;
+  const long long grid = (tokens + block - 1) / block * parts;
+  if (grid > kMaxSlots) return TSQ_ERR_UNSUPPORTED;
+  const int shift = page_shift(cache->page_tokens);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const bool bf16 = cache->dtype == TSQ_BF16;
+  cudaError_t e;
+  if (cache->head_dim == 128) {
+    e = bf16 ? launch_store<true, 128>(p, shift, static_cast<int>(grid), st) : launch_store<false, 128>(p, shift, static_cast<int>(grid), st);
+  } else {
+    e = bf16 ? launch_store<true, 64>(p, shift, static_cast<int>(grid), st) : launch_store<false, 64>(p, shift, static_cast<int>(grid), st);
+  }
+  return launched(e);
+}
+
+tsq_status_t tsq_cache_load(const tsq_cache_t* cache, const int32_t* slots, int64_t tokens, void* k, int64_t k_stride, void* v, int64_t v_stride,
+                            void* cuda_stream) {
+  const tsq_status_t fine = check_cache(cache);
+  if (fine != TSQ_OK) return fine;
+  if (tokens < 0 || tokens > kMaxSlots || (tokens > 0 && (!slots || !aligned(slots, 4)))) return TSQ_ERR_INVALID_ARG;
+  if (!rows_fit(k, k_stride, tokens, cache->kv_heads, cache->head_dim) || !rows_fit(v, v_stride, tokens, cache->kv_heads, cache->head_dim)) return TSQ_ERR_INVALID_ARG;
+  if (tokens == 0) return TSQ_OK;
+  LoadParams p;
+  std::memset(&p, 0, sizeof p);
+  p.k_codes = cache->k_codes;
+  p.v_codes = cache->v_codes;
+  p.k_scale = cache->k_scale;
+  p.v_scale = cache->v_scale;
+  p.k = static_cast<uint16_t*>(k);
+  p.v = static_cast<uint16_t*>(v);
+  p.k_stride = k_stride;
+  p.v_stride = v_stride;
+  p.tokens = tokens;
+  p.slots = slots;
+  p.heads = cache->kv_heads;
+  p.page_shift = page_shift(cache->page_tokens);
+  p.n_slots = static_cast<uint32_t>(cache->pages * cache->page_tokens);
+  const int row = 2 * cache->kv_heads * (cache->head_dim / 16);
+  p.block = std::max(1, 4 * kLoadThreads / row);
+  const int grid = static_cast<int>((tokens + p.block - 1) / p.block);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const bool bf16 = cache->dtype == TSQ_BF16;
+  cudaError_t e;
+  if (cache->head_dim == 128) {
+    e = bf16 ? launch_overlapped(load_kernel<true, 128>, grid, kLoadThreads, 0, st, p) : launch_overlapped(load_kernel<false, 128>, grid, kLoadThreads, 0, st, p);
+  } else {
+    e = bf16 ? launch_overlapped(load_kernel<true, 64>, grid, kLoadThreads, 0, st, p) : launch_overlapped(load_kernel<false, 64>, grid, kLoadThreads, 0, st, p);
+  }
+  return launched(e);
+}
+
+static tsq_status_t check_attention_sizes(const tsq_cache_t* cache, int64_t tokens, int32_t q_heads, int32_t requests, int32_t max_query) {
+  const tsq_status_t fine = check_cache(cache);
+  if (fine != TSQ_OK) return fine;
+  if (tokens < 0 || tokens > kMaxSlots || requests < 0 || max_query < 1 || q_heads < 1 || q_heads % cache->kv_heads != 0) return TSQ_ERR_INVALID_ARG;
+  return q_heads / cache->kv_heads > 64 || requests > kMaxRequests ? TSQ_ERR_UNSUPPORTED : TSQ_OK;
+}
+
+tsq_status_t tsq_cache_workspace(const tsq_cache_t* cache, int64_t tokens, int32_t q_heads, int32_t requests, int32_t max_query, size_t* workspace_bytes) {
+  if (!workspace_bytes) return TSQ_ERR_INVALID_ARG;
+  const tsq_status_t fine = check_attention_sizes(cache, tokens, q_heads, requests, max_query);
+  if (fine != TSQ_OK) return fine;
+  const int sms = current_sms();
+  if (sms < 1) return launched(cudaErrorInvalidDevice);
+  *workspace_bytes = workspace_size(sms, cache->head_dim);
+  return TSQ_OK;
+}
+
+tsq_status_t tsq_cache_workspace_init(void* ws_dev, size_t ws_bytes, void* cuda_stream) {
+  if (!ws_dev || !aligned(ws_dev, 16)) return TSQ_ERR_INVALID_ARG;
+  const int sms = current_sms();
+  if (sms < 1) return launched(cudaErrorInvalidDevice);
+  if (ws_bytes < workspace_counters(sms)) return TSQ_ERR_BUFFER_TOO_SMALL;
+  if (cudaMemsetAsync(ws_dev, 0, workspace_counters(sms), static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) {
+    cudaGetLastError();
+    return TSQ_ERR_CUDA;
+  }
+  return TSQ_OK;
+}
+
+tsq_status_t tsq_cache_attention(const tsq_cache_t* cache, const void* q, int64_t q_stride, int32_t q_heads, int64_t tokens, const int32_t* query_start,
+                                 const int32_t* lengths, int32_t requests, int32_t max_query, const int32_t* block_table, int32_t table_pages, float scale,
+                                 void* out, int64_t out_stride, void* ws_dev, size_t ws_bytes, void* cuda_stream) {
+  const tsq_status_t fine = check_attention_sizes(cache, tokens, q_heads, requests, max_query);
+  if (fine != TSQ_OK) return fine;
+  if (table_pages < 0 || !(std::fabs(scale) <= 3.0e38f) || !ws_dev || !aligned(ws_dev, 16)) return TSQ_ERR_INVALID_ARG;
+  if (requests > 0 && (!query_start || !lengths || (table_pages > 0 && !block_table))) return TSQ_ERR_INVALID_ARG;
+  if (!aligned(query_start, 4) || !aligned(lengths, 4) || !aligned(block_table, 4)) return TSQ_ERR_INVALID_ARG;
+  if (!rows_fit(q, q_stride, tokens, q_heads, cache->head_dim) || !rows_fit(out, out_stride, tokens, q_heads, cache->head_dim)) return TSQ_ERR_INVALID_ARG;
+  const int sms = current_sms();
+  if (sms < 1) return launched(cudaErrorInvalidDevice);
+  if (ws_bytes < workspace_size(sms, cache->head_dim)) return TSQ_ERR_BUFFER_TOO_SMALL;
+  if (requests == 0 || tokens == 0) return TSQ_OK;
+  AttentionParams p;
+  std::memset(&p, 0, sizeof p);
+  p.q = q;
+  p.out = out;
+  p.query_start = query_start;
+  p.lengths = lengths;
+  p.table = block_table;
+  p.k_codes = cache->k_codes;
+  p.v_codes = cache->v_codes;
+  p.k_scale = cache->k_scale;
+  p.v_scale = cache->v_scale;
+  p.q_stride = q_stride;
+  p.out_stride = out_stride;
+  p.tokens = tokens;
+  p.requests = requests;
+  p.pages = static_cast<int32_t>(cache->pages);
+  p.page_shift = page_shift(cache->page_tokens);
+  p.table_pages = table_pages;
+  p.kv_heads = cache->kv_heads;
+  p.group = q_heads / cache->kv_heads;
+  p.max_query = max_query;
+  p.scale_log2 = scale * 1.4426950408889634f;
+  p.counters = static_cast<unsigned int*>(ws_dev);
+  p.partials = reinterpret_cast<float*>(static_cast<unsigned char*>(ws_dev) + workspace_counters(sms));
+  return launched(launch_attention_rows(p, cache->dtype == TSQ_BF16, cache->head_dim, kRowsCtasPerSm * sms, static_cast<cudaStream_t>(cuda_stream)));
+}
+
+}  // extern "C"

@@ -1,0 +1,124 @@
+// Device-side parts that the kernels of attention over the paged 8-bit cache share.
+#ifndef TSQ_CACHE_DEVICE_CUH_
+#define TSQ_CACHE_DEVICE_CUH_
+
+#include "tsq_cache.h"
+#include "tsq_device.cuh"
+
+namespace tsq {
+
+// A page's scale of 0 counts as this in the logarithm and the inverse: its codes still add nothing that binary32 sums would keep.
+constexpr float kLeastScale = 7.888609052210118e-31f;  // 2^-100
+
+// A request as the kernels read it: every number is brought into the range of the arrays first.
+struct Request {
+  long long start;   // first row
+  int rows;          // rows that are written
+  int keys;          // keys that can be seen: within the table
+  long long before;  // position of row 0 (negative: rows that see nothing)
+
+  __device__ __forceinline__ int tiles(int tile, const AttentionParams& p) const {
+    return static_cast<int>((static_cast<long long>(rows) * p.group + tile - 1) / tile);
+  }
+  __device__ __forceinline__ int key_units(int unit) const { return keys > 0 ? (keys - 1) / unit + 1 : 1; }
+  __device__ __forceinline__ unsigned long long units(int tile, int unit, const AttentionParams& p) const {
+    return rows == 0 ? 0ull : static_cast<unsigned long long>(tiles(tile, p)) * static_cast<unsigned>(key_units(unit)) * static_cast<unsigned>(p.kv_heads);
+  }
+  // keys that row j sees
+  __device__ __forceinline__ int seen(int j) const { return static_cast<int>(max(0ll, min(static_cast<long long>(keys), before + j + 1))); }
+};
+
+__device__ __forceinline__ Request request_of(const AttentionParams& p, int i) {
+  Request r;
+  const long long begin = min(max(static_cast<long long>(p.query_start[i]), 0ll), p.tokens);
+  const long long end = min(max(static_cast<long long>(p.query_start[i + 1]), begin), p.tokens);
+  const long long length = max(p.lengths[i], 0);
+  r.start = begin;
+  r.rows = static_cast<int>(min(end - begin, static_cast<long long>(p.max_query)));
+  r.keys = static_cast<int>(min(length, static_cast<long long>(p.table_pages) << p.page_shift));
+  r.before = length - (end - begin);
+  return r;
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  uint32_t u;
+  memcpy(&u, &h, sizeof u);
+  return u;
+}
+__device__ __forceinline__ float quad_max(float v) {
+  v = fmaxf(v, __shfl_xor_sync(kFull, v, 1));
+  return fmaxf(v, __shfl_xor_sync(kFull, v, 2));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+  v += __shfl_xor_sync(kFull, v, 1);
+  return v + __shfl_xor_sync(kFull, v, 2);
+}
+
+// Two codes with their sign bit inverted (code + 128) as binary16 numbers: 0x6400 + byte is 1024 + code + 128, and the difference to 1152 is exact.
+__device__ __forceinline__ uint32_t less_1152(uint32_t pair) {
+  const __half2 d = __hsub2(Elem<false>::as2(pair), Elem<false>::as2(0x64806480u));
+  return Elem<false>::bits(d);
+}
+__device__ __forceinline__ uint32_t widen_lo(uint32_t u) { return less_1152(__byte_perm(u, 0x64646464u, 0x4140)); }
+__device__ __forceinline__ uint32_t widen_hi(uint32_t u) { return less_1152(__byte_perm(u, 0x64646464u, 0x4342)); }
+
+// Power of two that brings a row whose largest magnitude is `top` to just below 2^15 (2^112 at most), and the inverse.  Both stay in binary32's normal range; a row that is zero or not
+// finite is left alone.
+__device__ __forceinline__ float row_power(float top, float& inverse) {
+  const int e = static_cast<int>(__float_as_uint(top) >> 23);              // biased exponent; 0: below the normal range
+  const bool plain = e > 0 && e < 255;
+  const int up = plain ? min(14 - (e - 127), 112) : 0;
+  inverse = __uint_as_float(static_cast<uint32_t>(127 - up) << 23);
+  return __uint_as_float(static_cast<uint32_t>(127 + up) << 23);
+}
+
+// The A operands of the products with the keys: rows row0 + g and row0 + g + 8 of the tile (zeros past its `rows`), for thread c of a row's four the dimensions
+// c * D / 4 ... in order, four per product step; brought to binary16 by a power of two per row, whose inverse is the row's factor.
+template <bool BF16, int D>
+__device__ __forceinline__ void load_queries(const AttentionParams& p, const Request& r, int head, int row0, int rows, int g, int c, uint32_t (&qa)[D / 16][4],
+                                             float& factor_a, float& factor_b) {
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int row = g + 8 * half, at = row0 + row;
+    uint32_t w[D / 8];
+    if (row < rows) {
+      const uint16_t* const from = static_cast<const uint16_t*>(p.q) + (r.start + at / p.group) * p.q_stride +
+                                   (static_cast<long long>(head) * p.group + at % p.group) * D + c * (D / 4);
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k) {
+        const uint4 v = reinterpret_cast<const uint4*>(from)[k];
+        w[4 * k] = v.x, w[4 * k + 1] = v.y, w[4 * k + 2] = v.z, w[4 * k + 3] = v.w;
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < D / 8; ++k) w[k] = 0u;
+    }
+    uint32_t top = 0u;
+#pragma unroll
+    for (int k = 0; k < D / 8; ++k) top = max(top, max(w[k] & 0x7fffu, (w[k] >> 16) & 0x7fffu));
+    top = max(top, __shfl_xor_sync(kFull, top, 1));
+    top = max(top, __shfl_xor_sync(kFull, top, 2));
+    float factor;
+    const float power = row_power(Elem<BF16>::pattern_f32(top), factor);
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+      qa[k][half] = pack_half2(Elem<BF16>::lo_f32(w[2 * k]) * power, Elem<BF16>::hi_f32(w[2 * k]) * power);
+      qa[k][2 + half] = pack_half2(Elem<BF16>::lo_f32(w[2 * k + 1]) * power, Elem<BF16>::hi_f32(w[2 * k + 1]) * power);
+    }
+    if (half == 0) {
+      factor_a = factor;
+    } else {
+      factor_b = factor;
+    }
+  }
+}
+
+}  // namespace tsq
+
+#endif  // TSQ_CACHE_DEVICE_CUH_
