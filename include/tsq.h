@@ -325,6 +325,7 @@ tsq_status_t tsq_cache_load(const tsq_cache_t *cache, const int32_t *slots, int6
  * 64 times; query head h reads key head h / (q_heads / kv_heads).  Request i owns the rows query_start[i] .. query_start[i + 1) and has lengths[i]
  * tokens in the cache, its own of this step among them; its row j is the token at position lengths[i] - n_i + j and sees the positions up to its own:
  *   out = sum_p softmax_p(scale * <q, k_p>) v_p
+ * A value scale below 2^-60 counts as 2^-60; the scales of the value pages that a row sees may differ by a factor of 2^80.
  * Rows that see no key (n_i > lengths[i]) are written as zeros, rows behind the last request's are left as they were.  Scores, the softmax's
  * sum and the accumulators are binary32; weights are rounded to binary16, relative to the largest of their row times its page's scale.
  * A page outside the cache in block_table, and what lies past table_pages, is not seen.  Codes and scales behind a request's last token are not used, whatever they hold.
@@ -338,6 +339,11 @@ tsq_status_t tsq_cache_load(const tsq_cache_t *cache, const int32_t *slots, int6
 tsq_status_t tsq_cache_workspace(const tsq_cache_t *cache, int64_t tokens, int32_t q_heads, int32_t requests, int32_t max_query,
                                  size_t *workspace_bytes);
 tsq_status_t tsq_cache_workspace_init(void *ws_dev, size_t ws_bytes, void *cuda_stream);
+/*
+ * TSQ_OK, or TSQ_ERR_TIMEOUT if a wait inside an attention call's kernel ran out since the workspace was initialised (every wait is for the call's own work: it
+ * cannot in a sound call).  Synchronises `cuda_stream`; `status` is HOST.
+ */
+tsq_status_t tsq_cache_workspace_status(const void *ws_dev, uint32_t *status, void *cuda_stream);
 tsq_status_t tsq_cache_attention(const tsq_cache_t *cache, const void *q, int64_t q_stride, int32_t q_heads, int64_t tokens,
                                  const int32_t *query_start, const int32_t *lengths, int32_t requests, int32_t max_query,
                                  const int32_t *block_table, int32_t table_pages, float scale, void *out,

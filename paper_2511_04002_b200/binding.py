@@ -24,7 +24,7 @@ EXPORTS = ["tsq_plan", "tsq_plan_variant", "tsq_plan_sizes", "tsq_workspace_init
            "tsq_blob_info",
            "tsq_workspace_status", "tsq_encode_host", "tsq_decode_host", "tsq_kernel_launch_count",
            "tsq_plan_destroy", "tsq_status_string",
-           "tsq_cache_slots", "tsq_cache_store", "tsq_cache_load", "tsq_cache_workspace", "tsq_cache_workspace_init", "tsq_cache_attention",
+           "tsq_cache_slots", "tsq_cache_store", "tsq_cache_load", "tsq_cache_workspace", "tsq_cache_workspace_init", "tsq_cache_workspace_status", "tsq_cache_attention",
            "tsq_model_kv_bits", "tsq_model_io_bits", "tsq_model_outage", "tsq_model_latency", "tsq_model_best_rate"]
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtsq.so")
@@ -90,8 +90,10 @@ def lib() -> C.CDLL:
     L.tsq_cache_load.argtypes = [cache, ip, i64, vp, i64, vp, i64, vp]
     L.tsq_cache_workspace.argtypes = [cache, i64, i32, i32, i32, C.POINTER(sz)]
     L.tsq_cache_workspace_init.argtypes = [vp, sz, vp]
+    L.tsq_cache_workspace_status.argtypes = [vp, C.POINTER(C.c_uint32), vp]
     L.tsq_cache_attention.argtypes = [cache, vp, i64, i32, i64, ip, ip, i32, i32, ip, i32, C.c_float, vp, i64, vp, sz, vp]
-    for name in ("tsq_cache_slots", "tsq_cache_store", "tsq_cache_load", "tsq_cache_workspace", "tsq_cache_workspace_init", "tsq_cache_attention"):
+    for name in ("tsq_cache_slots", "tsq_cache_store", "tsq_cache_load", "tsq_cache_workspace", "tsq_cache_workspace_init", "tsq_cache_workspace_status",
+                 "tsq_cache_attention"):
         getattr(L, name).restype = C.c_int
     L.tsq_model_kv_bits.argtypes = [i64, i32, i32, i32, i64, d, d]
     L.tsq_model_io_bits.argtypes = [i64, i32, i32, i32, i64, d, d, i32]
@@ -288,6 +290,12 @@ class Cache:
     def workspace_init(self, ws: torch.Tensor, stream=None) -> None:
         with torch.cuda.device(self.device):
             _check(lib().tsq_cache_workspace_init(ws.data_ptr(), ws.numel(), _stream(stream)), "tsq_cache_workspace_init")
+
+    def workspace_status(self, ws: torch.Tensor, stream=None) -> int:
+        out = C.c_uint32(0)
+        with torch.cuda.device(self.device):
+            _check(lib().tsq_cache_workspace_status(ws.data_ptr(), C.byref(out), _stream(stream)), "tsq_cache_workspace_status")
+        return int(out.value)
 
     def attention(self, q: torch.Tensor, query_start: torch.Tensor, lengths: torch.Tensor, block_table: torch.Tensor, out: torch.Tensor,
                   ws: torch.Tensor, max_query: int, scale: Optional[float] = None, stream=None) -> None:

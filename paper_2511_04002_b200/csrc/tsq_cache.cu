@@ -371,9 +371,12 @@ cudaError_t launch_store(const StoreParams& p, int shift, int grid, cudaStream_t
   }
 }
 
-size_t workspace_counters(int sms) { return static_cast<size_t>(align16(4ull * kRowsCtasPerSm * sms)); }
-size_t workspace_size(int sms, int head_dim) {
-  return workspace_counters(sms) + static_cast<size_t>(align16(8ull * kRowsCtasPerSm * sms * rows_slot_floats(head_dim)));
+// Workspace: 16 bytes with the status, the counters of either kernel, the slots of sums.
+bool few_query_rows(long long max_query, int group) { return max_query * group <= kRowsTile; }
+size_t workspace_head(int sms) { return static_cast<size_t>(align16(16ull + 4ull * sms * std::max(kRowsCtasPerSm * kRowsCounters, kTilesCounters))); }
+size_t workspace_size(int sms, int head_dim, bool few) {
+  const unsigned long long rows = few ? 1ull * kRowsCtasPerSm * kRowsSlots * kRowsTile : 128ull * kTilesSlots;
+  return workspace_head(sms) + static_cast<size_t>(align16(4ull * rows * sms * (head_dim + 2)));
 }
 
 }  // namespace
@@ -506,7 +509,7 @@ tsq_status_t tsq_cache_workspace(const tsq_cache_t* cache, int64_t tokens, int32
   if (fine != TSQ_OK) return fine;
   const int sms = current_sms();
   if (sms < 1) return launched(cudaErrorInvalidDevice);
-  *workspace_bytes = workspace_size(sms, cache->head_dim);
+  *workspace_bytes = workspace_size(sms, cache->head_dim, few_query_rows(max_query, q_heads / cache->kv_heads));
   return TSQ_OK;
 }
 
@@ -514,8 +517,8 @@ tsq_status_t tsq_cache_workspace_init(void* ws_dev, size_t ws_bytes, void* cuda_
   if (!ws_dev || !aligned(ws_dev, 16)) return TSQ_ERR_INVALID_ARG;
   const int sms = current_sms();
   if (sms < 1) return launched(cudaErrorInvalidDevice);
-  if (ws_bytes < workspace_counters(sms)) return TSQ_ERR_BUFFER_TOO_SMALL;
-  if (cudaMemsetAsync(ws_dev, 0, workspace_counters(sms), static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) {
+  if (ws_bytes < workspace_head(sms)) return TSQ_ERR_BUFFER_TOO_SMALL;
+  if (cudaMemsetAsync(ws_dev, 0, workspace_head(sms), static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) {
     cudaGetLastError();
     return TSQ_ERR_CUDA;
   }
@@ -533,7 +536,8 @@ tsq_status_t tsq_cache_attention(const tsq_cache_t* cache, const void* q, int64_
   if (!rows_fit(q, q_stride, tokens, q_heads, cache->head_dim) || !rows_fit(out, out_stride, tokens, q_heads, cache->head_dim)) return TSQ_ERR_INVALID_ARG;
   const int sms = current_sms();
   if (sms < 1) return launched(cudaErrorInvalidDevice);
-  if (ws_bytes < workspace_size(sms, cache->head_dim)) return TSQ_ERR_BUFFER_TOO_SMALL;
+  const bool few = few_query_rows(max_query, q_heads / cache->kv_heads);
+  if (ws_bytes < workspace_size(sms, cache->head_dim, few)) return TSQ_ERR_BUFFER_TOO_SMALL;
   if (requests == 0 || tokens == 0) return TSQ_OK;
   AttentionParams p;
   std::memset(&p, 0, sizeof p);
@@ -557,9 +561,22 @@ tsq_status_t tsq_cache_attention(const tsq_cache_t* cache, const void* q, int64_
   p.group = q_heads / cache->kv_heads;
   p.max_query = max_query;
   p.scale_log2 = scale * 1.4426950408889634f;
-  p.counters = static_cast<unsigned int*>(ws_dev);
-  p.partials = reinterpret_cast<float*>(static_cast<unsigned char*>(ws_dev) + workspace_counters(sms));
-  return launched(launch_attention_rows(p, cache->dtype == TSQ_BF16, cache->head_dim, kRowsCtasPerSm * sms, static_cast<cudaStream_t>(cuda_stream)));
+  p.status = static_cast<unsigned int*>(ws_dev);
+  p.counters = p.status + 4;
+  p.partials = reinterpret_cast<float*>(static_cast<unsigned char*>(ws_dev) + workspace_head(sms));
+  const bool bf16 = cache->dtype == TSQ_BF16;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  return launched(few ? launch_attention_rows(p, bf16, cache->head_dim, kRowsCtasPerSm * sms, st) : launch_attention_tiles(p, bf16, cache->head_dim, sms, st));
+}
+
+tsq_status_t tsq_cache_workspace_status(const void* ws_dev, uint32_t* status, void* cuda_stream) {
+  if (!ws_dev || !status || !aligned(ws_dev, 16)) return TSQ_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (cudaMemcpyAsync(status, ws_dev, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) {
+    cudaGetLastError();
+    return TSQ_ERR_CUDA;
+  }
+  return TSQ_OK;
 }
 
 }  // extern "C"

@@ -23,15 +23,21 @@ struct AttentionParams {
   int32_t requests, table_pages, pages, kv_heads, group, max_query;
   int32_t page_shift;                      // log2 of the page's tokens
   float scale_log2;                        // scale * log2(e)
-  unsigned int* counters;                  // one per CTA, 0 between calls
-  float* partials;                         // two slots per CTA
+  unsigned int* status;                    // of the workspace
+  unsigned int* counters;                  // 0 between calls
+  float* partials;                         // sums of tiles that several CTAs have a part of
 };
 
-// What a call of the row kernel needs of the workspace: a counter and two slots of 16 rows of accumulators, maxima and sums for every CTA.
+// Up to 16 query rows (query heads of a key head times max_query): tiles of 16 rows, three CTAs per SM.  A CTA has one counter and two slots of 16 rows of
+// accumulators, maxima and sums in the workspace.
 constexpr int kRowsCtasPerSm = 3;
 constexpr int kRowsTile = 16;
-inline size_t rows_slot_floats(int head_dim) { return static_cast<size_t>(kRowsTile) * (head_dim + 2); }
+constexpr int kRowsCounters = 1, kRowsSlots = 2;
+// More: tiles of 256 rows, one CTA per SM, a counter for each warp of 32 rows, four slots of 128 rows.
+constexpr int kTilesRows = 256;
+constexpr int kTilesCounters = 8, kTilesSlots = 4;
 cudaError_t launch_attention_rows(const AttentionParams& p, bool bf16, int head_dim, int ctas, cudaStream_t stream);
+cudaError_t launch_attention_tiles(const AttentionParams& p, bool bf16, int head_dim, int ctas, cudaStream_t stream);
 
 }  // namespace tsq
 

@@ -7,8 +7,9 @@
 
 namespace tsq {
 
-// A page's scale of 0 counts as this in the logarithm and the inverse: its codes still add nothing that binary32 sums would keep.
-constexpr float kLeastScale = 7.888609052210118e-31f;  // 2^-100
+// Weights are 2^(score + log2 s_v - m) and the softmax's sum takes them over s_v: both have to stay in binary32's range for every page that counts.  A values' scale below
+// this counts as this (tsq_cache_store's are 2^-40 at least): what its codes add is under 2^-53, and a page may lie 2^80 below another of the row before its keys leave the sum.
+constexpr float kLeastScale = 8.673617379884035e-19f;  // 2^-60
 
 // A request as the kernels read it: every number is brought into the range of the arrays first.
 struct Request {

@@ -1,0 +1,669 @@
+// Attention over the paged 8-bit cache for many query rows per request (prompts, chunks of prompts), on the tensor cores' asynchronous products.
+
+#include "tsq_cache.h"
+#include "tsq_cache_device.cuh"
+#include "tsq_device.cuh"
+#include "tsq_internal.h"
+
+namespace tsq {
+namespace {
+
+constexpr int kKeys = 128;                   // tokens of a step
+constexpr int kGranules = kKeys / 16;        // parts of a step that lie within one page
+constexpr int kThreads = 4 * 128;            // two softmax warpgroups, one that widens codes, one whose first warp issues the products
+// Registers: 128 a thread at launch, dealt out again among the four: 2 * 168 + 112 + 64 = 4 * 128.
+constexpr int kSoftmaxRegs = 168, kWidenRegs = 112, kProductRegs = 64;
+constexpr int kMeta = 4;                     // steps whose scales are kept
+constexpr uint32_t kPolls = 1u << 20;        // of a wait inside the CTA: tens of milliseconds at least, where a sound one takes microseconds
+
+// ---- barriers, tensor memory, products -----------------------------------------------------------
+
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("{\n\t.reg .b64 s;\n\tmbarrier.arrive.shared::cta.b64 s, [%0];\n\t}" ::"r"(bar) : "memory");
+}
+// Whether the phase of that parity has ended; false after kPolls polls.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
+  for (uint32_t n = 0; n < kPolls; ++n) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    if (done) return true;
+  }
+  return false;
+}
+
+template <int N>
+__device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+__device__ __forceinline__ void tm_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tm_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tm_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tm_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+#define TSQ_R8(v, i) "=r"(v[i]), "=r"(v[i + 1]), "=r"(v[i + 2]), "=r"(v[i + 3]), "=r"(v[i + 4]), "=r"(v[i + 5]), "=r"(v[i + 6]), "=r"(v[i + 7])
+#define TSQ_W8(v, i) "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]), "r"(v[i + 4]), "r"(v[i + 5]), "r"(v[i + 6]), "r"(v[i + 7])
+// 32 columns of the warp's 32 lanes
+__device__ __forceinline__ void tm_load32(uint32_t (&v)[32], uint32_t at) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, "
+      "[%32];"
+      : TSQ_R8(v, 0), TSQ_R8(v, 8), TSQ_R8(v, 16), TSQ_R8(v, 24)
+      : "r"(at));
+}
+__device__ __forceinline__ void tm_store32(uint32_t at, const uint32_t* v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
+      "%32};" ::"r"(at),
+      TSQ_W8(v, 0), TSQ_W8(v, 8), TSQ_W8(v, 16), TSQ_W8(v, 24)
+      : "memory");
+}
+
+__device__ __forceinline__ void tm_store16(uint32_t at, const uint32_t (&v)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at), TSQ_W8(v, 0), TSQ_W8(v, 8) : "memory");
+}
+__device__ __forceinline__ float4 shared_float4(uint32_t at) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at));
+  return v;
+}
+
+// Shared-memory descriptors of 128-byte swizzled operands: rows of 128 bytes, eight rows to a 1024-byte atom.
+// K-major (queries, keys): atoms follow one another down the rows.  MN-major (values: a row is a token, its 64 dimensions contiguous): atoms follow
+// one another along the tokens, the second 64 dimensions lie kHalf bytes behind.
+constexpr int kHalf = 128 * 128;             // 128 rows of 64 binary16 numbers
+__device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t leading, uint32_t stride) {
+  return static_cast<uint64_t>((at & 0x3ffffu) >> 4) | static_cast<uint64_t>(leading >> 4) << 16 | static_cast<uint64_t>(stride >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// Instruction descriptor: binary32 sums, binary16 operands, 128 rows.
+__host__ __device__ constexpr uint32_t product_of(int columns, bool b_mn_major) {
+  return 1u << 4 | (b_mn_major ? 1u << 16 : 0u) | static_cast<uint32_t>(columns / 8) << 17 | (128u / 16u) << 24;
+}
+__device__ __forceinline__ void product_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(what),
+               "r"(static_cast<uint32_t>(add))
+               : "memory");
+}
+__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(what),
+               "r"(static_cast<uint32_t>(add))
+               : "memory");
+}
+
+// ---- work ----------------------------------------------------------------------------------------
+
+// Steps of the tile of 256 rows that begins at row0: by the keys its last row sees, one at least.
+__device__ __forceinline__ int steps_of(const Request& r, long long rows, long long row0, const AttentionParams& p) {
+  const int seen = r.seen(static_cast<int>((min(rows, row0 + kTilesRows) - 1) / p.group));
+  return seen > 0 ? (seen - 1) / kKeys + 1 : 1;
+}
+
+// Where a CTA is in its share of the work.  Order: request, key head, tile of rows, step.
+struct Place {
+  int request, head, tile;
+  Request r;
+  long long rows;                 // rows of the request times the group
+  int steps;                      // of the tile
+  int k0, k1;                     // steps that the CTA takes of it
+  unsigned long long unit, end;   // the first of them; where the CTA's share ends
+
+  __device__ __forceinline__ void take(const AttentionParams& p) {
+    steps = steps_of(r, rows, static_cast<long long>(tile) * kTilesRows, p);
+    k1 = static_cast<int>(min(static_cast<unsigned long long>(steps), k0 + (end - unit)));
+  }
+  __device__ __forceinline__ bool next(const AttentionParams& p) {
+    unit += k1 - k0;
+    if (unit >= end) return false;
+    k0 = 0;
+    if (static_cast<long long>(++tile) * kTilesRows >= rows) {
+      tile = 0;
+      if (++head == p.kv_heads) {
+        head = 0;
+        do {
+          if (++request >= p.requests) return false;
+          r = request_of(p, request);
+        } while (r.rows == 0);
+        rows = static_cast<long long>(r.rows) * p.group;
+      }
+    }
+    take(p);
+    return true;
+  }
+  // steps of the half of the tile (128 rows) that group t has: as far as its last row sees, 0 where it has no row
+  __device__ __forceinline__ int limit(int t, const AttentionParams& p) const {
+    const long long row0 = static_cast<long long>(tile) * kTilesRows + 128 * t;
+    if (row0 >= rows) return 0;
+    const int seen = r.seen(static_cast<int>((min(rows, row0 + 128) - 1) / p.group));
+    return min(k1, seen > 0 ? (seen - 1) / kKeys + 1 : 1);
+  }
+};
+
+template <int D>
+struct Shared {
+  static constexpr int kHalves = D / 64;
+  static constexpr int kOperand = kHalves * kHalf;        // 128 rows of D binary16 numbers
+  static constexpr int kQ = 0, kK = 2 * kOperand, kV = 4 * kOperand;
+  static constexpr int kScales = 6 * kOperand;
+  static constexpr int kBars = kScales + kMeta * kGranules * 16;
+  static constexpr int kBytes = kBars + 256;
+};
+enum Bar { kKFull = 0, kKFree = 2, kVFull = 4, kVFree = 6, kSFull = 8, kPReady = 10, kODone = 12, kQFull = 14, kBarCount = 16 };
+
+// A CTA's two groups of 128 threads have 128 query rows each, a thread a row; a tile is the 256 rows of one (request, key head) that follow one another, the group's query
+// heads of a token side by side, so that widened codes serve both groups and all heads.  Per step of 128 tokens:
+//   widening group  codes from global memory (a step ahead in registers) to binary16 (exact) in shared memory, two buffers each for keys and values
+//   product warp    S = Q K^T into tensor memory for each group, then O += P V with P from tensor memory
+//   softmax groups  S out of tensor memory, w = 2^(S * scale + log2 s_v - m) to binary16 in S's place, sums in binary32
+// While one group works on its scores the tensor cores have the other's products.  m is a reference that follows the row's maximum only when a
+// score is more than 2^8 above it: then the step is done again and O is scaled in tensor memory.  Every CTA takes the same number of steps whatever the requests'
+// lengths are; tiles that several CTAs have a part of are added up through the workspace by the one that comes last, in the order of the steps.
+// Bound by the exponentials and by what surrounds them: 16 of them per SM and clock are 1024 clocks for a group's step, as long as its two products take.
+template <bool BF16, int D>
+__global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const AttentionParams p) {
+  using Sh = Shared<D>;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ unsigned long long s_scan[kThreads / 32], s_begin;
+  __shared__ uint32_t s_tmem, s_failed;
+  __shared__ int s_found;
+  launch_dependents();
+  wait_for_prior_grids();
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  const uint32_t smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
+  unsigned char* const smem_at = smem_raw + (smem - smem_addr(smem_raw));
+
+  // ---- this CTA's share ----
+  unsigned long long* const s_units = reinterpret_cast<unsigned long long*>(smem_at);
+  for (int i = warp; i < p.requests; i += kThreads / 32) {
+    const Request r = request_of(p, i);
+    const long long rows = static_cast<long long>(r.rows) * p.group;
+    unsigned long long sum = 0;
+    for (long long row0 = static_cast<long long>(lane) * kTilesRows; row0 < rows; row0 += 32ll * kTilesRows) sum += steps_of(r, rows, row0, p);
+#pragma unroll
+    for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(kFull, sum, d);
+    if (lane == 0) s_units[i] = sum;                       // of one key head
+  }
+  if (tid == 0) {
+    s_failed = 0u;
+    s_found = 0;
+    s_begin = 0;
+    const uint32_t bars = smem + Sh::kBars;
+    for (int i = 0; i < kBarCount; ++i) bar_init(bars + 8 * i, i < kKFree || (i >= kVFull && i < kVFree) || (i >= kPReady && i < kODone) || i >= kQFull ? 128u : 1u);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_proxy_async_smem();
+  }
+  __syncthreads();
+  unsigned long long total;
+  Place place;
+  {
+    const int per = (p.requests + kThreads - 1) / kThreads;
+    const int i0 = min(tid * per, p.requests), i1 = min(i0 + per, p.requests);
+    unsigned long long mine = 0;
+    for (int i = i0; i < i1; ++i) mine += s_units[i] * static_cast<unsigned>(p.kv_heads);
+    unsigned long long in = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+      const unsigned long long up = __shfl_up_sync(kFull, in, d);
+      if (lane >= d) in += up;
+    }
+    if (lane == 31) s_scan[warp] = in;
+    __syncthreads();
+    unsigned long long at = in - mine;
+    total = 0;
+    for (int w = 0; w < kThreads / 32; ++w) {
+      if (w < warp) at += s_scan[w];
+      total += s_scan[w];
+    }
+    const unsigned long long ctas = total < gridDim.x ? total : gridDim.x;
+    if (blockIdx.x >= ctas) return;
+    place.unit = blockIdx.x * total / ctas;
+    place.end = (blockIdx.x + 1) * total / ctas;
+    for (int i = i0; i < i1; ++i) {
+      const unsigned long long n = s_units[i] * static_cast<unsigned>(p.kv_heads);
+      if (at <= place.unit && place.unit < at + n) {
+        s_found = i;
+        s_begin = at;
+      }
+      at += n;
+    }
+    __syncthreads();
+  }
+  const unsigned long long ctas = total < gridDim.x ? total : gridDim.x;
+  {
+    place.request = s_found;
+    place.r = request_of(p, place.request);
+    place.rows = static_cast<long long>(place.r.rows) * p.group;
+    const unsigned long long of_head = s_units[place.request], in = place.unit - s_begin;
+    place.head = static_cast<int>(in / of_head);
+    unsigned long long rest = in % of_head;                // steps of this head's tiles in front of `unit`
+    // every warp by itself: 32 tiles at a time
+    int tile = 0;
+    for (;;) {
+      const long long row0 = static_cast<long long>(tile + lane) * kTilesRows;
+      const int n = row0 < place.rows ? steps_of(place.r, place.rows, row0, p) : 0;
+      int upto = n;
+#pragma unroll
+      for (int d = 1; d < 32; d *= 2) {
+        const int up = __shfl_up_sync(kFull, upto, d);
+        if (lane >= d) upto += up;
+      }
+      const uint32_t past = __ballot_sync(kFull, static_cast<unsigned long long>(upto) > rest);
+      if (past != 0u) {
+        const int l = __ffs(static_cast<int>(past)) - 1;
+        rest -= __shfl_sync(kFull, upto - n, l);
+        tile += l;
+        break;
+      }
+      rest -= __shfl_sync(kFull, upto, 31);
+      tile += 32;
+      if (static_cast<long long>(tile) * kTilesRows >= place.rows) {  // not reached: the request has the unit
+        tile = 0;
+        rest = 0;
+        break;
+      }
+    }
+    place.tile = tile;
+    place.k0 = static_cast<int>(rest);
+    place.take(p);
+  }
+  if (warp == 12) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tm_fence_before();
+  __syncthreads();
+  tm_fence_after();
+  const uint32_t tmem = s_tmem, bars = smem + Sh::kBars;
+  bool ok = true;
+  const unsigned long long share = place.unit;             // the CTA's first step
+  // a wait that runs out ends the warp's work, and the others' waits run out in turn
+  auto wait = [&](int bar, uint32_t parity) {
+    ok = __all_sync(kFull, ok && bar_wait(bars + 8 * bar, parity));
+    return ok;
+  };
+
+  if (warp < 8) {
+    // ---- softmax ----
+    regs_up<kSoftmaxRegs>();
+    const int t = warp / 4, row = tid % 128;
+    const uint32_t lanes = static_cast<uint32_t>(warp % 4) << 21;  // lane 32 * (warp % 4) in the upper half of an address
+    const uint32_t s_at = tmem + lanes + 128 * t, o_at = tmem + lanes + 256 + D * t;
+    uint32_t count = 0;                                    // steps of this group so far
+    do {
+      const int limit = place.limit(t, p);
+      const long long row0 = static_cast<long long>(place.tile) * kTilesRows + 128 * t;
+      if (row0 >= place.rows) continue;
+      const int rows = static_cast<int>(min(128ll, place.rows - row0));
+      const bool live = row < rows;
+      const long long at = row0 + min(row, rows - 1);
+      const int token = static_cast<int>(at / p.group), query_head = place.head * p.group + static_cast<int>(at % p.group);
+      const bool any = limit > place.k0;                   // the CTA has steps that this half of the tile sees
+      float m = 0.0f, l = 0.0f;
+      bool have = false;
+      if (any) {
+        // the row, brought to binary16 by a power of two
+        const uint16_t* const from = static_cast<const uint16_t*>(p.q) + (place.r.start + token) * p.q_stride + static_cast<long long>(query_head) * D;
+        uint32_t top = 0u;
+        uint4 v[D / 8];
+#pragma unroll
+        for (int k = 0; k < D / 8; ++k) {
+          v[k] = live ? reinterpret_cast<const uint4*>(from)[k] : make_uint4(0u, 0u, 0u, 0u);
+          const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7fffu, (w[e] >> 16) & 0x7fffu));
+        }
+        float factor;
+        const float power = row_power(Elem<BF16>::pattern_f32(top), factor);
+        const float sign = p.scale_log2 < 0.0f ? -power : power;  // the scores' factors below are not negative
+        unsigned char* const q_at = smem_at + Sh::kQ + t * Sh::kOperand;
+#pragma unroll
+        for (int k = 0; k < D / 8; ++k) {
+          const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+          uint32_t h[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) h[e] = pack_half2(Elem<BF16>::lo_f32(w[e]) * sign, Elem<BF16>::hi_f32(w[e]) * sign);
+          *reinterpret_cast<uint4*>(q_at + (k / 8) * kHalf + row * 128 + (((k % 8) ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+        }
+        fence_proxy_async_smem();
+        bar_arrive(bars + 8 * (kQFull + t));
+        const float by_scale = factor * fabsf(p.scale_log2);
+        const int seen = place.r.seen(token), seen_first = place.r.seen(static_cast<int>(row0 / p.group));
+        for (int j = place.k0; j < limit; ++j, ++count) {
+          if (!wait(kSFull + t, count & 1u)) break;
+          tm_fence_after();
+          const uint32_t scales = smem + Sh::kScales + static_cast<uint32_t>((place.unit + (j - place.k0) - share) % kMeta) * (kGranules * 16);
+          const bool mask = (j + 1) * kKeys > seen_first;
+          // the largest score: raw sums within a granule, which has one factor that is not negative
+          float most = -INFINITY;
+#pragma unroll
+          for (int chunk = 0; chunk < kKeys / 32; ++chunk) {
+            uint32_t s[32];
+            tm_load32(s, s_at + 32 * chunk);
+            tm_wait_ld();
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+              if (mask) {
+                const int left = seen - (j * kKeys + 32 * chunk + 16 * g);  // keys of the granule that the row sees
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[16 * g + e] = e < left ? s[16 * g + e] : 0xff800000u;
+              }
+              float raw = __uint_as_float(s[16 * g]);
+#pragma unroll
+              for (int e = 1; e < 15; e += 2) raw = fmaxf(raw, fmaxf(__uint_as_float(s[16 * g + e]), __uint_as_float(s[16 * g + e + 1])));
+              raw = fmaxf(raw, __uint_as_float(s[16 * g + 15]));
+              const float4 f = shared_float4(scales + 16 * (2 * chunk + g));  // score factor, log2 and inverse of the values' scale
+              const float x = __fmaf_rn(raw, f.x * by_scale, f.y);
+              most = fmaxf(most, raw == -INFINITY ? raw : x);
+            }
+          }
+          const bool up = have ? most > m + 8.0f : most > -INFINITY;
+          if (__any_sync(kFull, up)) {
+            float by = 1.0f;
+            if (up) {
+              by = have ? exp2_fast(m - most) : 0.0f;
+              m = most;
+              have = true;
+            }
+            l *= by;
+            if (j > place.k0) {                            // the sums so far follow the reference
+              if (!wait(kODone + t, (count - 1u) & 1u)) break;
+              tm_fence_after();
+#pragma unroll 1
+              for (int d = 0; d < D; d += 32) {
+                uint32_t o[32];
+                tm_load32(o, o_at + d);
+                tm_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
+                tm_store32(o_at + d, o);
+              }
+              tm_wait_st();
+            }
+          }
+          // weights: those of 32 scores take the place of 16
+#pragma unroll
+          for (int chunk = 0; chunk < kKeys / 32; ++chunk) {
+            uint32_t s[32], w[16];
+            tm_load32(s, s_at + 32 * chunk);
+            tm_wait_ld();
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+              const int left = mask ? seen - (j * kKeys + 32 * chunk + 16 * g) : 16;
+              const float4 f = shared_float4(scales + 16 * (2 * chunk + g));
+              const float a = f.x * by_scale, b = f.y - m;
+              float part = 0.0f;
+#pragma unroll
+              for (int e = 0; e < 16; e += 2) {
+                float x0 = __fmaf_rn(__uint_as_float(s[16 * g + e]), a, b), x1 = __fmaf_rn(__uint_as_float(s[16 * g + e + 1]), a, b);
+                if (mask) {
+                  x0 = e < left ? x0 : -INFINITY;
+                  x1 = e + 1 < left ? x1 : -INFINITY;
+                }
+                x0 = exp2_fast(x0);
+                x1 = exp2_fast(x1);
+                part += x0 + x1;
+                w[8 * g + e / 2] = pack_half2(x0, x1);
+              }
+              l = __fmaf_rn(part, f.z, l);
+            }
+            tm_store16(s_at + 16 * chunk, w);
+          }
+          tm_wait_st();
+          tm_fence_before();
+          bar_arrive(bars + 8 * (kPReady + t));
+        }
+        if (!wait(kODone + t, (count - 1u) & 1u)) break;
+        tm_fence_after();
+      }
+      // ---- the row, or its part ----
+      uint16_t* const to = static_cast<uint16_t*>(p.out) + (place.r.start + token) * p.out_stride + static_cast<long long>(query_head) * D;
+      if (place.k0 == 0 && place.k1 == place.steps) {
+        const float by = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll 1
+        for (int d = 0; d < D; d += 32) {
+          uint32_t o[32];
+          tm_load32(o, o_at + d);
+          tm_wait_ld();
+          if (live) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 8) {
+              uint32_t w[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) w[k] = Elem<BF16>::pack_rn(__uint_as_float(o[e + 2 * k]) * by, __uint_as_float(o[e + 2 * k + 1]) * by);
+              *reinterpret_cast<uint4*>(to + d + e) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          }
+        }
+        tm_fence_before();
+        continue;
+      }
+      // a slot holds columns of 128 rows: maxima, sums, then the dimensions
+      constexpr long long kSlot = 128ll * (D + 2);
+      float* const slot = p.partials + (4ll * blockIdx.x + 2 * t + (place.k0 > 0 ? 0 : 1)) * kSlot + row;
+      slot[0] = l != 0.0f ? m : -INFINITY;                  // a row whose scores are no numbers has a sum that is none
+      slot[128] = l;
+      if (any) {
+#pragma unroll 1
+        for (int d = 0; d < D; d += 32) {
+          uint32_t o[32];
+          tm_load32(o, o_at + d);
+          tm_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 32; ++e) slot[128 * (2 + d + e)] = __uint_as_float(o[e]);
+        }
+        tm_fence_before();
+      }
+      const unsigned long long tile_begin = place.unit - place.k0;
+      const int first = static_cast<int>(((tile_begin + 1) * ctas - 1) / total), last = static_cast<int>(((tile_begin + place.steps) * ctas - 1) / total);
+      __threadfence();
+      __syncwarp();
+      unsigned int done = 0u;                              // a warp's rows by themselves
+      if (lane == 0) done = atomicInc(p.counters + 8 * first + warp, static_cast<unsigned>(last - first));
+      if (__shfl_sync(kFull, done, 0) == static_cast<unsigned>(last - first)) {
+        __threadfence();
+        float top = -INFINITY, all = 0.0f;
+        for (int n = first; n <= last; ++n) {
+          const float* const part = p.partials + (4ll * n + 2 * t + (n == first ? 1 : 0)) * kSlot + row;
+          top = fmaxf(top, __ldcg(part));
+        }
+        for (int n = first; n <= last; ++n) {
+          const float* const part = p.partials + (4ll * n + 2 * t + (n == first ? 1 : 0)) * kSlot + row;
+          const float mine = __ldcg(part);
+          if (mine != -INFINITY) all = __fmaf_rn(__ldcg(part + 128), exp2_fast(mine - top), all);
+        }
+        const float by = all == 0.0f ? 0.0f : 1.0f / all;
+#pragma unroll 1
+        for (int d = 0; d < D; d += 16) {
+          float o[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[e] = 0.0f;
+          for (int n = first; n <= last; ++n) {
+            const float* const part = p.partials + (4ll * n + 2 * t + (n == first ? 1 : 0)) * kSlot + row;
+            const float mine = __ldcg(part);
+            if (mine == -INFINITY) continue;
+            const float w = exp2_fast(mine - top);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = __fmaf_rn(__ldcg(part + 128 * (2 + d + e)), w, o[e]);
+          }
+          if (live) {
+#pragma unroll
+            for (int e = 0; e < 16; e += 8) {
+              uint32_t w[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) w[k] = Elem<BF16>::pack_rn(o[e + 2 * k] * by, o[e + 2 * k + 1] * by);
+              *reinterpret_cast<uint4*>(to + d + e) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          }
+        }
+      }
+    } while (ok && place.next(p));
+  } else if (warp < 12) {
+    // ---- codes to binary16 ----
+    regs_down<kWidenRegs>();
+    constexpr int kChunks = D / 16;                        // 16-byte chunks of a token's codes
+    constexpr int kItems = kKeys * kChunks / 128;          // per thread and step
+    const int w = warp - 8, in_group = tid - 256;
+    // eight neighbouring lanes write four chunks of two neighbouring tokens: the swizzle puts those in different banks
+    const int token0 = D == 128 ? w * 4 + (lane >> 4) * 2 + ((lane >> 2) & 1) : w * 8 + (lane >> 2);
+    const int chunk = D == 128 ? (lane & 3) | ((lane >> 3) & 1) << 2 : lane & 3;
+    uint32_t n = 0;                                        // steps so far
+    uint4 k[kItems], v[kItems];
+    float4 scale = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    auto page_at = [&](const Place& at, int j, int granule) {
+      const int token = j * kKeys + 16 * granule;
+      if (token >= at.r.keys) return -1;
+      const int id = p.table[static_cast<long long>(at.request) * p.table_pages + (token >> p.page_shift)];
+      return static_cast<unsigned>(id) < static_cast<unsigned>(p.pages) ? id : -1;
+    };
+    auto fetch = [&](const Place& at, int j, const int8_t* codes, uint4 (&into)[kItems]) {
+#pragma unroll
+      for (int it = 0; it < kItems; ++it) {
+        const int token = token0 + it * (128 / kChunks), id = page_at(at, j, token / 16);
+        into[it] = make_uint4(0u, 0u, 0u, 0u);
+        if (id >= 0)
+          into[it] = *(reinterpret_cast<const uint4*>(codes + (((static_cast<long long>(id) * p.kv_heads + at.head) << p.page_shift) +
+                                                               ((j * kKeys + token) & ((1 << p.page_shift) - 1))) * D) + chunk);
+      }
+    };
+    auto fetch_scale = [&](const Place& at, int j) {
+      if (in_group >= kGranules) return;
+      const int id = page_at(at, j, in_group);
+      scale = make_float4(0.0f, -INFINITY, 0.0f, 0.0f);    // nothing of a page that is not there is seen
+      if (id >= 0) {
+        const long long page_head = static_cast<long long>(id) * p.kv_heads + at.head;
+        const float vs = fmaxf(p.v_scale[page_head], kLeastScale);
+        scale = make_float4(p.k_scale[page_head], __log2f(vs), 1.0f / vs, 0.0f);
+      }
+    };
+    auto widen = [&](const uint4 (&from)[kItems], unsigned char* to) {
+#pragma unroll
+      for (int it = 0; it < kItems; ++it) {
+        const int token = token0 + it * (128 / kChunks);
+        const uint32_t u[4] = {from[it].x ^ 0x80808080u, from[it].y ^ 0x80808080u, from[it].z ^ 0x80808080u, from[it].w ^ 0x80808080u};
+        unsigned char* const at = to + (chunk / 4) * kHalf + token * 128;
+        const int c = 2 * (chunk % 4), x = token & 7;
+        *reinterpret_cast<uint4*>(at + ((c ^ x) << 4)) = make_uint4(widen_lo(u[0]), widen_hi(u[0]), widen_lo(u[1]), widen_hi(u[1]));
+        *reinterpret_cast<uint4*>(at + (((c + 1) ^ x) << 4)) = make_uint4(widen_lo(u[2]), widen_hi(u[2]), widen_lo(u[3]), widen_hi(u[3]));
+      }
+    };
+    int j = place.k0;
+    bool more = true;
+    fetch_scale(place, j);
+    fetch(place, j, p.k_codes, k);
+    fetch(place, j, p.v_codes, v);
+    while (more) {
+      if (!wait(kKFree + (n & 1u), ((n >> 1) & 1u) ^ 1u)) break;
+      if (in_group < kGranules) reinterpret_cast<float4*>(smem_at + Sh::kScales)[(n % kMeta) * kGranules + in_group] = scale;
+      widen(k, smem_at + Sh::kK + (n & 1u) * Sh::kOperand);
+      fence_proxy_async_smem();
+      bar_arrive(bars + 8 * (kKFull + (n & 1u)));
+      if (++j >= place.k1) {                               // the step behind this one
+        more = place.next(p);
+        j = place.k0;
+      }
+      if (more) {
+        fetch_scale(place, j);
+        fetch(place, j, p.k_codes, k);
+      }
+      if (!wait(kVFree + (n & 1u), ((n >> 1) & 1u) ^ 1u)) break;
+      widen(v, smem_at + Sh::kV + (n & 1u) * Sh::kOperand);
+      fence_proxy_async_smem();
+      bar_arrive(bars + 8 * (kVFull + (n & 1u)));
+      if (more) fetch(place, j, p.v_codes, v);
+      ++n;
+    }
+  } else {
+    regs_down<kProductRegs>();
+  }
+  if (warp == 12) {
+    // ---- products ----
+    constexpr uint32_t kScores = product_of(kKeys, false), kSums = product_of(D, true);
+    uint32_t n = 0, count[2] = {0u, 0u}, tiles[2] = {0u, 0u};
+    do {
+      const int limit[2] = {place.limit(0, p), place.limit(1, p)};
+      for (int j = place.k0; j <= place.k1 && ok; ++j) {
+        const uint32_t buffer = n & 1u, before = (n - 1u) & 1u;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if (j > place.k0 && j - 1 < limit[t]) {          // the sums of the step before
+            if (!wait(kVFull + before, ((n - 1u) >> 1) & 1u) || !wait(kPReady + t, (count[t] - 1u) & 1u)) break;
+            tm_fence_after();
+            if (lane == 0) {
+              const uint32_t v_at = smem + Sh::kV + before * Sh::kOperand;
+#pragma unroll
+              for (int k = 0; k < kKeys / 16; ++k)
+                product_ts(tmem + 256 + D * t, tmem + 128 * t + 8 * k, operand(v_at + 2048 * k, kHalf, 1024), kSums, j - 1 > place.k0 || k > 0);
+              tm_commit(bars + 8 * (kODone + t));
+            }
+            __syncwarp();
+          }
+          if (j < limit[t]) {
+            if (j == place.k0 && !wait(kQFull + t, tiles[t] & 1u)) break;
+            if (!wait(kKFull + buffer, (n >> 1) & 1u)) break;
+            if (count[t] > 0 && !wait(kODone + t, (count[t] - 1u) & 1u)) break;  // the weights in the scores' place have been used
+            tm_fence_after();
+            if (lane == 0) {
+              const uint32_t q_at = smem + Sh::kQ + t * Sh::kOperand, k_at = smem + Sh::kK + buffer * Sh::kOperand;
+#pragma unroll
+              for (int k = 0; k < D / 16; ++k) {
+                const uint32_t off = (k / 4) * kHalf + (k % 4) * 32;
+                product_ss(tmem + 128 * t, operand(q_at + off, 16, 1024), operand(k_at + off, 16, 1024), kScores, k > 0);
+              }
+              tm_commit(bars + 8 * (kSFull + t));
+            }
+            __syncwarp();
+            ++count[t];
+          }
+        }
+        if (lane == 0) {
+          if (j < place.k1) tm_commit(bars + 8 * (kKFree + buffer));
+          if (j > place.k0) tm_commit(bars + 8 * (kVFree + before));
+        }
+        __syncwarp();
+        if (j < place.k1) ++n;
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) tiles[t] += limit[t] > place.k0 ? 1u : 0u;
+    } while (ok && place.next(p));
+    // everything issued has ended before the tensor memory is given back
+    if (lane == 0) {
+      for (int t = 0; t < 2; ++t) {
+        if (count[t] > 0) {
+          bar_wait(bars + 8 * (kSFull + t), (count[t] - 1u) & 1u);
+          bar_wait(bars + 8 * (kODone + t), (count[t] - 1u) & 1u);
+        }
+      }
+    }
+    __syncwarp();
+  }
+  if (!ok) s_failed = 1u;
+  tm_fence_before();
+  __syncthreads();
+  tm_fence_after();
+  if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  if (tid == 0 && s_failed != 0u) atomicExch(p.status, static_cast<unsigned>(TSQ_ERR_TIMEOUT));
+}
+
+template <bool BF16, int D>
+cudaError_t launch(const AttentionParams& p, int ctas, cudaStream_t stream) {
+  constexpr int bytes = Shared<D>::kBytes + 1024;
+  static_assert(Shared<D>::kScales >= 8 * kMaxRequests, "the unit counts fit in front of the scales");
+  const cudaError_t e = cudaFuncSetAttribute(attention_tiles_kernel<BF16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e != cudaSuccess) return e;
+  return launch_overlapped(attention_tiles_kernel<BF16, D>, ctas, kThreads, bytes, stream, p);
+}
+
+}  // namespace
+
+cudaError_t launch_attention_tiles(const AttentionParams& p, bool bf16, int head_dim, int ctas, cudaStream_t stream) {
+  if (head_dim == 128) return bf16 ? launch<true, 128>(p, ctas, stream) : launch<false, 128>(p, ctas, stream);
+  return bf16 ? launch<true, 64>(p, ctas, stream) : launch<false, 64>(p, ctas, stream);
+}
+
+}  // namespace tsq

@@ -162,6 +162,7 @@ def check_attention(s, added, group, scale=None, lengths=None, table=None, q=Non
     args = (q, s.ints(starts), s.ints(lengths), s.table if table is None else table, out, ws, most)
     s.cache.attention(*args, scale=scale, **kw)
     torch.cuda.synchronize()
+    assert s.cache.workspace_status(ws) == 0
     want, tol = attention_ref(s, q, starts, lengths, s.D ** -0.5 if scale is None else scale, table)
     got = out.double().cpu()
     assert bool((got[starts[-1]:] == 5.0).all()), "rows behind the last request's"
