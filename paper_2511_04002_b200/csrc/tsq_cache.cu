@@ -566,7 +566,7 @@ tsq_status_t tsq_cache_attention(const tsq_cache_t* cache, const void* q, int64_
   p.partials = reinterpret_cast<float*>(static_cast<unsigned char*>(ws_dev) + workspace_head(sms));
   const bool bf16 = cache->dtype == TSQ_BF16;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  return launched(few ? launch_attention_rows(p, bf16, cache->head_dim, kRowsCtasPerSm * sms, st) : launch_attention_tiles(p, bf16, cache->head_dim, sms, st));
+  return launched(few ? launch_attention_rows(p, bf16, cache->head_dim, sms, st) : launch_attention_tiles(p, bf16, cache->head_dim, sms, st));
 }
 
 tsq_status_t tsq_cache_workspace_status(const void* ws_dev, uint32_t* status, void* cuda_stream) {

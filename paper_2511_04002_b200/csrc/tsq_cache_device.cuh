@@ -22,8 +22,9 @@ struct Request {
     return static_cast<int>((static_cast<long long>(rows) * p.group + tile - 1) / tile);
   }
   __device__ __forceinline__ int key_units(int unit) const { return keys > 0 ? (keys - 1) / unit + 1 : 1; }
-  __device__ __forceinline__ unsigned long long units(int tile, int unit, const AttentionParams& p) const {
-    return rows == 0 ? 0ull : static_cast<unsigned long long>(tiles(tile, p)) * static_cast<unsigned>(key_units(unit)) * static_cast<unsigned>(p.kv_heads);
+  // a tile counts `more` units above those of its keys
+  __device__ __forceinline__ unsigned long long units(int tile, int unit, int more, const AttentionParams& p) const {
+    return rows == 0 ? 0ull : static_cast<unsigned long long>(tiles(tile, p)) * static_cast<unsigned>(key_units(unit) + more) * static_cast<unsigned>(p.kv_heads);
   }
   // keys that row j sees
   __device__ __forceinline__ int seen(int j) const { return static_cast<int>(max(0ll, min(static_cast<long long>(keys), before + j + 1))); }
@@ -52,14 +53,6 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   memcpy(&u, &h, sizeof u);
   return u;
 }
-__device__ __forceinline__ float quad_max(float v) {
-  v = fmaxf(v, __shfl_xor_sync(kFull, v, 1));
-  return fmaxf(v, __shfl_xor_sync(kFull, v, 2));
-}
-__device__ __forceinline__ float quad_sum(float v) {
-  v += __shfl_xor_sync(kFull, v, 1);
-  return v + __shfl_xor_sync(kFull, v, 2);
-}
 
 // Two codes with their sign bit inverted (code + 128) as binary16 numbers: 0x6400 + byte is 1024 + code + 128, and the difference to 1152 is exact.
 __device__ __forceinline__ uint32_t less_1152(uint32_t pair) {
@@ -77,47 +70,6 @@ __device__ __forceinline__ float row_power(float top, float& inverse) {
   const int up = plain ? min(14 - (e - 127), 112) : 0;
   inverse = __uint_as_float(static_cast<uint32_t>(127 - up) << 23);
   return __uint_as_float(static_cast<uint32_t>(127 + up) << 23);
-}
-
-// The A operands of the products with the keys: rows row0 + g and row0 + g + 8 of the tile (zeros past its `rows`), for thread c of a row's four the dimensions
-// c * D / 4 ... in order, four per product step; brought to binary16 by a power of two per row, whose inverse is the row's factor.
-template <bool BF16, int D>
-__device__ __forceinline__ void load_queries(const AttentionParams& p, const Request& r, int head, int row0, int rows, int g, int c, uint32_t (&qa)[D / 16][4],
-                                             float& factor_a, float& factor_b) {
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    const int row = g + 8 * half, at = row0 + row;
-    uint32_t w[D / 8];
-    if (row < rows) {
-      const uint16_t* const from = static_cast<const uint16_t*>(p.q) + (r.start + at / p.group) * p.q_stride +
-                                   (static_cast<long long>(head) * p.group + at % p.group) * D + c * (D / 4);
-#pragma unroll
-      for (int k = 0; k < D / 32; ++k) {
-        const uint4 v = reinterpret_cast<const uint4*>(from)[k];
-        w[4 * k] = v.x, w[4 * k + 1] = v.y, w[4 * k + 2] = v.z, w[4 * k + 3] = v.w;
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < D / 8; ++k) w[k] = 0u;
-    }
-    uint32_t top = 0u;
-#pragma unroll
-    for (int k = 0; k < D / 8; ++k) top = max(top, max(w[k] & 0x7fffu, (w[k] >> 16) & 0x7fffu));
-    top = max(top, __shfl_xor_sync(kFull, top, 1));
-    top = max(top, __shfl_xor_sync(kFull, top, 2));
-    float factor;
-    const float power = row_power(Elem<BF16>::pattern_f32(top), factor);
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k) {
-      qa[k][half] = pack_half2(Elem<BF16>::lo_f32(w[2 * k]) * power, Elem<BF16>::hi_f32(w[2 * k]) * power);
-      qa[k][2 + half] = pack_half2(Elem<BF16>::lo_f32(w[2 * k + 1]) * power, Elem<BF16>::hi_f32(w[2 * k + 1]) * power);
-    }
-    if (half == 0) {
-      factor_a = factor;
-    } else {
-      factor_b = factor;
-    }
-  }
 }
 
 }  // namespace tsq

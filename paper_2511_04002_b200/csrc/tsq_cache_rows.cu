@@ -10,9 +10,9 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
-constexpr int kStages = 4;                   // of a warp's ring
 constexpr int kStepTokens = 16;              // tokens of a warp's step: within one page
 constexpr int kUnitTokens = kWarps * kStepTokens;
+constexpr int kTileUnits = 2;                // what beginning and ending a tile costs, in units
 
 // One m16n8k16 product, binary16 in, binary32 sums.
 __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -24,6 +24,28 @@ __device__ __forceinline__ uint4 lds128(uint32_t at) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
   return v;
+}
+__device__ __forceinline__ float4 lds128f(uint32_t at) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at));
+  return v;
+}
+// An 8 x 8 block of binary16 numbers, a row's two neighbours in each thread, transposed.
+__device__ __forceinline__ uint32_t transposed(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+// Over the eight threads that have the same columns.
+__device__ __forceinline__ float column_max(float v) {
+  v = fmaxf(v, __shfl_xor_sync(kFull, v, 4));
+  v = fmaxf(v, __shfl_xor_sync(kFull, v, 8));
+  return fmaxf(v, __shfl_xor_sync(kFull, v, 16));
+}
+__device__ __forceinline__ float column_sum(float v) {
+  v += __shfl_xor_sync(kFull, v, 4);
+  v += __shfl_xor_sync(kFull, v, 8);
+  return v + __shfl_xor_sync(kFull, v, 16);
 }
 __device__ __forceinline__ uint2 lds64(uint32_t at) {
   uint2 v;
@@ -44,32 +66,77 @@ __device__ __forceinline__ int placed(int t, int c) {
   return D == 128 ? t * 128 + ((c ^ (t & 7)) << 4) : t * 64 + ((c ^ ((t >> 1) & 3)) << 4);
 }
 
-template <int D>
+// The B operands of the products with the keys: thread (g, c) has of the rows row0 + 8 t + g of the tile (zeros past its `rows`) the dimensions
+// c * D / 4 ... in order, four per product step; brought to binary16 by a power of two per row.  factor: the inverses for the rows 8 t + 2 c and 8 t + 2 c + 1.
+template <bool BF16, int D, int NT>
+__device__ __forceinline__ void load_queries(const AttentionParams& p, const Request& r, int head, int row0, int rows, int g, int c, uint32_t (&q)[NT][D / 16][2],
+                                             float (&factor)[NT][2]) {
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int row = 8 * t + g, at = row0 + row;
+    uint32_t w[D / 8];
+    if (row < rows) {
+      const uint16_t* const from = static_cast<const uint16_t*>(p.q) + (r.start + at / p.group) * p.q_stride +
+                                   (static_cast<long long>(head) * p.group + at % p.group) * D + c * (D / 4);
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k) {
+        const uint4 v = reinterpret_cast<const uint4*>(from)[k];
+        w[4 * k] = v.x, w[4 * k + 1] = v.y, w[4 * k + 2] = v.z, w[4 * k + 3] = v.w;
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < D / 8; ++k) w[k] = 0u;
+    }
+    uint32_t top = 0u;
+#pragma unroll
+    for (int k = 0; k < D / 8; ++k) top = max(top, max(w[k] & 0x7fffu, (w[k] >> 16) & 0x7fffu));
+    top = max(top, __shfl_xor_sync(kFull, top, 1));
+    top = max(top, __shfl_xor_sync(kFull, top, 2));
+    float inverse;
+    const float power = row_power(Elem<BF16>::pattern_f32(top), inverse);
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+      q[t][k][0] = pack_half2(Elem<BF16>::lo_f32(w[2 * k]) * power, Elem<BF16>::hi_f32(w[2 * k]) * power);
+      q[t][k][1] = pack_half2(Elem<BF16>::lo_f32(w[2 * k + 1]) * power, Elem<BF16>::hi_f32(w[2 * k + 1]) * power);
+    }
+    factor[t][0] = __shfl_sync(kFull, inverse, 8 * c);    // of the thread with g = 2 c
+    factor[t][1] = __shfl_sync(kFull, inverse, 8 * c + 4);
+  }
+}
+
+// Tiles of 8 query rows (NT = 1) or 16 (NT = 2).
+template <int D, int NT>
 struct Layout {
+  static constexpr int kRows = 8 * NT;
+  static constexpr int kCtasPerSm = NT == 1 ? kRowsCtasPerSm : 3;
+  static constexpr int kStages = NT == 1 ? 3 : 4;        // of a warp's ring
   static constexpr int kRowChunks = D / 16;
   static constexpr int kHalf = kStepTokens * D;          // bytes of a stage's keys, and of its values
   static constexpr int kStage = 2 * kHalf;
   static constexpr int kRing = kStages * kStage;         // of a warp
-  static constexpr int kRowFloats = D + 16;              // a row of a warp's accumulators, four floats more behind each quarter
-  static constexpr int kSums = kWarps * kRowsTile * kRowFloats * 4;
-  static constexpr int kMerge = kSums + kWarps * kRowsTile * 8;
-  static constexpr size_t kBytes = kWarps * kRing > kMerge ? kWarps * kRing : kMerge;
+  static constexpr int kRowFloats = D + 36;              // a row of a warp's sums: four floats more behind each eighth, and four at the end
+  static constexpr int kSums = kWarps * kRows * kRowFloats * 4;
+  static constexpr int kMerge = kSums + kWarps * kRows * 8;
+  static constexpr int kScales = kWarps * kRing > kMerge ? kWarps * kRing : kMerge;  // 64 steps' factors for each warp
+  static constexpr int kBytes = kScales + kWarps * 64 * 16;
 };
 
-// Work is cut into units of 64 tokens of one (request, key head, tile of 16 query rows), numbered in that order, and every CTA takes the same number of
-// neighbouring units whatever the requests' lengths are.  A tile whose units lie in one CTA is written by it; otherwise the CTAs leave their sums in the workspace
-// (at most two tiles of a CTA are unfinished: its first and its last) and the CTA that comes last adds them up in the order of the units.
+// Work is cut into units of 64 tokens of one (request, key head, tile of query rows), numbered in that order, and every CTA takes the same number of
+// neighbouring units whatever the requests' lengths are; a tile counts kTileUnits more, for what it costs to begin and to end one.  A tile whose units lie in
+// one CTA is written by it; otherwise the CTAs leave their sums in the workspace (at most two tiles of a CTA are unfinished: its first and its last) and the
+// CTA that comes last adds them up in the order of the units.
 //
 // Within a unit each of the four warps has 16 tokens, a ring of stages of its own and its own sums; the warps meet only at a tile's end.
-// Codes go from HBM to shared memory by asynchronous copies and are widened to binary16 in registers (exact).  The order of the head's
-// dimensions in the products is free: thread c of a row's four takes D / 4 neighbouring ones, so a row is read as 16-byte chunks.  Scores: q scaled by a power of two
-// per row (exact), code products summed in binary32, times the page's scale.  With the values' scale s_v of the page, weights are
+// Codes go from HBM to shared memory by asynchronous copies and are widened to binary16 in registers (exact).  Both products have the codes as their 16-row
+// operand and the query rows as columns, eight to a product: S^T = K Q^T, O^T += V^T P^T, where P^T is S^T transposed by 8 x 8 blocks.  The order of the
+// head's dimensions in the products is free: thread c of a token's four takes D / 4 neighbouring ones, so a token is read as 16-byte chunks.  Scores: q
+// scaled by a power of two per row (exact), code products summed in binary32, times the page's scale.  With the values' scale s_v of the page, weights are
 // w = 2^(score + log2 s_v - m), rounded to binary16 for the product with the values' codes, and the softmax's sum takes w / s_v.
-template <bool BF16, int D>
-__global__ void __launch_bounds__(kThreads, kRowsCtasPerSm) attention_rows_kernel(const AttentionParams p) {
-  using L = Layout<D>;
+template <bool BF16, int D, int NT>
+__global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention_rows_kernel(const AttentionParams p) {
+  using L = Layout<D, NT>;
   constexpr int kSteps = D / 16;                          // of the products with the keys
-  constexpr int kTiles = D / 8;                           // of the accumulators, 8 dimensions each
+  constexpr int kTiles = D / 16;                          // of the sums, 16 dimensions each
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ unsigned long long s_scan[kWarps];
   __shared__ int s_found;
@@ -86,7 +153,7 @@ __global__ void __launch_bounds__(kThreads, kRowsCtasPerSm) attention_rows_kerne
     const int per = (p.requests + kThreads - 1) / kThreads;
     const int i0 = min(tid * per, p.requests), i1 = min(i0 + per, p.requests);
     unsigned long long mine = 0;
-    for (int i = i0; i < i1; ++i) mine += request_of(p, i).units(kRowsTile, kUnitTokens, p);
+    for (int i = i0; i < i1; ++i) mine += request_of(p, i).units(L::kRows, kUnitTokens, kTileUnits, p);
     unsigned long long in = mine;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
@@ -104,7 +171,7 @@ __global__ void __launch_bounds__(kThreads, kRowsCtasPerSm) attention_rows_kerne
     }
     for (int i = i0; i < i1; ++i) {
       s_units[i] = at;
-      at += request_of(p, i).units(kRowsTile, kUnitTokens, p);
+      at += request_of(p, i).units(L::kRows, kUnitTokens, kTileUnits, p);
     }
   }
   const unsigned long long ctas = total < gridDim.x ? total : gridDim.x;
@@ -127,285 +194,304 @@ __global__ void __launch_bounds__(kThreads, kRowsCtasPerSm) attention_rows_kerne
   int i = s_found;
   unsigned long long rest = unit - s_begin;               // units of request i in front of `unit`
   Request r = request_of(p, i);
-  const uint32_t ring = smem_addr(smem) + warp * L::kRing;
+  const uint32_t ring = smem_addr(smem) + warp * L::kRing, scales = smem_addr(smem) + L::kScales + warp * (64 * 16);
 
   while (unit < unit_end) {
-    const int tiles = r.tiles(kRowsTile, p), keys = r.key_units(kUnitTokens);
-    const int head_tile = static_cast<int>(rest / keys), head = head_tile / tiles, tile = head_tile % tiles;
-    const int k0 = static_cast<int>(rest % keys);
-    const int k1 = static_cast<int>(min(static_cast<unsigned long long>(keys), k0 + (unit_end - unit)));
-    const int row0 = tile * kRowsTile, rows = min(kRowsTile, r.rows * p.group - row0);
-    // keys that the tile's first and last rows, and this thread's two, see
-    const int seen_first = r.seen(row0 / p.group), seen_last = r.seen((row0 + rows - 1) / p.group);
-    const int seen_a = r.seen((row0 + min(g, rows - 1)) / p.group), seen_b = r.seen((row0 + min(g + 8, rows - 1)) / p.group);
+    const int tiles = r.tiles(L::kRows, p), keys = r.key_units(kUnitTokens), span = keys + kTileUnits;
+    const int head_tile = static_cast<int>(rest / span), head = head_tile / tiles, tile = head_tile % tiles;
+    const int from = static_cast<int>(rest % span), upto = static_cast<int>(min(static_cast<unsigned long long>(span), from + (unit_end - unit)));
+    const int k0 = max(0, from - kTileUnits), k1 = max(0, upto - kTileUnits);
+    const unsigned long long tile_begin = unit - from;
+    unit += upto - from;
+    rest += upto - from;
+    if (k1 > k0) {
+      const int row0 = tile * L::kRows, rows = min(L::kRows, r.rows * p.group - row0);
+      // keys that the tile's first and last rows see
+      const int seen_first = r.seen(row0 / p.group), seen_last = r.seen((row0 + rows - 1) / p.group);
 
-    // ---- codes on their way ----
-    const int base = k0 * kUnitTokens + warp * kStepTokens;
-    const int n_steps = max(0, min(k1 - k0, (seen_last - base + kUnitTokens - 1) / kUnitTokens));
-    const int32_t* const table = p.table + static_cast<long long>(i) * p.table_pages;
-    // page, score factor, log2 and inverse of the values' scale of step 32 b + lane, for the batch b that is being worked off and the next
-    int page_0 = -1, page_1 = -1;
-    float fk_0 = 0.0f, fk_1 = 0.0f, lv_0 = 0.0f, lv_1 = 0.0f, iv_0 = 0.0f, iv_1 = 0.0f;
-    auto fetch = [&](int b, int& page, float& fk, float& lv, float& iv) {
-      const int step = 32 * b + lane, token = base + step * kUnitTokens;
-      int id = -1;
+      // ---- the first codes on their way ----
+      const int base = k0 * kUnitTokens + warp * kStepTokens;
+      const int n_steps = max(0, min(k1 - k0, (seen_last - base + kUnitTokens - 1) / kUnitTokens));
+      const int32_t* const table = p.table + static_cast<long long>(i) * p.table_pages;
+      // page of step 32 b + lane, -1 where there is none
+      auto page_of = [&](int b) {
+        const int step = 32 * b + lane;
+        const int id = step < n_steps ? table[(base + step * kUnitTokens) >> p.page_shift] : -1;
+        return static_cast<unsigned>(id) < static_cast<unsigned>(p.pages) ? id : -1;
+      };
+      // for the batch that is being worked off and the one behind it, and what is read ahead for the next
+      int page_0 = page_of(0), page_1 = n_steps > 32 ? page_of(1) : -1, page_ahead = -1;
       float ks = 0.0f, vs = 1.0f;
-      if (step < n_steps) {
-        id = table[token >> p.page_shift];
-        if (static_cast<unsigned>(id) >= static_cast<unsigned>(p.pages)) id = -1;
-        if (id >= 0) {
-          ks = p.k_scale[static_cast<long long>(id) * p.kv_heads + head];
-          vs = fmaxf(p.v_scale[static_cast<long long>(id) * p.kv_heads + head], kLeastScale);
-        }
-      }
-      page = id;
-      fk = ks * p.scale_log2;
-      lv = __log2f(vs);
-      iv = 1.0f / vs;
-    };
-    fetch(0, page_0, fk_0, lv_0, iv_0);
-    fetch(1, page_1, fk_1, lv_1, iv_1);
-    auto issue = [&](int step) {
-      if (step < n_steps) {
-        const int id = __shfl_sync(kFull, (step >> 5) & 1 ? page_1 : page_0, step & 31);
-        if (id >= 0) {
-          const int token = base + step * kUnitTokens;
-          const long long at = (((static_cast<long long>(id) * p.kv_heads + head) << p.page_shift) + (token & ((1 << p.page_shift) - 1))) * D;
-          const uint32_t stage = ring + (step % kStages) * L::kStage;
+      auto fetch_scales = [&](int page) {
+        ks = page >= 0 ? p.k_scale[static_cast<long long>(page) * p.kv_heads + head] : 0.0f;
+        vs = page >= 0 ? p.v_scale[static_cast<long long>(page) * p.kv_heads + head] : 1.0f;
+      };
+      // score factor, log2 and inverse of the values' scale of a batch's steps
+      auto put_scales = [&](int b) {
+        const float v = fmaxf(vs, kLeastScale);
+        asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(scales + ((b & 1) * 32 + lane) * 16), "f"(ks * p.scale_log2), "f"(__log2f(v)), "f"(1.0f / v), "f"(0.0f)
+                     : "memory");
+      };
+      auto issue = [&](int step) {
+        if (step < n_steps) {
+          const int id = __shfl_sync(kFull, (step >> 5) & 1 ? page_1 : page_0, step & 31);
+          if (id >= 0) {
+            const int token = base + step * kUnitTokens;
+            const long long at = (((static_cast<long long>(id) * p.kv_heads + head) << p.page_shift) + (token & ((1 << p.page_shift) - 1))) * D + lane * 16;
+            const int8_t *const k_from = p.k_codes + at, *const v_from = p.v_codes + at;
+            const uint32_t stage = ring + (step % L::kStages) * L::kStage;
 #pragma unroll
-          for (int n = 0; n < kStepTokens * L::kRowChunks / 32; ++n) {
-            const int item = n * 32 + lane;
-            const int to = placed<D>(item / L::kRowChunks, item % L::kRowChunks);
-            copy16(stage + to, p.k_codes + at + item * 16);
-            copy16(stage + L::kHalf + to, p.v_codes + at + item * 16);
+            for (int n = 0; n < kStepTokens * L::kRowChunks / 32; ++n) {
+              const int item = n * 32 + lane;
+              const int to = placed<D>(item / L::kRowChunks, item % L::kRowChunks);
+              copy16(stage + to, k_from + n * 512);
+              copy16(stage + L::kHalf + to, v_from + n * 512);
+            }
           }
         }
+        copies_commit();
+      };
+      __syncthreads();                                      // the shared memory is free of the last tile's sums, and of the unit counts
+#pragma unroll
+      for (int s = 0; s < L::kStages - 1; ++s) issue(s);
+
+      // ---- queries, scales ----
+      uint32_t q[NT][kSteps][2];
+      float factor[NT][2];                                  // of the rows 8 t + 2 c and 8 t + 2 c + 1, whose scores this thread has
+      load_queries<BF16, D, NT>(p, r, head, row0, rows, g, c, q, factor);
+      fetch_scales(page_0);
+      put_scales(0);
+      if (n_steps > 32) {
+        fetch_scales(page_1);
+        put_scales(1);
       }
-      copies_commit();
-    };
-    __syncthreads();                                      // the shared memory is free of the last tile's sums, and of the unit counts
+      int seen[NT][2];
 #pragma unroll
-    for (int s = 0; s < kStages - 1; ++s) issue(s);
-
-    // ---- queries ----
-    uint32_t qa[kSteps][4];
-    float factor_a, factor_b;
-    load_queries<BF16, D>(p, r, head, row0, rows, g, c, qa, factor_a, factor_b);
-
-    float acc[kTiles][4];
+      for (int t = 0; t < NT; ++t) {
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.0f;
-    float m_a = -INFINITY, m_b = -INFINITY, l_a = 0.0f, l_b = 0.0f;
-
-    for (int step = 0; step < n_steps; ++step) {
-      copies_wait<kStages - 2>();
+        for (int h = 0; h < 2; ++h) seen[t][h] = r.seen((row0 + min(8 * t + 2 * c + h, rows - 1)) / p.group);
+      }
       __syncwarp();
-      issue(step + kStages - 1);
-      const bool odd = ((step >> 5) & 1) != 0;
-      const int id = __shfl_sync(kFull, odd ? page_1 : page_0, step & 31);
-      const float f = __shfl_sync(kFull, odd ? fk_1 : fk_0, step & 31);
-      const float bias = __shfl_sync(kFull, odd ? lv_1 : lv_0, step & 31);
-      const float inverse = __shfl_sync(kFull, odd ? iv_1 : iv_0, step & 31);
-      if ((step & 31) == 31 && step + 1 < n_steps) {      // the batch after the next takes this one's place
-        if (odd) {
-          fetch((step >> 5) + 2, page_1, fk_1, lv_1, iv_1);
-        } else {
-          fetch((step >> 5) + 2, page_0, fk_0, lv_0, iv_0);
-        }
-      }
-      if (id < 0) continue;
-      const uint32_t stage = ring + (step % kStages) * L::kStage;
-      const int token0 = base + step * kUnitTokens;
 
-      // scores of 16 rows and 16 tokens
-      float s[2][4];
+      float acc[NT][kTiles][4];
+      float m[NT][2], l[NT][2];
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.0f;
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int d = 0; d < kTiles; ++d) acc[t][d][0] = acc[t][d][1] = acc[t][d][2] = acc[t][d][3] = 0.0f;
+        m[t][0] = m[t][1] = -INFINITY;
+        l[t][0] = l[t][1] = 0.0f;
+      }
+
+      for (int step = 0; step < n_steps; ++step) {
+        copies_wait<L::kStages - 2>();
+        __syncwarp();
+        issue(step + L::kStages - 1);
+        const int id = __shfl_sync(kFull, (step >> 5) & 1 ? page_1 : page_0, step & 31);
+        const float4 f = lds128f(scales + (step & 63) * 16);
+        // the batch after the next takes this one's place: its pages and scales are read while this one's last steps are worked off
+        if ((step & 7) == 7 && (step | 31) + 33 < n_steps) {
+          if ((step & 31) == 15) page_ahead = page_of((step >> 5) + 2);
+          if ((step & 31) == 23) fetch_scales(page_ahead);
+        }
+        if ((step & 31) == 31) {
+          if (step + 33 < n_steps) {
+            __syncwarp();
+            put_scales(step >> 5);
+          }
+          if ((step >> 5) & 1) {
+            page_1 = page_ahead;
+          } else {
+            page_0 = page_ahead;
+          }
+          page_ahead = -1;
+        }
+        if (id < 0) continue;
+        const uint32_t stage = ring + (step % L::kStages) * L::kStage;
+        const int token0 = base + step * kUnitTokens;
+
+        // scores of 16 tokens and the rows
+        float s[NT][4];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.0f;
 #pragma unroll
         for (int h = 0; h < D / 64; ++h) {
-          const uint4 w = lds128(stage + placed<D>(8 * t + g, c * (D / 64) + h));
-          const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+          const uint4 w0 = lds128(stage + placed<D>(g, c * (D / 64) + h)), w1 = lds128(stage + placed<D>(g + 8, c * (D / 64) + h));
+          const uint32_t a0[4] = {w0.x, w0.y, w0.z, w0.w}, a1[4] = {w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const uint32_t u = words[k] ^ 0x80808080u;
-            mma_16816(s[t], qa[4 * h + k], widen_lo(u), widen_hi(u));
+            const uint32_t u0 = a0[k] ^ 0x80808080u, u1 = a1[k] ^ 0x80808080u;
+            const uint32_t a[4] = {widen_lo(u0), widen_lo(u1), widen_hi(u0), widen_hi(u1)};
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mma_16816(s[t], a, q[t][4 * h + k][0], q[t][4 * h + k][1]);
+          }
+        }
+        bool over = false;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const float f0 = f.x * factor[t][0], f1 = f.x * factor[t][1];
+          s[t][0] = __fmaf_rn(s[t][0], f0, f.y);
+          s[t][1] = __fmaf_rn(s[t][1], f1, f.y);
+          s[t][2] = __fmaf_rn(s[t][2], f0, f.y);
+          s[t][3] = __fmaf_rn(s[t][3], f1, f.y);
+          if (token0 + kStepTokens > seen_first) {
+            if (token0 + g >= seen[t][0]) s[t][0] = -INFINITY;
+            if (token0 + g >= seen[t][1]) s[t][1] = -INFINITY;
+            if (token0 + g + 8 >= seen[t][0]) s[t][2] = -INFINITY;
+            if (token0 + g + 8 >= seen[t][1]) s[t][3] = -INFINITY;
+          }
+          over = over || fmaxf(s[t][0], s[t][2]) > m[t][0] + 8.0f || fmaxf(s[t][1], s[t][3]) > m[t][1] + 8.0f;
+        }
+        // m is a reference, not the maximum: it follows only when a score is more than 2^8 above it (a weight stays below 2^9 in binary16)
+        if (__any_sync(kFull, over)) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            float by[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const float now = fmaxf(m[t][h], column_max(fmaxf(s[t][h], s[t][2 + h])));
+              by[h] = m[t][h] == -INFINITY ? 0.0f : exp2_fast(m[t][h] - now);
+              m[t][h] = now;
+              l[t][h] *= by[h];
+            }
+#pragma unroll
+            for (int d = 0; d < kTiles; ++d) {
+              acc[t][d][0] *= by[0];
+              acc[t][d][1] *= by[1];
+              acc[t][d][2] *= by[0];
+              acc[t][d][3] *= by[1];
+            }
+          }
+        }
+        uint32_t w[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const float ref0 = m[t][0] == -INFINITY ? 0.0f : m[t][0], ref1 = m[t][1] == -INFINITY ? 0.0f : m[t][1];
+          const float x0 = exp2_fast(s[t][0] - ref0), x1 = exp2_fast(s[t][1] - ref1), x2 = exp2_fast(s[t][2] - ref0), x3 = exp2_fast(s[t][3] - ref1);
+          l[t][0] = __fmaf_rn(x0 + x2, f.z, l[t][0]);
+          l[t][1] = __fmaf_rn(x1 + x3, f.z, l[t][1]);
+          w[t][0] = transposed(pack_half2(x0, x1));
+          w[t][1] = transposed(pack_half2(x2, x3));
+        }
+
+        // values: thread (g, c) has the dimensions g * D / 8 ... of the tokens 2c, 2c + 1, 2c + 8, 2c + 9
+        uint32_t v[4][D / 32];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int token = 2 * c + (t & 1) + 8 * (t >> 1);
+          if constexpr (D == 128) {
+            const uint4 x = lds128(stage + L::kHalf + placed<D>(token, g));
+            v[t][0] = x.x, v[t][1] = x.y, v[t][2] = x.z, v[t][3] = x.w;
+          } else {
+            const uint2 x = lds64(stage + L::kHalf + placed<D>(token, g / 2) + 8 * (g % 2));
+            v[t][0] = x.x, v[t][1] = x.y;
+          }
+#pragma unroll
+          for (int k = 0; k < D / 32; ++k) v[t][k] ^= 0x80808080u;
+        }
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) {
+          const uint32_t x0 = __byte_perm(v[0][k], v[1][k], 0x5140), x1 = __byte_perm(v[0][k], v[1][k], 0x7362);
+          const uint32_t y0 = __byte_perm(v[2][k], v[3][k], 0x5140), y1 = __byte_perm(v[2][k], v[3][k], 0x7362);
+          const uint32_t a0[4] = {widen_lo(x0), widen_hi(x0), widen_lo(y0), widen_hi(y0)}, a1[4] = {widen_lo(x1), widen_hi(x1), widen_lo(y1), widen_hi(y1)};
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            mma_16816(acc[t][2 * k], a0, w[t][0], w[t][1]);
+            mma_16816(acc[t][2 * k + 1], a1, w[t][0], w[t][1]);
           }
         }
       }
-      const float fa = f * factor_a, fb = f * factor_b;
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        s[t][0] = __fmaf_rn(s[t][0], fa, bias);
-        s[t][1] = __fmaf_rn(s[t][1], fa, bias);
-        s[t][2] = __fmaf_rn(s[t][2], fb, bias);
-        s[t][3] = __fmaf_rn(s[t][3], fb, bias);
-      }
-      if (token0 + kStepTokens > seen_first) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const int token = token0 + 8 * t + 2 * c;
-          if (token >= seen_a) s[t][0] = -INFINITY;
-          if (token + 1 >= seen_a) s[t][1] = -INFINITY;
-          if (token >= seen_b) s[t][2] = -INFINITY;
-          if (token + 1 >= seen_b) s[t][3] = -INFINITY;
-        }
-      }
-      // m is a reference, not the maximum: it follows only when a score is more than 2^8 above it (a weight stays below 2^9 in binary16)
-      const float top_a = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
-      const float top_b = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
-      if (__any_sync(kFull, top_a > m_a + 8.0f || top_b > m_b + 8.0f)) {
-        const float new_a = fmaxf(m_a, quad_max(top_a)), new_b = fmaxf(m_b, quad_max(top_b));
-        const float by_a = m_a == -INFINITY ? 0.0f : exp2_fast(m_a - new_a), by_b = m_b == -INFINITY ? 0.0f : exp2_fast(m_b - new_b);
-        m_a = new_a;
-        m_b = new_b;
-        l_a *= by_a;
-        l_b *= by_b;
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-          acc[t][0] *= by_a;
-          acc[t][1] *= by_a;
-          acc[t][2] *= by_b;
-          acc[t][3] *= by_b;
-        }
-      }
-      const float ref_a = m_a == -INFINITY ? 0.0f : m_a, ref_b = m_b == -INFINITY ? 0.0f : m_b;
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        s[t][0] = exp2_fast(s[t][0] - ref_a);
-        s[t][1] = exp2_fast(s[t][1] - ref_a);
-        s[t][2] = exp2_fast(s[t][2] - ref_b);
-        s[t][3] = exp2_fast(s[t][3] - ref_b);
-        l_a = __fmaf_rn(s[t][0] + s[t][1], inverse, l_a);
-        l_b = __fmaf_rn(s[t][2] + s[t][3], inverse, l_b);
-      }
-      const uint32_t pa[4] = {pack_half2(s[0][0], s[0][1]), pack_half2(s[0][2], s[0][3]), pack_half2(s[1][0], s[1][1]), pack_half2(s[1][2], s[1][3])};
 
-      // values: thread (g, c) has the dimensions g * D / 8 ... of the tokens 2c, 2c + 1, 2c + 8, 2c + 9
-      uint32_t v[4][D / 32];
+      // ---- the four warps' sums ----
+      copies_wait<0>();
+      __syncthreads();                                      // every warp has read its stages
+      float* const sums = reinterpret_cast<float*>(smem);
+      float2* const stats = reinterpret_cast<float2*>(smem + L::kSums);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int token = 2 * c + (t & 1) + 8 * (t >> 1);
-        if constexpr (D == 128) {
-          const uint4 w = lds128(stage + L::kHalf + placed<D>(token, g));
-          v[t][0] = w.x, v[t][1] = w.y, v[t][2] = w.z, v[t][3] = w.w;
-        } else {
-          const uint2 w = lds64(stage + L::kHalf + placed<D>(token, g / 2) + 8 * (g % 2));
-          v[t][0] = w.x, v[t][1] = w.y;
-        }
+      for (int t = 0; t < NT; ++t) {
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k) v[t][k] ^= 0x80808080u;
-      }
+        for (int h = 0; h < 2; ++h) {
+          const int row = warp * L::kRows + 8 * t + 2 * c + h;
+          const float all = column_sum(l[t][h]);
+          if (g == 0) stats[row] = make_float2(m[t][h], all);
+          float* const at = sums + row * L::kRowFloats + g * (D / 8 + 4);
 #pragma unroll
-      for (int k = 0; k < D / 32; ++k) {
-        const uint32_t x0 = __byte_perm(v[0][k], v[1][k], 0x5140), x1 = __byte_perm(v[0][k], v[1][k], 0x7362);
-        const uint32_t y0 = __byte_perm(v[2][k], v[3][k], 0x5140), y1 = __byte_perm(v[2][k], v[3][k], 0x7362);
-        mma_16816(acc[4 * k], pa, widen_lo(x0), widen_lo(y0));
-        mma_16816(acc[4 * k + 1], pa, widen_hi(x0), widen_hi(y0));
-        mma_16816(acc[4 * k + 2], pa, widen_lo(x1), widen_lo(y1));
-        mma_16816(acc[4 * k + 3], pa, widen_hi(x1), widen_hi(y1));
-      }
-    }
-    l_a = quad_sum(l_a);
-    l_b = quad_sum(l_b);
-
-    // ---- the four warps' sums ----
-    copies_wait<0>();
-    __syncthreads();                                      // every warp has read its stages
-    float* const sums = reinterpret_cast<float*>(smem);
-    float2* const stats = reinterpret_cast<float2*>(smem + L::kSums);
-    {
-      float* const at = sums + (warp * kRowsTile + g) * L::kRowFloats;
-#pragma unroll
-      for (int col = 0; col < 2; ++col) {
-        const int d0 = (2 * c + col) * (D / 8), padded = d0 + d0 / (D / 4) * 4;
-#pragma unroll
-        for (int t = 0; t < kTiles; t += 4) {
-          *reinterpret_cast<float4*>(at + padded + t) = make_float4(acc[t][col], acc[t + 1][col], acc[t + 2][col], acc[t + 3][col]);
-          *reinterpret_cast<float4*>(at + 8 * L::kRowFloats + padded + t) =
-              make_float4(acc[t][2 + col], acc[t + 1][2 + col], acc[t + 2][2 + col], acc[t + 3][2 + col]);
+          for (int d = 0; d < kTiles; d += 2) *reinterpret_cast<float4*>(at + 2 * d) = make_float4(acc[t][d][h], acc[t][d][2 + h], acc[t][d + 1][h], acc[t][d + 1][2 + h]);
         }
       }
-      if (c == 0) {
-        stats[warp * kRowsTile + g] = make_float2(m_a, l_a);
-        stats[warp * kRowsTile + g + 8] = make_float2(m_b, l_b);
-      }
-    }
-    __syncthreads();
-    const int row = tid / 8, part = tid % 8, d0 = part * (D / 8), padded = d0 + d0 / (D / 4) * 4;
-    float o[D / 8], m = -INFINITY, l = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) m = fmaxf(m, stats[w * kRowsTile + row].x);
-#pragma unroll
-    for (int d = 0; d < D / 8; ++d) o[d] = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      const float2 st = stats[w * kRowsTile + row];
-      const float by = st.x == -INFINITY ? 0.0f : exp2_fast(st.x - m);
-      l += st.y * by;
-      const float* const from = sums + (w * kRowsTile + row) * L::kRowFloats + padded;
-#pragma unroll
-      for (int d = 0; d < D / 8; d += 4) {
-        const float4 f4 = *reinterpret_cast<const float4*>(from + d);
-        o[d] += f4.x * by;
-        o[d + 1] += f4.y * by;
-        o[d + 2] += f4.z * by;
-        o[d + 3] += f4.w * by;
-      }
-    }
-    bool write = row < rows;
-    if (k0 > 0 || k1 < keys) {                            // other CTAs have units of this tile
-      const unsigned long long tile_begin = unit - k0;
-      const int first = static_cast<int>(((tile_begin + 1) * ctas - 1) / total), last = static_cast<int>(((tile_begin + keys) * ctas - 1) / total);
-      constexpr int kSlot = kRowsTile * (D + 2);
-      float* const mine = p.partials + (2ll * blockIdx.x + (k0 > 0 ? 0 : 1)) * kSlot;
-      if (write) {
-#pragma unroll
-        for (int d = 0; d < D / 8; d += 4) *reinterpret_cast<float4*>(mine + row * D + d0 + d) = make_float4(o[d], o[d + 1], o[d + 2], o[d + 3]);
-        if (part == 0) *reinterpret_cast<float2*>(mine + kRowsTile * D + 2 * row) = make_float2(m, l);
-      }
-      __threadfence();
       __syncthreads();
-      if (tid == 0) s_last = atomicInc(p.counters + first, static_cast<unsigned>(last - first)) == static_cast<unsigned>(last - first);
-      __syncthreads();
-      write = write && s_last != 0u;
-      if (write) {
+      constexpr int kParts = kThreads / L::kRows, kDims = D / kParts;  // threads of a row, and what each has of it
+      const int row = tid / kParts, d0 = tid % kParts * kDims, padded = d0 + d0 / (D / 8) * 4;
+      float o[kDims], top = -INFINITY, all = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, stats[w * L::kRows + row].x);
+#pragma unroll
+      for (int d = 0; d < kDims; ++d) o[d] = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float2 st = stats[w * L::kRows + row];
+        const float by = st.x == -INFINITY ? 0.0f : exp2_fast(st.x - top);
+        all += st.y * by;
+        const float* const at = sums + (w * L::kRows + row) * L::kRowFloats + padded;
+#pragma unroll
+        for (int d = 0; d < kDims; d += 4) {
+          const float4 f4 = *reinterpret_cast<const float4*>(at + d);
+          o[d] += f4.x * by;
+          o[d + 1] += f4.y * by;
+          o[d + 2] += f4.z * by;
+          o[d + 3] += f4.w * by;
+        }
+      }
+      bool write = row < rows;
+      if (k0 > 0 || k1 < keys) {                            // other CTAs have units of this tile
+        const int first = static_cast<int>(((tile_begin + kTileUnits + 1) * ctas - 1) / total), last = static_cast<int>(((tile_begin + span) * ctas - 1) / total);
+        constexpr int kSlot = L::kRows * (D + 2);
+        float* const mine = p.partials + (2ll * blockIdx.x + (k0 > 0 ? 0 : 1)) * kSlot;
+        if (write) {
+#pragma unroll
+          for (int d = 0; d < kDims; d += 4) *reinterpret_cast<float4*>(mine + row * D + d0 + d) = make_float4(o[d], o[d + 1], o[d + 2], o[d + 3]);
+          if (d0 == 0) *reinterpret_cast<float2*>(mine + L::kRows * D + 2 * row) = make_float2(top, all);
+        }
         __threadfence();
-        m = -INFINITY;
-        l = 0.0f;
+        __syncthreads();
+        if (tid == 0) s_last = atomicInc(p.counters + first, static_cast<unsigned>(last - first)) == static_cast<unsigned>(last - first);
+        __syncthreads();
+        write = write && s_last != 0u;
+        if (write) {
+          __threadfence();
+          top = -INFINITY;
+          all = 0.0f;
 #pragma unroll
-        for (int d = 0; d < D / 8; ++d) o[d] = 0.0f;
-        for (int n = first; n <= last; ++n) {
-          const float* const from = p.partials + (2ll * n + (n == first ? 1 : 0)) * kSlot;
-          const float2 st = __ldcg(reinterpret_cast<const float2*>(from + kRowsTile * D + 2 * row));
-          const float top = fmaxf(m, st.x);
-          const float by = st.x == -INFINITY ? 0.0f : exp2_fast(st.x - top), old = m == -INFINITY ? 0.0f : exp2_fast(m - top);
-          m = top;
-          l = l * old + st.y * by;
+          for (int d = 0; d < kDims; ++d) o[d] = 0.0f;
+#pragma unroll 4
+          for (int n = first; n <= last; ++n) {
+            const float* const part = p.partials + (2ll * n + (n == first ? 1 : 0)) * kSlot;
+            const float2 st = __ldcg(reinterpret_cast<const float2*>(part + L::kRows * D + 2 * row));
+            const float now = fmaxf(top, st.x);
+            const float by = st.x == -INFINITY ? 0.0f : exp2_fast(st.x - now), old = top == -INFINITY ? 0.0f : exp2_fast(top - now);
+            top = now;
+            all = all * old + st.y * by;
 #pragma unroll
-          for (int d = 0; d < D / 8; d += 4) {
-            const float4 f4 = __ldcg(reinterpret_cast<const float4*>(from + row * D + d0 + d));
-            o[d] = o[d] * old + f4.x * by;
-            o[d + 1] = o[d + 1] * old + f4.y * by;
-            o[d + 2] = o[d + 2] * old + f4.z * by;
-            o[d + 3] = o[d + 3] * old + f4.w * by;
+            for (int d = 0; d < kDims; d += 4) {
+              const float4 f4 = __ldcg(reinterpret_cast<const float4*>(part + row * D + d0 + d));
+              o[d] = o[d] * old + f4.x * by;
+              o[d + 1] = o[d + 1] * old + f4.y * by;
+              o[d + 2] = o[d + 2] * old + f4.z * by;
+              o[d + 3] = o[d + 3] * old + f4.w * by;
+            }
           }
         }
       }
-    }
-    if (write) {
-      const float by = l == 0.0f ? 0.0f : 1.0f / l;
-      const int at = row0 + row;
-      uint16_t* const to = static_cast<uint16_t*>(p.out) + (r.start + at / p.group) * p.out_stride + (static_cast<long long>(head) * p.group + at % p.group) * D + d0;
-      uint32_t packed[D / 16];
+      if (write) {
+        const float by = all == 0.0f ? 0.0f : 1.0f / all;
+        const int at = row0 + row;
+        uint16_t* const to = static_cast<uint16_t*>(p.out) + (r.start + at / p.group) * p.out_stride + (static_cast<long long>(head) * p.group + at % p.group) * D + d0;
 #pragma unroll
-      for (int d = 0; d < D / 16; ++d) packed[d] = Elem<BF16>::pack_rn(o[2 * d] * by, o[2 * d + 1] * by);
-#pragma unroll
-      for (int d = 0; d < D / 16; d += 4) *reinterpret_cast<uint4*>(to + 2 * d) = make_uint4(packed[d], packed[d + 1], packed[d + 2], packed[d + 3]);
+        for (int d = 0; d < kDims; d += 4)
+          *reinterpret_cast<uint2*>(to + d) = make_uint2(Elem<BF16>::pack_rn(o[d] * by, o[d + 1] * by), Elem<BF16>::pack_rn(o[d + 2] * by, o[d + 3] * by));
+      }
     }
-    unit += k1 - k0;
-    rest += k1 - k0;
-    if (unit < unit_end && rest == r.units(kRowsTile, kUnitTokens, p)) {
+    if (unit < unit_end && rest == r.units(L::kRows, kUnitTokens, kTileUnits, p)) {
       do {
         r = request_of(p, ++i);
       } while (r.rows == 0 && i + 1 < p.requests);
@@ -415,21 +501,26 @@ __global__ void __launch_bounds__(kThreads, kRowsCtasPerSm) attention_rows_kerne
   }
 }
 
-template <bool BF16, int D>
-cudaError_t launch(const AttentionParams& p, int ctas, cudaStream_t stream) {
-  static_assert(Layout<D>::kBytes >= 8 * kMaxRequests || D == 64, "unit counts fit");
-  constexpr size_t smem = Layout<D>::kBytes > 8 * kMaxRequests ? Layout<D>::kBytes : 8 * kMaxRequests;
-  const size_t bytes = p.requests * 8ull > Layout<D>::kBytes ? smem : Layout<D>::kBytes;
-  const cudaError_t e = cudaFuncSetAttribute(attention_rows_kernel<BF16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+template <bool BF16, int D, int NT>
+cudaError_t launch(const AttentionParams& p, int sms, cudaStream_t stream) {
+  using L = Layout<D, NT>;
+  constexpr size_t most = L::kBytes > 8 * kMaxRequests ? L::kBytes : 8 * kMaxRequests;  // the unit counts lie in the same place
+  const size_t bytes = p.requests * 8ull > L::kBytes ? most : L::kBytes;
+  const cudaError_t e = cudaFuncSetAttribute(attention_rows_kernel<BF16, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most));
   if (e != cudaSuccess) return e;
-  return launch_overlapped(attention_rows_kernel<BF16, D>, ctas, kThreads, bytes, stream, p);
+  return launch_overlapped(attention_rows_kernel<BF16, D, NT>, sms * L::kCtasPerSm, kThreads, bytes, stream, p);
+}
+
+template <bool BF16, int D>
+cudaError_t launch(const AttentionParams& p, int sms, cudaStream_t stream) {
+  return static_cast<long long>(p.max_query) * p.group <= 8 ? launch<BF16, D, 1>(p, sms, stream) : launch<BF16, D, 2>(p, sms, stream);
 }
 
 }  // namespace
 
-cudaError_t launch_attention_rows(const AttentionParams& p, bool bf16, int head_dim, int ctas, cudaStream_t stream) {
-  if (head_dim == 128) return bf16 ? launch<true, 128>(p, ctas, stream) : launch<false, 128>(p, ctas, stream);
-  return bf16 ? launch<true, 64>(p, ctas, stream) : launch<false, 64>(p, ctas, stream);
+cudaError_t launch_attention_rows(const AttentionParams& p, bool bf16, int head_dim, int sms, cudaStream_t stream) {
+  if (head_dim == 128) return bf16 ? launch<true, 128>(p, sms, stream) : launch<false, 128>(p, sms, stream);
+  return bf16 ? launch<true, 64>(p, sms, stream) : launch<false, 64>(p, sms, stream);
 }
 
 }  // namespace tsq

@@ -661,9 +661,9 @@ cudaError_t launch(const AttentionParams& p, int ctas, cudaStream_t stream) {
 
 }  // namespace
 
-cudaError_t launch_attention_tiles(const AttentionParams& p, bool bf16, int head_dim, int ctas, cudaStream_t stream) {
-  if (head_dim == 128) return bf16 ? launch<true, 128>(p, ctas, stream) : launch<false, 128>(p, ctas, stream);
-  return bf16 ? launch<true, 64>(p, ctas, stream) : launch<false, 64>(p, ctas, stream);
+cudaError_t launch_attention_tiles(const AttentionParams& p, bool bf16, int head_dim, int sms, cudaStream_t stream) {
+  if (head_dim == 128) return bf16 ? launch<true, 128>(p, sms, stream) : launch<false, 128>(p, sms, stream);
+  return bf16 ? launch<true, 64>(p, sms, stream) : launch<false, 64>(p, sms, stream);
 }
 
 }  // namespace tsq
