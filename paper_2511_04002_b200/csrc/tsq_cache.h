@@ -28,11 +28,11 @@ struct AttentionParams {
   float* partials;                         // sums of tiles that several CTAs have a part of
 };
 
-// Up to 16 query rows (query heads of a key head times max_query): tiles of 8 rows, four CTAs per SM, or of 16 rows, three.  A CTA has one counter and two
-// slots of a tile's accumulators, maxima and sums in the workspace.
+// Up to 16 query rows (query heads of a key head times max_query): tiles of 8 rows, four CTAs per SM, or of 16 rows, three.  A CTA has a counter for each level of
+// the sums of parts and two slots of a tile's accumulators, maxima and sums in the workspace.
 constexpr int kRowsCtasPerSm = 4;            // the more of the two
 constexpr int kRowsTile = 16;                // likewise
-constexpr int kRowsCounters = 1, kRowsSlots = 2;
+constexpr int kRowsCounters = 3, kRowsSlots = 2;
 // More: tiles of 256 rows, one CTA per SM, a counter for each warp of 32 rows, four slots of 128 rows.
 constexpr int kTilesRows = 256;
 constexpr int kTilesCounters = 8, kTilesSlots = 4;

@@ -42,6 +42,24 @@ __device__ __forceinline__ Request request_of(const AttentionParams& p, int i) {
   return r;
 }
 
+// n * total / parts; 64-bit divisions only where the numbers need them
+__device__ __forceinline__ unsigned long long scaled(unsigned int n, unsigned long long total, unsigned int parts) {
+  const unsigned long long v = n * total;
+  return v >> 32 ? v / parts : static_cast<unsigned int>(v) / parts;
+}
+// The CTA whose share [c * total / ctas, (c + 1) * total / ctas) holds `unit`.
+__device__ __forceinline__ int owner_of(unsigned long long unit, unsigned long long total, unsigned int ctas) {
+  const unsigned long long v = (unit + 1) * ctas - 1;
+  return static_cast<int>(v >> 32 || total >> 32 ? v / total : static_cast<unsigned int>(v) / static_cast<unsigned int>(total));
+}
+// Counts an arrival and gives what was counted before; `most` sets the counter back to 0.  What the CTA's threads wrote in front of the barrier before this is
+// visible to the thread that counts last, and behind its next barrier to its CTA.
+__device__ __forceinline__ unsigned int count_arrival(unsigned int* counter, unsigned int most) {
+  unsigned int before;
+  asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(before) : "l"(counter), "r"(most) : "memory");
+  return before;
+}
+
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -12,6 +12,7 @@ constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kStepTokens = 16;              // tokens of a warp's step: within one page
 constexpr int kUnitTokens = kWarps * kStepTokens;
+constexpr int kFanIn = 16;                   // parts of a tile that are added up at once
 constexpr int kTileUnits = 2;                // what beginning and ending a tile costs, in units
 
 // One m16n8k16 product, binary16 in, binary32 sums.
@@ -67,26 +68,26 @@ __device__ __forceinline__ int placed(int t, int c) {
 }
 
 // The B operands of the products with the keys: thread (g, c) has of the rows row0 + 8 t + g of the tile (zeros past its `rows`) the dimensions
-// c * D / 4 ... in order, four per product step; brought to binary16 by a power of two per row.  factor: the inverses for the rows 8 t + 2 c and 8 t + 2 c + 1.
-template <bool BF16, int D, int NT>
-__device__ __forceinline__ void load_queries(const AttentionParams& p, const Request& r, int head, int row0, int rows, int g, int c, uint32_t (&q)[NT][D / 16][2],
-                                             float (&factor)[NT][2]) {
+// c * D / 4 ... in order, four per product step.  As they lie in memory:
+template <int D, int NT>
+__device__ __forceinline__ void read_queries(const AttentionParams& p, const Request& r, int head, int row0, int rows, int g, int c, uint4 (&raw)[NT][D / 32]) {
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int row = 8 * t + g, at = row0 + row;
+    const uint16_t* const from = static_cast<const uint16_t*>(p.q) + (r.start + at / p.group) * p.q_stride +
+                                 (static_cast<long long>(head) * p.group + at % p.group) * D + c * (D / 4);
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k) raw[t][k] = row < rows ? reinterpret_cast<const uint4*>(from)[k] : make_uint4(0u, 0u, 0u, 0u);
+  }
+}
+// brought to binary16 by a power of two per row.  factor: the inverses for the rows 8 t + 2 c and 8 t + 2 c + 1.
+template <bool BF16, int D, int NT>
+__device__ __forceinline__ void scale_queries(const uint4 (&raw)[NT][D / 32], int c, uint32_t (&q)[NT][D / 16][2], float (&factor)[NT][2]) {
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
     uint32_t w[D / 8];
-    if (row < rows) {
-      const uint16_t* const from = static_cast<const uint16_t*>(p.q) + (r.start + at / p.group) * p.q_stride +
-                                   (static_cast<long long>(head) * p.group + at % p.group) * D + c * (D / 4);
 #pragma unroll
-      for (int k = 0; k < D / 32; ++k) {
-        const uint4 v = reinterpret_cast<const uint4*>(from)[k];
-        w[4 * k] = v.x, w[4 * k + 1] = v.y, w[4 * k + 2] = v.z, w[4 * k + 3] = v.w;
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < D / 8; ++k) w[k] = 0u;
-    }
+    for (int k = 0; k < D / 32; ++k) w[4 * k] = raw[t][k].x, w[4 * k + 1] = raw[t][k].y, w[4 * k + 2] = raw[t][k].z, w[4 * k + 3] = raw[t][k].w;
     uint32_t top = 0u;
 #pragma unroll
     for (int k = 0; k < D / 8; ++k) top = max(top, max(w[k] & 0x7fffu, (w[k] >> 16) & 0x7fffu));
@@ -146,14 +147,17 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
   wait_for_prior_grids();
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, c = lane % 4;
 
-  // units in front of each request
-  unsigned long long* const s_units = reinterpret_cast<unsigned long long*>(smem);
-  unsigned long long total;
+  // the CTA's share, and the request that has its first unit: every thread sums its requests' units, and the one whose sums reach past the first unit tells the others
+  unsigned long long total, unit, unit_end;
+  unsigned int ctas;
   {
     const int per = (p.requests + kThreads - 1) / kThreads;
     const int i0 = min(tid * per, p.requests), i1 = min(i0 + per, p.requests);
-    unsigned long long mine = 0;
-    for (int i = i0; i < i1; ++i) mine += request_of(p, i).units(L::kRows, kUnitTokens, kTileUnits, p);
+    unsigned long long mine = 0, n = 0;
+    for (int i = i0; i < i1; ++i) {
+      n = request_of(p, i).units(L::kRows, kUnitTokens, kTileUnits, p);
+      mine += n;
+    }
     unsigned long long in = mine;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
@@ -161,6 +165,10 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
       if (lane >= d) in += up;
     }
     if (lane == 31) s_scan[warp] = in;
+    if (tid == 0) {
+      s_found = 0;
+      s_begin = 0;
+    }
     __syncthreads();
     unsigned long long at = in - mine;
     total = 0;
@@ -169,28 +177,23 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
       if (w < warp) at += s_scan[w];
       total += s_scan[w];
     }
-    for (int i = i0; i < i1; ++i) {
-      s_units[i] = at;
-      at += request_of(p, i).units(L::kRows, kUnitTokens, kTileUnits, p);
+    ctas = total < gridDim.x ? static_cast<unsigned int>(total) : gridDim.x;
+    if (blockIdx.x >= ctas) return;
+    unit = scaled(blockIdx.x, total, ctas);
+    unit_end = scaled(blockIdx.x + 1, total, ctas);
+    if (at <= unit && unit < at + mine) {
+      for (int i = i0; i < i1; ++i) {
+        if (per > 1) n = request_of(p, i).units(L::kRows, kUnitTokens, kTileUnits, p);
+        if (unit < at + n) {
+          s_found = i;
+          s_begin = at;
+          break;
+        }
+        at += n;
+      }
     }
+    __syncthreads();
   }
-  const unsigned long long ctas = total < gridDim.x ? total : gridDim.x;
-  if (blockIdx.x >= ctas) return;
-  unsigned long long unit = blockIdx.x * total / ctas;
-  const unsigned long long unit_end = (blockIdx.x + 1) * total / ctas;
-  if (tid == 0) {
-    s_found = 0;
-    s_begin = unit;
-  }
-  __syncthreads();
-  for (int i = tid; i < p.requests; i += kThreads) {
-    const unsigned long long begin = s_units[i], end = i + 1 < p.requests ? s_units[i + 1] : total;
-    if (begin <= unit && unit < end) {
-      s_found = i;
-      s_begin = begin;
-    }
-  }
-  __syncthreads();
   int i = s_found;
   unsigned long long rest = unit - s_begin;               // units of request i in front of `unit`
   Request r = request_of(p, i);
@@ -198,8 +201,8 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
 
   while (unit < unit_end) {
     const int tiles = r.tiles(L::kRows, p), keys = r.key_units(kUnitTokens), span = keys + kTileUnits;
-    const int head_tile = static_cast<int>(rest / span), head = head_tile / tiles, tile = head_tile % tiles;
-    const int from = static_cast<int>(rest % span), upto = static_cast<int>(min(static_cast<unsigned long long>(span), from + (unit_end - unit)));
+    const int head_tile = static_cast<int>(scaled(1, rest, span)), head = head_tile / tiles, tile = head_tile % tiles;
+    const int from = static_cast<int>(rest - static_cast<unsigned long long>(head_tile) * span), upto = static_cast<int>(min(static_cast<unsigned long long>(span), from + (unit_end - unit)));
     const int k0 = max(0, from - kTileUnits), k1 = max(0, upto - kTileUnits);
     const unsigned long long tile_begin = unit - from;
     unit += upto - from;
@@ -212,6 +215,8 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
       // ---- the first codes on their way ----
       const int base = k0 * kUnitTokens + warp * kStepTokens;
       const int n_steps = max(0, min(k1 - k0, (seen_last - base + kUnitTokens - 1) / kUnitTokens));
+      uint4 raw[NT][D / 32];
+      read_queries<D, NT>(p, r, head, row0, rows, g, c, raw);
       const int32_t* const table = p.table + static_cast<long long>(i) * p.table_pages;
       // page of step 32 b + lane, -1 where there is none
       auto page_of = [&](int b) {
@@ -251,15 +256,15 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
         }
         copies_commit();
       };
-      __syncthreads();                                      // the shared memory is free of the last tile's sums, and of the unit counts
+      __syncthreads();                                      // the shared memory is free of the last tile's sums
 #pragma unroll
       for (int s = 0; s < L::kStages - 1; ++s) issue(s);
 
       // ---- queries, scales ----
+      fetch_scales(page_0);
       uint32_t q[NT][kSteps][2];
       float factor[NT][2];                                  // of the rows 8 t + 2 c and 8 t + 2 c + 1, whose scores this thread has
-      load_queries<BF16, D, NT>(p, r, head, row0, rows, g, c, q, factor);
-      fetch_scales(page_0);
+      scale_queries<BF16, D, NT>(raw, c, q, factor);
       put_scales(0);
       if (n_steps > 32) {
         fetch_scales(page_1);
@@ -442,46 +447,61 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
           o[d + 3] += f4.w * by;
         }
       }
-      bool write = row < rows;
+      bool write = true;
       if (k0 > 0 || k1 < keys) {                            // other CTAs have units of this tile
-        const int first = static_cast<int>(((tile_begin + kTileUnits + 1) * ctas - 1) / total), last = static_cast<int>(((tile_begin + span) * ctas - 1) / total);
+        // Parts are added up sixteen at a time by the CTA that comes last of the sixteen, their sums likewise: the order does not depend on who comes when.
+        const int first = owner_of(tile_begin + kTileUnits, total, ctas), parts = owner_of(tile_begin + span - 1, total, ctas) - first + 1;
         constexpr int kSlot = L::kRows * (D + 2);
-        float* const mine = p.partials + (2ll * blockIdx.x + (k0 > 0 ? 0 : 1)) * kSlot;
-        if (write) {
+        const auto slot_of = [&](int n) { return p.partials + (2ll * (first + n) + (n == 0 ? 1 : 0)) * kSlot; };
+        int part = static_cast<int>(blockIdx.x) - first;
+        unsigned int* counters = p.counters;
+        for (int stride = 1; stride < parts && write; stride *= kFanIn, counters += gridDim.x) {
+          const int begin = part / (kFanIn * stride) * (kFanIn * stride), members = min(kFanIn, (parts - begin + stride - 1) / stride);
+          if (members > 1) {
+            float* const mine = slot_of(part);
+            if (row < rows) {
 #pragma unroll
-          for (int d = 0; d < kDims; d += 4) *reinterpret_cast<float4*>(mine + row * D + d0 + d) = make_float4(o[d], o[d + 1], o[d + 2], o[d + 3]);
-          if (d0 == 0) *reinterpret_cast<float2*>(mine + L::kRows * D + 2 * row) = make_float2(top, all);
-        }
-        __threadfence();
-        __syncthreads();
-        if (tid == 0) s_last = atomicInc(p.counters + first, static_cast<unsigned>(last - first)) == static_cast<unsigned>(last - first);
-        __syncthreads();
-        write = write && s_last != 0u;
-        if (write) {
-          __threadfence();
-          top = -INFINITY;
-          all = 0.0f;
-#pragma unroll
-          for (int d = 0; d < kDims; ++d) o[d] = 0.0f;
-#pragma unroll 4
-          for (int n = first; n <= last; ++n) {
-            const float* const part = p.partials + (2ll * n + (n == first ? 1 : 0)) * kSlot;
-            const float2 st = __ldcg(reinterpret_cast<const float2*>(part + L::kRows * D + 2 * row));
-            const float now = fmaxf(top, st.x);
-            const float by = st.x == -INFINITY ? 0.0f : exp2_fast(st.x - now), old = top == -INFINITY ? 0.0f : exp2_fast(top - now);
-            top = now;
-            all = all * old + st.y * by;
-#pragma unroll
-            for (int d = 0; d < kDims; d += 4) {
-              const float4 f4 = __ldcg(reinterpret_cast<const float4*>(part + row * D + d0 + d));
-              o[d] = o[d] * old + f4.x * by;
-              o[d + 1] = o[d + 1] * old + f4.y * by;
-              o[d + 2] = o[d + 2] * old + f4.z * by;
-              o[d + 3] = o[d + 3] * old + f4.w * by;
+              for (int d = 0; d < kDims; d += 4) *reinterpret_cast<float4*>(mine + row * D + d0 + d) = make_float4(o[d], o[d + 1], o[d + 2], o[d + 3]);
+              if (d0 == 0) *reinterpret_cast<float2*>(mine + L::kRows * D + 2 * row) = make_float2(top, all);
             }
+            __syncthreads();
+            if (tid == 0) s_last = count_arrival(counters + first + begin, static_cast<unsigned>(members - 1)) == static_cast<unsigned>(members - 1);
+            __syncthreads();
+            write = s_last != 0u;
+            if (write && row < rows) {
+              float2 st[kFanIn];
+              top = -INFINITY;
+#pragma unroll
+              for (int n = 0; n < kFanIn; ++n) {
+                st[n] = n < members ? __ldcg(reinterpret_cast<const float2*>(slot_of(begin + n * stride) + L::kRows * D) + row) : make_float2(-INFINITY, 0.0f);
+              }
+#pragma unroll
+              for (int n = 0; n < kFanIn; ++n) top = fmaxf(top, st[n].x);
+              all = 0.0f;
+#pragma unroll
+              for (int d = 0; d < kDims; ++d) o[d] = 0.0f;
+#pragma unroll
+              for (int n = 0; n < kFanIn; ++n) {
+                if (n < members) {
+                  const float by = st[n].x == -INFINITY ? 0.0f : exp2_fast(st[n].x - top);
+                  all = __fmaf_rn(st[n].y, by, all);
+#pragma unroll
+                  for (int d = 0; d < kDims; d += 4) {
+                    const float4 f4 = __ldcg(reinterpret_cast<const float4*>(slot_of(begin + n * stride) + row * D + d0 + d));
+                    o[d] = __fmaf_rn(f4.x, by, o[d]);
+                    o[d + 1] = __fmaf_rn(f4.y, by, o[d + 1]);
+                    o[d + 2] = __fmaf_rn(f4.z, by, o[d + 2]);
+                    o[d + 3] = __fmaf_rn(f4.w, by, o[d + 3]);
+                  }
+                }
+              }
+            }
+            __syncthreads();                                // every thread has read what the next level writes over
           }
+          part = begin;
         }
       }
+      write = write && row < rows;
       if (write) {
         const float by = all == 0.0f ? 0.0f : 1.0f / all;
         const int at = row0 + row;
@@ -504,11 +524,9 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
 template <bool BF16, int D, int NT>
 cudaError_t launch(const AttentionParams& p, int sms, cudaStream_t stream) {
   using L = Layout<D, NT>;
-  constexpr size_t most = L::kBytes > 8 * kMaxRequests ? L::kBytes : 8 * kMaxRequests;  // the unit counts lie in the same place
-  const size_t bytes = p.requests * 8ull > L::kBytes ? most : L::kBytes;
-  const cudaError_t e = cudaFuncSetAttribute(attention_rows_kernel<BF16, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most));
+  const cudaError_t e = cudaFuncSetAttribute(attention_rows_kernel<BF16, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
   if (e != cudaSuccess) return e;
-  return launch_overlapped(attention_rows_kernel<BF16, D, NT>, sms * L::kCtasPerSm, kThreads, bytes, stream, p);
+  return launch_overlapped(attention_rows_kernel<BF16, D, NT>, sms * L::kCtasPerSm, kThreads, static_cast<size_t>(L::kBytes), stream, p);
 }
 
 template <bool BF16, int D>
