@@ -469,29 +469,40 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
             __syncthreads();
             write = s_last != 0u;
             if (write && row < rows) {
+              // loads without a branch between them, so that many are on their way: past the last part its data again, with weight 0
+              const auto part_at = [&](int n) { return slot_of(begin + min(n, members - 1) * stride); };
               float2 st[kFanIn];
+#pragma unroll
+              for (int n = 0; n < kFanIn; ++n) st[n] = __ldcg(reinterpret_cast<const float2*>(part_at(n) + L::kRows * D) + row);
               top = -INFINITY;
 #pragma unroll
               for (int n = 0; n < kFanIn; ++n) {
-                st[n] = n < members ? __ldcg(reinterpret_cast<const float2*>(slot_of(begin + n * stride) + L::kRows * D) + row) : make_float2(-INFINITY, 0.0f);
+                if (n >= members) st[n] = make_float2(-INFINITY, 0.0f);
+                top = fmaxf(top, st[n].x);
               }
-#pragma unroll
-              for (int n = 0; n < kFanIn; ++n) top = fmaxf(top, st[n].x);
               all = 0.0f;
 #pragma unroll
               for (int d = 0; d < kDims; ++d) o[d] = 0.0f;
+              constexpr int kBatch = 64 / kDims < kFanIn ? 64 / kDims : kFanIn;
 #pragma unroll
-              for (int n = 0; n < kFanIn; ++n) {
-                if (n < members) {
-                  const float by = st[n].x == -INFINITY ? 0.0f : exp2_fast(st[n].x - top);
-                  all = __fmaf_rn(st[n].y, by, all);
+              for (int n0 = 0; n0 < kFanIn; n0 += kBatch) {
+                if (n0 >= members) break;
+                float4 x[kBatch][kDims / 4];
 #pragma unroll
-                  for (int d = 0; d < kDims; d += 4) {
-                    const float4 f4 = __ldcg(reinterpret_cast<const float4*>(slot_of(begin + n * stride) + row * D + d0 + d));
-                    o[d] = __fmaf_rn(f4.x, by, o[d]);
-                    o[d + 1] = __fmaf_rn(f4.y, by, o[d + 1]);
-                    o[d + 2] = __fmaf_rn(f4.z, by, o[d + 2]);
-                    o[d + 3] = __fmaf_rn(f4.w, by, o[d + 3]);
+                for (int n = 0; n < kBatch; ++n) {
+#pragma unroll
+                  for (int d = 0; d < kDims / 4; ++d) x[n][d] = __ldcg(reinterpret_cast<const float4*>(part_at(n0 + n) + row * D + d0) + d);
+                }
+#pragma unroll
+                for (int n = 0; n < kBatch; ++n) {
+                  const float by = st[n0 + n].x == -INFINITY ? 0.0f : exp2_fast(st[n0 + n].x - top);
+                  all = __fmaf_rn(st[n0 + n].y, by, all);
+#pragma unroll
+                  for (int d = 0; d < kDims / 4; ++d) {
+                    o[4 * d] = __fmaf_rn(x[n][d].x, by, o[4 * d]);
+                    o[4 * d + 1] = __fmaf_rn(x[n][d].y, by, o[4 * d + 1]);
+                    o[4 * d + 2] = __fmaf_rn(x[n][d].z, by, o[4 * d + 2]);
+                    o[4 * d + 3] = __fmaf_rn(x[n][d].w, by, o[4 * d + 3]);
                   }
                 }
               }
