@@ -37,7 +37,7 @@ __device__ __forceinline__ long long warp_scan(long long v) {
 
 // Exclusive sums of tokens and new pages over the requests, by every CTA for itself: the lengths are a few kilobytes that come out of L2, and nothing has to
 // be waited for.  Then a thread per token: the request by bisection, the page from the table or, where the step begins it, from the free
-// list.  The token at a page's first place also writes the table's entry, so no entry is read that this call writes.
+// list.  The token at a page's first place also writes the table's entry; no entry is read that this call writes.
 // Bound by latency: two dependent reads and a scan (64 requests), and by the slots written (262144 tokens 1 MB).
 __global__ void __launch_bounds__(kSlotThreads) slots_kernel(const SlotParams p) {
   extern __shared__ int32_t s_requests[];  // [requests + 1] first token, [requests] rank of the first new page
@@ -92,39 +92,64 @@ __global__ void __launch_bounds__(kSlotThreads) slots_kernel(const SlotParams p)
     }
   }
   __syncthreads();
-  // every new token, with a row in slots or without one, and the rows behind the last request's
+  // every new token, with a row in slots or without one, and the rows behind the last request's: four neighbours for each thread, which mostly have
+  // the request and often the page in common
   const long long total = s_start[p.requests], end = max(total, p.tokens);
-  for (long long t = static_cast<long long>(blockIdx.x) * kSlotThreads + tid; t < end; t += static_cast<long long>(gridDim.x) * kSlotThreads) {
-    int32_t slot = -1;
-    if (t < total) {
-      int lo = 0, hi = p.requests - 1;  // the last request that starts at or in front of t: the one that has it
+  for (long long t0 = 4ll * (static_cast<long long>(blockIdx.x) * kSlotThreads + tid); t0 < end; t0 += 4ll * gridDim.x * kSlotThreads) {
+    int32_t slot[4] = {-1, -1, -1, -1};
+    if (t0 < total) {
+      int lo = 0, hi = p.requests - 1;  // the last request that starts at or in front of t0: the one that has it
       while (lo < hi) {
         const int mid = (lo + hi + 1) / 2;
-        if (s_start[mid] <= t) {
+        if (s_start[mid] <= t0) {
           lo = mid;
         } else {
           hi = mid - 1;
         }
       }
-      const long long held = max(p.held[lo], 0);
-      const long long position = held + (t - s_start[lo]);
-      const long long entry = position >> p.page_shift, first = (held + P - 1) >> p.page_shift;
-      const int place = static_cast<int>(position & (P - 1));
+      long long held = max(p.held[lo], 0), known = -1;  // known: the entry that `page` is of
       int32_t page = -1;
-      if (entry < p.table_pages) {
-        int32_t* const cell = p.table + static_cast<long long>(lo) * p.table_pages + entry;
-        if (entry < first) {
-          page = *cell;
-        } else {
-          const long long r = s_rank[lo] + (entry - first);
-          page = r < p.n_free ? p.free_pages[r] : -1;
-          if (place == 0) *cell = page;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const long long t = t0 + k;
+        if (t >= total) break;
+        if (t >= s_start[lo + 1]) {
+          do {
+            ++lo;
+          } while (t >= s_start[lo + 1]);  // below the total, so there is one
+          held = max(p.held[lo], 0);
+          known = -1;
         }
+        const long long position = held + (t - s_start[lo]);
+        const long long entry = position >> p.page_shift;
+        const int place = static_cast<int>(position & (P - 1));
+        if (entry != known) {
+          const long long first = (held + P - 1) >> p.page_shift;
+          known = entry;
+          page = -1;
+          if (entry < p.table_pages) {
+            int32_t* const cell = p.table + static_cast<long long>(lo) * p.table_pages + entry;
+            if (entry < first) {
+              page = *cell;
+            } else {
+              const long long r = s_rank[lo] + (entry - first);
+              page = r < p.n_free ? p.free_pages[r] : -1;
+              if (place == 0) *cell = page;
+            }
+          }
+        }
+        const long long at = (static_cast<long long>(page) << p.page_shift) + place;
+        if (page >= 0 && at <= most) slot[k] = static_cast<int32_t>(at);
       }
-      const long long at = (static_cast<long long>(page) << p.page_shift) + place;
-      if (page >= 0 && at <= most) slot = static_cast<int32_t>(at);
     }
-    if (t < p.tokens) p.slots[t] = slot;
+    if (t0 + 4 <= p.tokens && (reinterpret_cast<uintptr_t>(p.slots) & 15u) == 0) {
+      *reinterpret_cast<int4*>(p.slots + t0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (t0 + k < p.tokens) p.slots[t0 + k] = slot[k];
+      }
+    }
   }
 }
 
@@ -150,17 +175,26 @@ __device__ __forceinline__ uint32_t code_of(float x, float inverse) {
 }
 __device__ __forceinline__ int signed_byte(uint32_t w, int i) { return static_cast<int>(w << (24 - 8 * i)) >> 24; }
 
+// Four codes of one word from products in (-127.5, 127.5), each rounded by itself (mul and add on packed pairs came out as one operation): adding 1.5 * 2^23 rounds to the nearest integer (even in a tie) and leaves it in the low byte.
+__device__ __forceinline__ uint32_t codes_of(uint64_t x01, uint64_t x23) {
+  const uint64_t magic = pack2f(12582912.0f, 12582912.0f);
+  uint32_t t0, t1, t2, t3;
+  unpack2u(add2(x01, magic), t0, t1);
+  unpack2u(add2(x23, magic), t2, t3);
+  return __byte_perm(__byte_perm(t0, t1, 0x0040), __byte_perm(t2, t3, 0x0040), 0x5410);
+}
+
 // One CTA per head, keys or values, and block of tokens: for every run (tokens of one page) that begins in the block, the run's rows are read once into
-// registers, the largest finite |x| is reduced on the 15-bit patterns, and the codes are formed from the registers.  A page that was begun earlier has its codes
-// rescaled only when the scale grows.  Block: as many tokens as leave a few CTAs per SM, a page's run at most (store_block).
+// registers, the largest finite |x| is reduced on the 15-bit patterns, and the codes are formed from the registers.  The rows of the block are read while
+// the slots are still on their way; a run that begins with the block, the usual one, then only needs the rows past it.  A page that was begun earlier has its codes
+// rescaled only when the scale grows.  Block: as many tokens as leave a few CTAs per SM, a page's run at most (tsq_cache_store).
 template <bool BF16, int D, int P>
 __global__ void __launch_bounds__(kStoreThreads) store_kernel(const StoreParams p) {
   constexpr int kRowChunks = D / 8;                                    // 16-byte chunks of a row
   constexpr int kItems = (P * kRowChunks + kStoreThreads - 1) / kStoreThreads;
   __shared__ int32_t s_slot[kStoreBlock + P + 1];
-  __shared__ uint32_t s_lead[kStoreThreads / 32], s_max[kStoreThreads / 32], s_ok[kStoreThreads / 32];
+  __shared__ uint32_t s_max[2][kStoreThreads / 32];
   launch_dependents();
-  wait_for_prior_grids();
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   const int parts = 2 * p.heads;
   const long long t0 = static_cast<long long>(blockIdx.x / parts) * p.block;
@@ -169,61 +203,63 @@ __global__ void __launch_bounds__(kStoreThreads) store_kernel(const StoreParams 
   const long long stride = which ? p.v_stride : p.k_stride;
   int8_t* const codes = which ? p.v_codes : p.k_codes;
   float* const scales = which ? p.v_scale : p.k_scale;
+  const int early = static_cast<int>(min(static_cast<long long>(min(p.block, P)), p.tokens - t0));
+  wait_for_prior_grids();
   // s_slot[1 + i] is the slot of token t0 + i, s_slot[0] that of the token in front; -1: none
   for (int i = tid; i < p.block + P + 1; i += kStoreThreads) {
     const long long t = t0 + i - 1;
     const int32_t slot = t >= 0 && t < p.tokens ? p.slots[t] : -1;
     s_slot[i] = static_cast<uint32_t>(slot) < p.n_slots ? slot : -1;
   }
+  uint4 v[kItems];
+  const auto read_rows = [&](int j, int from, int to) {  // rows from .. to of the run that begins at token j of the block
+#pragma unroll
+    for (int it = 0; it < kItems; ++it) {
+      const int item = it * kStoreThreads + tid, row = item / kRowChunks;
+      if (row >= from && row < to) v[it] = __ldcs(reinterpret_cast<const uint4*>(x + (t0 + j + row) * stride + head * D) + item % kRowChunks);
+    }
+  };
+  read_rows(0, 0, early);
   __syncthreads();
-  bool leads = false;
-  if (tid < p.block) {
-    const int32_t slot = s_slot[1 + tid];
-    leads = slot >= 0 && (slot % P == 0 || s_slot[tid] != slot - 1);
-  }
-  const uint32_t mine = __ballot_sync(kFull, leads);
-  if (lane == 0) s_lead[warp] = mine;
-  __syncthreads();
-  for (int w = 0; w < kStoreBlock / 32; ++w) {
-    for (uint32_t left = s_lead[w]; left != 0; left &= left - 1) {
-      const int j = 32 * w + __ffs(static_cast<int>(left)) - 1;
+  int turn = 0;
+  for (int w = 0; w < p.block; w += 32) {
+    // every warp for itself, from the same slots
+    const int32_t its = w + lane < p.block ? s_slot[1 + w + lane] : -1;
+    const bool leads = its >= 0 && (its % P == 0 || s_slot[w + lane] != its - 1);
+    for (uint32_t left = __ballot_sync(kFull, leads); left != 0; left &= left - 1) {
+      const int j = w + __ffs(static_cast<int>(left)) - 1;
       const int32_t slot = s_slot[1 + j];
       const int place = slot % P;
-      // length of the run
-      const bool on = tid < P && place + tid < P && s_slot[1 + j + (tid < P ? tid : 0)] == slot + tid;
-      const uint32_t ok = __ballot_sync(kFull, on);
-      if (lane == 0) s_ok[warp] = ok;
-      __syncthreads();
-      int n = 0;
+      int n = 0;                                                       // length of the run
 #pragma unroll
-      for (int v = 0; v < kStoreThreads / 32; ++v) {
-        if (n == 32 * v) n += s_ok[v] == kFull ? 32 : __ffs(static_cast<int>(~s_ok[v])) - 1;
+      for (int u = 0; u < P; u += 32) {
+        const int i = u + lane;
+        const uint32_t on = __ballot_sync(kFull, i < P && place + i < P && s_slot[1 + j + (i < P ? i : 0)] == slot + i);
+        if (n == u) n += on == kFull ? 32 : __ffs(static_cast<int>(~on)) - 1;
       }
       const long long page_head = static_cast<long long>(slot / P) * p.heads + head;
       const float had = place > 0 ? scales[page_head] : 0.0f;
-      uint4 v[kItems];
-      uint32_t top = 0u;
+      read_rows(j, j == 0 ? early : 0, n);
+      uint32_t top = 0u, odd = 0u;
 #pragma unroll
       for (int it = 0; it < kItems; ++it) {
-        const int item = it * kStoreThreads + tid, row = item / kRowChunks;
-        v[it] = make_uint4(0u, 0u, 0u, 0u);
-        if (row < n) v[it] = __ldcs(reinterpret_cast<const uint4*>(x + (t0 + j + row) * stride + head * D) + item % kRowChunks);
-      }
-#pragma unroll
-      for (int it = 0; it < kItems; ++it) {
+        if ((it * kStoreThreads + tid) / kRowChunks >= n) v[it] = make_uint4(0u, 0u, 0u, 0u);
         const uint32_t words[4] = {v[it].x, v[it].y, v[it].z, v[it].w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const uint32_t lo = words[k] & 0x7fffu, hi = (words[k] >> 16) & 0x7fffu;
           if (lo < Elem<BF16>::kInfPattern) top = max(top, lo);
           if (hi < Elem<BF16>::kInfPattern) top = max(top, hi);
+          odd = max(odd, max(lo, hi));
         }
       }
+      const bool finite = odd < Elem<BF16>::kInfPattern;               // of this thread's values
       top = __reduce_max_sync(kFull, top);
-      if (lane == 0) s_max[warp] = top;
+      if (lane == 0) s_max[turn][warp] = top;
       __syncthreads();
 #pragma unroll
-      for (int u = 0; u < kStoreThreads / 32; ++u) top = max(top, s_max[u]);
+      for (int u = 0; u < kStoreThreads / 32; ++u) top = max(top, s_max[turn][u]);
+      turn ^= 1;
       const float scale = fmaxf(fmaxf(Elem<BF16>::pattern_f32(top) / 127.0f, kScaleFloor), had);
       const float inverse = 1.0f / scale;
       int8_t* const page_codes = codes + page_head * (P * D);
@@ -235,9 +271,14 @@ __global__ void __launch_bounds__(kStoreThreads) store_kernel(const StoreParams 
         uint32_t out[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const uint32_t a = code_of(Elem<BF16>::lo_f32(words[2 * k]), inverse) | code_of(Elem<BF16>::hi_f32(words[2 * k]), inverse) << 8;
-          const uint32_t b = code_of(Elem<BF16>::lo_f32(words[2 * k + 1]), inverse) | code_of(Elem<BF16>::hi_f32(words[2 * k + 1]), inverse) << 8;
-          out[k] = a | b << 16;
+          const float x0 = Elem<BF16>::lo_f32(words[2 * k]), x1 = Elem<BF16>::hi_f32(words[2 * k]), x2 = Elem<BF16>::lo_f32(words[2 * k + 1]),
+                      x3 = Elem<BF16>::hi_f32(words[2 * k + 1]);
+          if (finite) {
+            // |x| <= 127 s up to three roundings: the code is within +-127 without a clamp
+            out[k] = codes_of(pack2f(__fmul_rn(x0, inverse), __fmul_rn(x1, inverse)), pack2f(__fmul_rn(x2, inverse), __fmul_rn(x3, inverse)));
+          } else {
+            out[k] = code_of(x0, inverse) | code_of(x1, inverse) << 8 | code_of(x2, inverse) << 16 | code_of(x3, inverse) << 24;
+          }
         }
         *reinterpret_cast<uint2*>(page_codes + (place + row) * D + (item % kRowChunks) * 8) = make_uint2(out[0], out[1]);
       }
@@ -245,7 +286,7 @@ __global__ void __launch_bounds__(kStoreThreads) store_kernel(const StoreParams 
         const float ratio = had / scale;
         for (int item = tid; item < place * (D / 16); item += kStoreThreads) {
           uint4* const at = reinterpret_cast<uint4*>(page_codes) + item;
-          uint4 c = *at;
+          const uint4 c = *at;
           uint32_t words[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
@@ -257,8 +298,7 @@ __global__ void __launch_bounds__(kStoreThreads) store_kernel(const StoreParams 
           *at = make_uint4(words[0], words[1], words[2], words[3]);
         }
       }
-      if (tid == 0) scales[page_head] = scale;
-      __syncthreads();  // s_ok and s_max are free again
+      if (tid == 0) scales[page_head] = scale;                         // read by every thread in front of the barrier above
     }
   }
 }
@@ -266,6 +306,7 @@ __global__ void __launch_bounds__(kStoreThreads) store_kernel(const StoreParams 
 // ---- reading tokens back -------------------------------------------------------------------------
 
 constexpr int kLoadThreads = 256;
+constexpr int kLoadItems = 4;             // most chunks of a thread
 
 struct LoadParams {
   const int8_t *k_codes, *v_codes;
@@ -277,35 +318,64 @@ struct LoadParams {
   uint32_t n_slots;
 };
 
-// A thread per 16 codes: one 16-byte load, two 16-byte stores.  Bound by HBM.
+// The four codes of a word (sign bits inverted) times a scale: 2^23 + byte less 2^23 + 128 is the code, exactly.
+__device__ __forceinline__ void widen4(uint32_t u, float scale, float (&x)[4]) {
+#pragma unroll
+  for (int b = 0; b < 4; ++b) x[b] = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440 + b)) - 8388736.0f) * scale;
+}
+
+// A thread per 16 codes: one 16-byte load, two 16-byte stores; a thread has up to four, whose loads are on their way together.  Bound by HBM.
 template <bool BF16, int D>
 __global__ void __launch_bounds__(kLoadThreads) load_kernel(const LoadParams p) {
   launch_dependents();
-  wait_for_prior_grids();
   const uint32_t row = static_cast<uint32_t>(p.heads) * (D / 16);          // chunks of a token's keys
   const long long t0 = static_cast<long long>(blockIdx.x) * p.block;
-  const uint32_t rows = static_cast<uint32_t>(min(static_cast<long long>(p.block), p.tokens - t0));
-  for (uint32_t item = threadIdx.x; item < rows * row * 2u; item += kLoadThreads) {
-    const uint32_t which = item >= rows * row ? 1u : 0u, in = item - which * rows * row;
-    const uint32_t r = in / row, chunk = in - r * row, head = chunk / (D / 16), c = chunk % (D / 16);
-    const uint32_t slot = static_cast<uint32_t>(p.slots[t0 + r]);
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
-    float scale = 0.0f;
-    if (slot < p.n_slots) {
-      const long long page_head = static_cast<long long>(slot >> p.page_shift) * p.heads + head;
-      const uint4 v = __ldcs(reinterpret_cast<const uint4*>((which ? p.v_codes : p.k_codes) + ((page_head << p.page_shift) + (slot & ((1u << p.page_shift) - 1u))) * D) + c);
-      scale = (which ? p.v_scale : p.k_scale)[page_head];
-      w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-    }
-    uint32_t out[8];
+  const uint32_t rows = static_cast<uint32_t>(min(static_cast<long long>(p.block), p.tokens - t0)), items = rows * row * 2u;
+  wait_for_prior_grids();
+  for (uint32_t first = threadIdx.x; first < items; first += kLoadItems * kLoadThreads) {
+    uint32_t slot[kLoadItems], head[kLoadItems], chunk[kLoadItems];
+    uint16_t* to[kLoadItems];
+    const int8_t* codes[kLoadItems];
+    const float* scales[kLoadItems];
+    uint4 code[kLoadItems];
+    float scale[kLoadItems];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      out[k] = Elem<BF16>::pack_rn(static_cast<float>(signed_byte(w[k / 2], (k & 1) * 2)) * scale,
-                                   static_cast<float>(signed_byte(w[k / 2], (k & 1) * 2 + 1)) * scale);
+    for (int n = 0; n < kLoadItems; ++n) {
+      const uint32_t item = min(first + n * kLoadThreads, items - 1u);
+      const bool values = item >= rows * row;
+      const uint32_t in = values ? item - rows * row : item, r = in / row, of_row = in - r * row;
+      head[n] = of_row / (D / 16);
+      chunk[n] = of_row % (D / 16);
+      slot[n] = static_cast<uint32_t>(p.slots[t0 + r]);
+      to[n] = (values ? p.v : p.k) + (t0 + r) * (values ? p.v_stride : p.k_stride) + head[n] * D + chunk[n] * 16;
+      codes[n] = values ? p.v_codes : p.k_codes;
+      scales[n] = values ? p.v_scale : p.k_scale;
     }
-    uint4* const to = reinterpret_cast<uint4*>((which ? p.v : p.k) + (t0 + r) * (which ? p.v_stride : p.k_stride) + head * D + c * 16);
-    __stcs(to, make_uint4(out[0], out[1], out[2], out[3]));
-    __stcs(to + 1, make_uint4(out[4], out[5], out[6], out[7]));
+#pragma unroll
+    for (int n = 0; n < kLoadItems; ++n) {
+      code[n] = make_uint4(0u, 0u, 0u, 0u);
+      scale[n] = 0.0f;
+      if (slot[n] < p.n_slots) {
+        const long long page_head = static_cast<long long>(slot[n] >> p.page_shift) * p.heads + head[n];
+        code[n] = __ldcs(reinterpret_cast<const uint4*>(codes[n] + ((page_head << p.page_shift) + (slot[n] & ((1u << p.page_shift) - 1u))) * D) + chunk[n]);
+        scale[n] = scales[n][page_head];
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < kLoadItems; ++n) {
+      if (first + n * kLoadThreads >= items) break;
+      const uint32_t w[4] = {code[n].x ^ 0x80808080u, code[n].y ^ 0x80808080u, code[n].z ^ 0x80808080u, code[n].w ^ 0x80808080u};
+      uint32_t out[8];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float x[4];
+        widen4(w[k], scale[n], x);
+        out[2 * k] = Elem<BF16>::pack_rn(x[0], x[1]);
+        out[2 * k + 1] = Elem<BF16>::pack_rn(x[2], x[3]);
+      }
+      __stcs(reinterpret_cast<uint4*>(to[n]), make_uint4(out[0], out[1], out[2], out[3]));
+      __stcs(reinterpret_cast<uint4*>(to[n]) + 1, make_uint4(out[4], out[5], out[6], out[7]));
+    }
   }
 }
 
@@ -483,7 +553,10 @@ tsq_status_t tsq_cache_load(const tsq_cache_t* cache, const int32_t* slots, int6
   p.page_shift = page_shift(cache->page_tokens);
   p.n_slots = static_cast<uint32_t>(cache->pages * cache->page_tokens);
   const int row = 2 * cache->kv_heads * (cache->head_dim / 16);
-  p.block = std::max(1, 4 * kLoadThreads / row);
+  // as many tokens as give each thread four chunks, fewer where that would leave SMs without work
+  const int sms = current_sms();
+  if (sms < 1) return launched(cudaErrorInvalidDevice);
+  p.block = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kLoadItems * kLoadThreads / row, tokens / (2 * sms))));
   const int grid = static_cast<int>((tokens + p.block - 1) / p.block);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const bool bf16 = cache->dtype == TSQ_BF16;
