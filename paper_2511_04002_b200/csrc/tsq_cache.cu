@@ -155,7 +155,8 @@ __global__ void __launch_bounds__(kSlotThreads) slots_kernel(const SlotParams p)
 
 // ---- quantising into the cache -------------------------------------------------------------------
 
-constexpr int kStoreThreads = 128;
+constexpr int kStoreItems = 4;            // 16-byte chunks of a thread
+__host__ __device__ constexpr int store_threads(int d, int page) { return d * page / (8 * kStoreItems) > 64 ? d * page / (8 * kStoreItems) : 64; }
 constexpr int kStoreBlock = 64;           // most tokens whose runs one CTA looks after
 constexpr float kScaleFloor = 9.094947017729282e-13f;  // 2^-40
 
@@ -189,7 +190,8 @@ __device__ __forceinline__ uint32_t codes_of(uint64_t x01, uint64_t x23) {
 // the slots are still on their way; a run that begins with the block, the usual one, then only needs the rows past it.  A page that was begun earlier has its codes
 // rescaled only when the scale grows.  Block: as many tokens as leave a few CTAs per SM, a page's run at most (tsq_cache_store).
 template <bool BF16, int D, int P>
-__global__ void __launch_bounds__(kStoreThreads) store_kernel(const StoreParams p) {
+__global__ void __launch_bounds__(store_threads(D, P)) store_kernel(const StoreParams p) {
+  constexpr int kStoreThreads = store_threads(D, P);
   constexpr int kRowChunks = D / 8;                                    // 16-byte chunks of a row
   constexpr int kItems = (P * kRowChunks + kStoreThreads - 1) / kStoreThreads;
   __shared__ int32_t s_slot[kStoreBlock + P + 1];
@@ -212,11 +214,14 @@ __global__ void __launch_bounds__(kStoreThreads) store_kernel(const StoreParams 
     s_slot[i] = static_cast<uint32_t>(slot) < p.n_slots ? slot : -1;
   }
   uint4 v[kItems];
+  constexpr int kRowStep = kStoreThreads / kRowChunks;                 // rows from one of a thread's chunks to the next
+  const int my_row = tid / kRowChunks;
+  const uint16_t* const my_x = x + (t0 + my_row) * stride + head * D + tid % kRowChunks * 8;
   const auto read_rows = [&](int j, int from, int to) {  // rows from .. to of the run that begins at token j of the block
 #pragma unroll
     for (int it = 0; it < kItems; ++it) {
-      const int item = it * kStoreThreads + tid, row = item / kRowChunks;
-      if (row >= from && row < to) v[it] = __ldcs(reinterpret_cast<const uint4*>(x + (t0 + j + row) * stride + head * D) + item % kRowChunks);
+      const int row = my_row + it * kRowStep;
+      if (row >= from && row < to) v[it] = __ldcs(reinterpret_cast<const uint4*>(my_x + (j + it * kRowStep) * stride));
     }
   };
   read_rows(0, 0, early);
@@ -240,20 +245,27 @@ __global__ void __launch_bounds__(kStoreThreads) store_kernel(const StoreParams 
       const long long page_head = static_cast<long long>(slot / P) * p.heads + head;
       const float had = place > 0 ? scales[page_head] : 0.0f;
       read_rows(j, j == 0 ? early : 0, n);
-      uint32_t top = 0u, odd = 0u;
+      uint32_t pair = 0u;                                              // largest 15-bit patterns of the lower and the upper halves
 #pragma unroll
       for (int it = 0; it < kItems; ++it) {
         if ((it * kStoreThreads + tid) / kRowChunks >= n) v[it] = make_uint4(0u, 0u, 0u, 0u);
-        const uint32_t words[4] = {v[it].x, v[it].y, v[it].z, v[it].w};
+        pair = __vmaxu2(__vmaxu2(pair, v[it].x & 0x7fff7fffu), __vmaxu2(v[it].y & 0x7fff7fffu, __vmaxu2(v[it].z & 0x7fff7fffu, v[it].w & 0x7fff7fffu)));
+      }
+      uint32_t top = max(pair & 0xffffu, pair >> 16);
+      const bool finite = top < Elem<BF16>::kInfPattern;               // this thread's values
+      if (!finite) {
+        top = 0u;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint32_t lo = words[k] & 0x7fffu, hi = (words[k] >> 16) & 0x7fffu;
-          if (lo < Elem<BF16>::kInfPattern) top = max(top, lo);
-          if (hi < Elem<BF16>::kInfPattern) top = max(top, hi);
-          odd = max(odd, max(lo, hi));
+        for (int it = 0; it < kItems; ++it) {
+          const uint32_t words[4] = {v[it].x, v[it].y, v[it].z, v[it].w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t lo = words[k] & 0x7fffu, hi = (words[k] >> 16) & 0x7fffu;
+            if (lo < Elem<BF16>::kInfPattern) top = max(top, lo);
+            if (hi < Elem<BF16>::kInfPattern) top = max(top, hi);
+          }
         }
       }
-      const bool finite = odd < Elem<BF16>::kInfPattern;               // of this thread's values
       top = __reduce_max_sync(kFull, top);
       if (lane == 0) s_max[turn][warp] = top;
       __syncthreads();
@@ -263,24 +275,33 @@ __global__ void __launch_bounds__(kStoreThreads) store_kernel(const StoreParams 
       const float scale = fmaxf(fmaxf(Elem<BF16>::pattern_f32(top) / 127.0f, kScaleFloor), had);
       const float inverse = 1.0f / scale;
       int8_t* const page_codes = codes + page_head * (P * D);
+      // chunk it * kStoreThreads + tid of the run lies as far behind chunk tid in the page as here
+      int8_t* const to = page_codes + place * D + tid * 8;
+      const int chunks = n * kRowChunks;
+      if (finite) {
+        // |x| <= 127 s up to three roundings: the code is within +-127 without a clamp
 #pragma unroll
-      for (int it = 0; it < kItems; ++it) {
-        const int item = it * kStoreThreads + tid, row = item / kRowChunks;
-        if (row >= n) continue;
-        const uint32_t words[4] = {v[it].x, v[it].y, v[it].z, v[it].w};
-        uint32_t out[2];
+        for (int it = 0; it < kItems; ++it) {
+          if (it * kStoreThreads + tid >= chunks) continue;
+          const uint32_t words[4] = {v[it].x, v[it].y, v[it].z, v[it].w};
+          uint32_t out[2];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const float x0 = Elem<BF16>::lo_f32(words[2 * k]), x1 = Elem<BF16>::hi_f32(words[2 * k]), x2 = Elem<BF16>::lo_f32(words[2 * k + 1]),
-                      x3 = Elem<BF16>::hi_f32(words[2 * k + 1]);
-          if (finite) {
-            // |x| <= 127 s up to three roundings: the code is within +-127 without a clamp
-            out[k] = codes_of(pack2f(__fmul_rn(x0, inverse), __fmul_rn(x1, inverse)), pack2f(__fmul_rn(x2, inverse), __fmul_rn(x3, inverse)));
-          } else {
-            out[k] = code_of(x0, inverse) | code_of(x1, inverse) << 8 | code_of(x2, inverse) << 16 | code_of(x3, inverse) << 24;
+          for (int k = 0; k < 2; ++k) {
+            out[k] = codes_of(pack2f(__fmul_rn(Elem<BF16>::lo_f32(words[2 * k]), inverse), __fmul_rn(Elem<BF16>::hi_f32(words[2 * k]), inverse)),
+                              pack2f(__fmul_rn(Elem<BF16>::lo_f32(words[2 * k + 1]), inverse), __fmul_rn(Elem<BF16>::hi_f32(words[2 * k + 1]), inverse)));
           }
+          *reinterpret_cast<uint2*>(to + it * (kStoreThreads * 8)) = make_uint2(out[0], out[1]);
         }
-        *reinterpret_cast<uint2*>(page_codes + (place + row) * D + (item % kRowChunks) * 8) = make_uint2(out[0], out[1]);
+      } else {
+#pragma unroll
+        for (int it = 0; it < kItems; ++it) {
+          if (it * kStoreThreads + tid >= chunks) continue;
+          const uint32_t words[4] = {v[it].x, v[it].y, v[it].z, v[it].w};
+          uint32_t out[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) out[k] = code_of(Elem<BF16>::lo_f32(words[k]), inverse) | code_of(Elem<BF16>::hi_f32(words[k]), inverse) << 8;
+          *reinterpret_cast<uint2*>(to + it * (kStoreThreads * 8)) = make_uint2(out[0] | out[1] << 16, out[2] | out[3] << 16);
+        }
       }
       if (place > 0 && scale != had) {
         const float ratio = had / scale;
@@ -320,61 +341,64 @@ struct LoadParams {
 
 // The four codes of a word (sign bits inverted) times a scale: 2^23 + byte less 2^23 + 128 is the code, exactly.
 __device__ __forceinline__ void widen4(uint32_t u, float scale, float (&x)[4]) {
-#pragma unroll
-  for (int b = 0; b < 4; ++b) x[b] = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440 + b)) - 8388736.0f) * scale;
+  const uint64_t less = pack2f(-8388736.0f, -8388736.0f), by = pack2f(scale, scale);
+  unpack2f(mul2(add2(pack2u(__byte_perm(u, 0x4b000000u, 0x7440), __byte_perm(u, 0x4b000000u, 0x7441)), less), by), x[0], x[1]);
+  unpack2f(mul2(add2(pack2u(__byte_perm(u, 0x4b000000u, 0x7442), __byte_perm(u, 0x4b000000u, 0x7443)), less), by), x[2], x[3]);
 }
 
-// A thread per 16 codes: one 16-byte load, two 16-byte stores; a thread has up to four, whose loads are on their way together.  Bound by HBM.
+// A thread per 8 codes: an 8-byte load and a 16-byte store, so that a warp writes whole sectors (16 codes and two stores 32 bytes apart: a third slower).  A thread has a place in the token, of the keys' chunks or the values', and takes it of
+// four tokens at once.  Bound by HBM.
 template <bool BF16, int D>
 __global__ void __launch_bounds__(kLoadThreads) load_kernel(const LoadParams p) {
   launch_dependents();
-  const uint32_t row = static_cast<uint32_t>(p.heads) * (D / 16);          // chunks of a token's keys
+  const int row = p.heads * (D / 8), all = 2 * row;                       // chunks of a token's keys; of its keys and values
+  const int together = max(1, kLoadThreads / all);                         // tokens that the CTA's threads have at once
   const long long t0 = static_cast<long long>(blockIdx.x) * p.block;
-  const uint32_t rows = static_cast<uint32_t>(min(static_cast<long long>(p.block), p.tokens - t0)), items = rows * row * 2u;
+  const int tokens = static_cast<int>(min(static_cast<long long>(p.block), p.tokens - t0));
+  const int mine = static_cast<int>(threadIdx.x) / all;                    // 0 where a token's chunks are more than the threads
   wait_for_prior_grids();
-  for (uint32_t first = threadIdx.x; first < items; first += kLoadItems * kLoadThreads) {
-    uint32_t slot[kLoadItems], head[kLoadItems], chunk[kLoadItems];
-    uint16_t* to[kLoadItems];
-    const int8_t* codes[kLoadItems];
-    const float* scales[kLoadItems];
-    uint4 code[kLoadItems];
-    float scale[kLoadItems];
+  if (mine >= together) return;
+  for (int chunk = static_cast<int>(threadIdx.x) - mine * all; chunk < all; chunk += kLoadThreads) {
+    const bool values = chunk >= row;
+    const int of_row = values ? chunk - row : chunk, head = of_row / (D / 8);
+    const int8_t* const codes = (values ? p.v_codes : p.k_codes) + (of_row % (D / 8)) * 8;
+    const float* const scales = (values ? p.v_scale : p.k_scale) + head;
+    const long long stride = values ? p.v_stride : p.k_stride;
+    uint16_t* const to = (values ? p.v : p.k) + t0 * stride + of_row * 8;
+    for (int first = mine; first < tokens; first += kLoadItems * together) {
+      uint32_t slot[kLoadItems];
+      uint2 code[kLoadItems];
+      float scale[kLoadItems];
 #pragma unroll
-    for (int n = 0; n < kLoadItems; ++n) {
-      const uint32_t item = min(first + n * kLoadThreads, items - 1u);
-      const bool values = item >= rows * row;
-      const uint32_t in = values ? item - rows * row : item, r = in / row, of_row = in - r * row;
-      head[n] = of_row / (D / 16);
-      chunk[n] = of_row % (D / 16);
-      slot[n] = static_cast<uint32_t>(p.slots[t0 + r]);
-      to[n] = (values ? p.v : p.k) + (t0 + r) * (values ? p.v_stride : p.k_stride) + head[n] * D + chunk[n] * 16;
-      codes[n] = values ? p.v_codes : p.k_codes;
-      scales[n] = values ? p.v_scale : p.k_scale;
-    }
-#pragma unroll
-    for (int n = 0; n < kLoadItems; ++n) {
-      code[n] = make_uint4(0u, 0u, 0u, 0u);
-      scale[n] = 0.0f;
-      if (slot[n] < p.n_slots) {
-        const long long page_head = static_cast<long long>(slot[n] >> p.page_shift) * p.heads + head[n];
-        code[n] = __ldcs(reinterpret_cast<const uint4*>(codes[n] + ((page_head << p.page_shift) + (slot[n] & ((1u << p.page_shift) - 1u))) * D) + chunk[n]);
-        scale[n] = scales[n][page_head];
+      for (int n = 0; n < kLoadItems; ++n) {
+        const int t = first + n * together;
+        slot[n] = t < tokens ? static_cast<uint32_t>(p.slots[t0 + t]) : 0xffffffffu;
       }
-    }
 #pragma unroll
-    for (int n = 0; n < kLoadItems; ++n) {
-      if (first + n * kLoadThreads >= items) break;
-      const uint32_t w[4] = {code[n].x ^ 0x80808080u, code[n].y ^ 0x80808080u, code[n].z ^ 0x80808080u, code[n].w ^ 0x80808080u};
-      uint32_t out[8];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        float x[4];
-        widen4(w[k], scale[n], x);
-        out[2 * k] = Elem<BF16>::pack_rn(x[0], x[1]);
-        out[2 * k + 1] = Elem<BF16>::pack_rn(x[2], x[3]);
+      for (int n = 0; n < kLoadItems; ++n) {
+        code[n] = make_uint2(0u, 0u);
+        scale[n] = 0.0f;
+        if (slot[n] < p.n_slots) {
+          const long long page = static_cast<long long>(slot[n] >> p.page_shift) * p.heads;
+          code[n] = __ldcs(reinterpret_cast<const uint2*>(codes + (((page + head) << p.page_shift) + (slot[n] & ((1u << p.page_shift) - 1u))) * D));
+          scale[n] = scales[page];
+        }
       }
-      __stcs(reinterpret_cast<uint4*>(to[n]), make_uint4(out[0], out[1], out[2], out[3]));
-      __stcs(reinterpret_cast<uint4*>(to[n]) + 1, make_uint4(out[4], out[5], out[6], out[7]));
+#pragma unroll
+      for (int n = 0; n < kLoadItems; ++n) {
+        const int t = first + n * together;
+        if (t >= tokens) break;
+        const uint32_t w[2] = {code[n].x ^ 0x80808080u, code[n].y ^ 0x80808080u};
+        uint32_t out[4];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float x[4];
+          widen4(w[k], scale[n], x);
+          out[2 * k] = Elem<BF16>::pack_rn(x[0], x[1]);
+          out[2 * k + 1] = Elem<BF16>::pack_rn(x[2], x[3]);
+        }
+        __stcs(reinterpret_cast<uint4*>(to + t * stride), make_uint4(out[0], out[1], out[2], out[3]));
+      }
     }
   }
 }
@@ -434,10 +458,10 @@ tsq_status_t launched(cudaError_t e) {
 template <bool BF16, int D>
 cudaError_t launch_store(const StoreParams& p, int shift, int grid, cudaStream_t stream) {
   switch (shift) {
-    case 4: return launch_overlapped(store_kernel<BF16, D, 16>, grid, kStoreThreads, 0, stream, p);
-    case 5: return launch_overlapped(store_kernel<BF16, D, 32>, grid, kStoreThreads, 0, stream, p);
-    case 6: return launch_overlapped(store_kernel<BF16, D, 64>, grid, kStoreThreads, 0, stream, p);
-    default: return launch_overlapped(store_kernel<BF16, D, 128>, grid, kStoreThreads, 0, stream, p);
+    case 4: return launch_overlapped(store_kernel<BF16, D, 16>, grid, store_threads(D, 16), 0, stream, p);
+    case 5: return launch_overlapped(store_kernel<BF16, D, 32>, grid, store_threads(D, 32), 0, stream, p);
+    case 6: return launch_overlapped(store_kernel<BF16, D, 64>, grid, store_threads(D, 64), 0, stream, p);
+    default: return launch_overlapped(store_kernel<BF16, D, 128>, grid, store_threads(D, 128), 0, stream, p);
   }
 }
 
@@ -552,11 +576,11 @@ tsq_status_t tsq_cache_load(const tsq_cache_t* cache, const int32_t* slots, int6
   p.heads = cache->kv_heads;
   p.page_shift = page_shift(cache->page_tokens);
   p.n_slots = static_cast<uint32_t>(cache->pages * cache->page_tokens);
-  const int row = 2 * cache->kv_heads * (cache->head_dim / 16);
-  // as many tokens as give each thread four chunks, fewer where that would leave SMs without work
+  const int row = 2 * cache->kv_heads * (cache->head_dim / 8);
+  // four tokens for each thread, fewer where that would leave SMs without work
   const int sms = current_sms();
   if (sms < 1) return launched(cudaErrorInvalidDevice);
-  p.block = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kLoadItems * kLoadThreads / row, tokens / (2 * sms))));
+  p.block = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kLoadItems * std::max(1, kLoadThreads / row), tokens / (2 * sms))));
   const int grid = static_cast<int>((tokens + p.block - 1) / p.block);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const bool bf16 = cache->dtype == TSQ_BF16;
