@@ -75,6 +75,62 @@ __device__ __forceinline__ float4 shared_float4(uint32_t at) {
   return v;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// Largest score of 32 keys (two granules, whose scales lie at `scales`) in the form that the weights' exponent has; with `mask` only the first `left` count.
+__device__ __forceinline__ float top_score(uint32_t (&s)[32], uint32_t scales, float by_scale, bool mask, int left) {
+  if (mask) {
+#pragma unroll
+    for (int e = 0; e < 32; ++e) s[e] = e < left ? s[e] : 0xff800000u;
+  }
+  float most = -INFINITY;
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    const uint32_t* const x = s + 16 * g;
+    float t0 = max3(__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2])), t1 = max3(__uint_as_float(x[3]), __uint_as_float(x[4]), __uint_as_float(x[5]));
+    t0 = max3(t0, __uint_as_float(x[6]), __uint_as_float(x[7]));
+    t1 = max3(t1, __uint_as_float(x[8]), __uint_as_float(x[9]));
+    t0 = max3(t0, __uint_as_float(x[10]), __uint_as_float(x[11]));
+    t1 = max3(t1, __uint_as_float(x[12]), __uint_as_float(x[13]));
+    t0 = max3(t0, __uint_as_float(x[14]), __uint_as_float(x[15]));
+    const float raw = fmaxf(t0, t1);
+    const float4 f = shared_float4(scales + 16 * g);       // score factor, log2 and inverse of the values' scale
+    const float v = __fmaf_rn(raw, f.x * by_scale, f.y);
+    most = fmaxf(most, raw == -INFINITY ? raw : v);
+  }
+  return most;
+}
+// Their weights in binary16, two to a word; returns the sum l and theirs over the values' scale.
+__device__ __forceinline__ float weights_of(const uint32_t (&s)[32], uint32_t (&w)[16], uint32_t scales, float by_scale, float m, float l, bool mask, int left) {
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    const float4 f = shared_float4(scales + 16 * g);
+    const float a = f.x * by_scale, b = f.y - m;
+    const uint64_t a2 = pack2f(a, a), b2 = pack2f(b, b);
+    uint64_t sum = 0ull;                                   // of even and of odd keys
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) {
+      float x0, x1;
+      unpack2f(fma2(pack2u(s[16 * g + e], s[16 * g + e + 1]), a2, b2), x0, x1);
+      if (mask) {
+        x0 = 16 * g + e < left ? x0 : -INFINITY;
+        x1 = 16 * g + e + 1 < left ? x1 : -INFINITY;
+      }
+      x0 = exp2_fast(x0);
+      x1 = exp2_fast(x1);
+      sum = add2(sum, pack2f(x0, x1));
+      w[8 * g + e / 2] = pack_half2(x0, x1);
+    }
+    float even, odd;
+    unpack2f(sum, even, odd);
+    l = __fmaf_rn(even + odd, f.z, l);
+  }
+  return l;
+}
+
 // Shared-memory descriptors of 128-byte swizzled operands: rows of 128 bytes, eight rows to a 1024-byte atom.
 // K-major (queries, keys): atoms follow one another down the rows.  MN-major (values: a row is a token, its 64 dimensions contiguous): atoms follow
 // one another along the tokens, the second 64 dimensions lie kHalf bytes behind.
@@ -338,28 +394,21 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
           if (!wait(kSFull + t, count & 1u)) break;
           tm_fence_after();
           const uint32_t scales = smem + Sh::kScales + static_cast<uint32_t>((place.unit + (j - place.k0) - share) % kMeta) * (kGranules * 16);
-          const bool mask = (j + 1) * kKeys > seen_first;
+          const int left = (j + 1) * kKeys > seen_first ? seen - j * kKeys : kKeys;  // keys of the step that the row sees
+          const bool mask = __any_sync(kFull, left < kKeys);
           // the largest score: raw sums within a granule, which has one factor that is not negative
           float most = -INFINITY;
-#pragma unroll
-          for (int chunk = 0; chunk < kKeys / 32; ++chunk) {
-            uint32_t s[32];
-            tm_load32(s, s_at + 32 * chunk);
-            tm_wait_ld();
-#pragma unroll
-            for (int g = 0; g < 2; ++g) {
-              if (mask) {
-                const int left = seen - (j * kKeys + 32 * chunk + 16 * g);  // keys of the granule that the row sees
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[16 * g + e] = e < left ? s[16 * g + e] : 0xff800000u;
-              }
-              float raw = __uint_as_float(s[16 * g]);
-#pragma unroll
-              for (int e = 1; e < 15; e += 2) raw = fmaxf(raw, fmaxf(__uint_as_float(s[16 * g + e]), __uint_as_float(s[16 * g + e + 1])));
-              raw = fmaxf(raw, __uint_as_float(s[16 * g + 15]));
-              const float4 f = shared_float4(scales + 16 * (2 * chunk + g));  // score factor, log2 and inverse of the values' scale
-              const float x = __fmaf_rn(raw, f.x * by_scale, f.y);
-              most = fmaxf(most, raw == -INFINITY ? raw : x);
+          {
+            uint32_t a[32], b[32];
+            tm_load32(a, s_at);
+#pragma unroll 1
+            for (int chunk = 0; chunk < kKeys / 32; chunk += 2) {
+              tm_wait_ld();
+              tm_load32(b, s_at + 32 * (chunk + 1));
+              most = fmaxf(most, top_score(a, scales + 32 * chunk, by_scale, mask, left - 32 * chunk));
+              tm_wait_ld();
+              if (chunk + 2 < kKeys / 32) tm_load32(a, s_at + 32 * (chunk + 2));
+              most = fmaxf(most, top_score(b, scales + 32 * (chunk + 1), by_scale, mask, left - 32 * (chunk + 1)));
             }
           }
           const bool up = have ? most > m + 8.0f : most > -INFINITY;
@@ -387,32 +436,20 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
             }
           }
           // weights: those of 32 scores take the place of 16
-#pragma unroll
-          for (int chunk = 0; chunk < kKeys / 32; ++chunk) {
-            uint32_t s[32], w[16];
-            tm_load32(s, s_at + 32 * chunk);
-            tm_wait_ld();
-#pragma unroll
-            for (int g = 0; g < 2; ++g) {
-              const int left = mask ? seen - (j * kKeys + 32 * chunk + 16 * g) : 16;
-              const float4 f = shared_float4(scales + 16 * (2 * chunk + g));
-              const float a = f.x * by_scale, b = f.y - m;
-              float part = 0.0f;
-#pragma unroll
-              for (int e = 0; e < 16; e += 2) {
-                float x0 = __fmaf_rn(__uint_as_float(s[16 * g + e]), a, b), x1 = __fmaf_rn(__uint_as_float(s[16 * g + e + 1]), a, b);
-                if (mask) {
-                  x0 = e < left ? x0 : -INFINITY;
-                  x1 = e + 1 < left ? x1 : -INFINITY;
-                }
-                x0 = exp2_fast(x0);
-                x1 = exp2_fast(x1);
-                part += x0 + x1;
-                w[8 * g + e / 2] = pack_half2(x0, x1);
-              }
-              l = __fmaf_rn(part, f.z, l);
+          {
+            uint32_t a[32], b[32], w[16];
+            tm_load32(a, s_at);
+#pragma unroll 1
+            for (int chunk = 0; chunk < kKeys / 32; chunk += 2) {
+              tm_wait_ld();
+              tm_load32(b, s_at + 32 * (chunk + 1));
+              l = weights_of(a, w, scales + 32 * chunk, by_scale, m, l, mask, left - 32 * chunk);
+              tm_wait_ld();                                // b is read before its first columns are written over
+              tm_store16(s_at + 16 * chunk, w);
+              if (chunk + 2 < kKeys / 32) tm_load32(a, s_at + 32 * (chunk + 2));
+              l = weights_of(b, w, scales + 32 * (chunk + 1), by_scale, m, l, mask, left - 32 * (chunk + 1));
+              tm_store16(s_at + 16 * (chunk + 1), w);
             }
-            tm_store16(s_at + 16 * chunk, w);
           }
           tm_wait_st();
           tm_fence_before();
@@ -515,28 +552,33 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
     uint32_t n = 0;                                        // steps so far
     uint4 k[kItems], v[kItems];
     float4 scale = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    auto page_at = [&](const Place& at, int j, int granule) {
+    // pages of the next step's granules; -1 where there is none
+    int pages[kItems], scale_page = -1;
+    auto page_at = [&](int j, int granule) {
       const int token = j * kKeys + 16 * granule;
-      if (token >= at.r.keys) return -1;
-      const int id = p.table[static_cast<long long>(at.request) * p.table_pages + (token >> p.page_shift)];
-      return static_cast<unsigned>(id) < static_cast<unsigned>(p.pages) ? id : -1;
+      if (token >= place.r.keys) return -1;
+      return p.table[static_cast<long long>(place.request) * p.table_pages + (token >> p.page_shift)];
     };
-    auto fetch = [&](const Place& at, int j, const int8_t* codes, uint4 (&into)[kItems]) {
+    auto fetch_pages = [&](int j) {
+#pragma unroll
+      for (int it = 0; it < kItems; ++it) pages[it] = page_at(j, (token0 + it * (128 / kChunks)) / 16);
+      if (in_group < kGranules) scale_page = page_at(j, in_group);
+    };
+    auto fetch = [&](int j, const int8_t* codes, uint4 (&into)[kItems]) {
 #pragma unroll
       for (int it = 0; it < kItems; ++it) {
-        const int token = token0 + it * (128 / kChunks), id = page_at(at, j, token / 16);
+        const int token = j * kKeys + token0 + it * (128 / kChunks);
         into[it] = make_uint4(0u, 0u, 0u, 0u);
-        if (id >= 0)
-          into[it] = *(reinterpret_cast<const uint4*>(codes + (((static_cast<long long>(id) * p.kv_heads + at.head) << p.page_shift) +
-                                                               ((j * kKeys + token) & ((1 << p.page_shift) - 1))) * D) + chunk);
+        if (static_cast<unsigned>(pages[it]) < static_cast<unsigned>(p.pages))
+          into[it] = *(reinterpret_cast<const uint4*>(codes + (((static_cast<long long>(pages[it]) * p.kv_heads + place.head) << p.page_shift) +
+                                                               (token & ((1 << p.page_shift) - 1))) * D) + chunk);
       }
     };
-    auto fetch_scale = [&](const Place& at, int j) {
+    auto fetch_scale = [&]() {
       if (in_group >= kGranules) return;
-      const int id = page_at(at, j, in_group);
       scale = make_float4(0.0f, -INFINITY, 0.0f, 0.0f);    // nothing of a page that is not there is seen
-      if (id >= 0) {
-        const long long page_head = static_cast<long long>(id) * p.kv_heads + at.head;
+      if (static_cast<unsigned>(scale_page) < static_cast<unsigned>(p.pages)) {
+        const long long page_head = static_cast<long long>(scale_page) * p.kv_heads + place.head;
         const float vs = fmaxf(p.v_scale[page_head], kLeastScale);
         scale = make_float4(p.k_scale[page_head], __log2f(vs), 1.0f / vs, 0.0f);
       }
@@ -554,28 +596,30 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
     };
     int j = place.k0;
     bool more = true;
-    fetch_scale(place, j);
-    fetch(place, j, p.k_codes, k);
-    fetch(place, j, p.v_codes, v);
+    fetch_pages(j);
+    fetch_scale();
+    fetch(j, p.k_codes, k);
+    fetch(j, p.v_codes, v);
     while (more) {
+      if (++j >= place.k1) {                               // the step behind this one
+        more = place.next(p);
+        j = place.k0;
+      }
+      if (more) fetch_pages(j);
       if (!wait(kKFree + (n & 1u), ((n >> 1) & 1u) ^ 1u)) break;
       if (in_group < kGranules) reinterpret_cast<float4*>(smem_at + Sh::kScales)[(n % kMeta) * kGranules + in_group] = scale;
       widen(k, smem_at + Sh::kK + (n & 1u) * Sh::kOperand);
       fence_proxy_async_smem();
       bar_arrive(bars + 8 * (kKFull + (n & 1u)));
-      if (++j >= place.k1) {                               // the step behind this one
-        more = place.next(p);
-        j = place.k0;
-      }
       if (more) {
-        fetch_scale(place, j);
-        fetch(place, j, p.k_codes, k);
+        fetch(j, p.k_codes, k);
+        fetch_scale();
       }
       if (!wait(kVFree + (n & 1u), ((n >> 1) & 1u) ^ 1u)) break;
       widen(v, smem_at + Sh::kV + (n & 1u) * Sh::kOperand);
       fence_proxy_async_smem();
       bar_arrive(bars + 8 * (kVFull + (n & 1u)));
-      if (more) fetch(place, j, p.v_codes, v);
+      if (more) fetch(j, p.v_codes, v);
       ++n;
     }
   } else {
