@@ -80,9 +80,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-// Largest score of 32 keys (two granules, whose scales lie at `scales`) in the form that the weights' exponent has; with `mask` only the first `left` count.
-__device__ __forceinline__ float top_score(uint32_t (&s)[32], uint32_t scales, float by_scale, bool mask, int left) {
-  if (mask) {
+// Largest score of 32 keys (two granules, whose scales lie at `scales`; a granule has one factor that is not negative) in the form that the weights' exponent has; with MASK only the first `left` count.
+template <bool MASK>
+__device__ __forceinline__ float top_score(uint32_t (&s)[32], uint32_t scales, float by_scale, int left) {
+  if constexpr (MASK) {
 #pragma unroll
     for (int e = 0; e < 32; ++e) s[e] = e < left ? s[e] : 0xff800000u;
   }
@@ -104,7 +105,8 @@ __device__ __forceinline__ float top_score(uint32_t (&s)[32], uint32_t scales, f
   return most;
 }
 // Their weights in binary16, two to a word; returns the sum l and theirs over the values' scale.
-__device__ __forceinline__ float weights_of(const uint32_t (&s)[32], uint32_t (&w)[16], uint32_t scales, float by_scale, float m, float l, bool mask, int left) {
+template <bool MASK>
+__device__ __forceinline__ float weights_of(const uint32_t (&s)[32], uint32_t (&w)[16], uint32_t scales, float by_scale, float m, float l, int left) {
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
     const float4 f = shared_float4(scales + 16 * g);
@@ -115,7 +117,7 @@ __device__ __forceinline__ float weights_of(const uint32_t (&s)[32], uint32_t (&
     for (int e = 0; e < 16; e += 2) {
       float x0, x1;
       unpack2f(fma2(pack2u(s[16 * g + e], s[16 * g + e + 1]), a2, b2), x0, x1);
-      if (mask) {
+      if constexpr (MASK) {
         x0 = 16 * g + e < left ? x0 : -INFINITY;
         x1 = 16 * g + e + 1 < left ? x1 : -INFINITY;
       }
@@ -127,6 +129,42 @@ __device__ __forceinline__ float weights_of(const uint32_t (&s)[32], uint32_t (&
     float even, odd;
     unpack2f(sum, even, odd);
     l = __fmaf_rn(even + odd, f.z, l);
+  }
+  return l;
+}
+
+// The same over a step's 128 keys, each part read from tensor memory while the one before is worked on.  Weights take the place of scores: those of 32
+// that of 16.
+template <bool MASK>
+__device__ __forceinline__ float step_top(uint32_t s_at, uint32_t scales, float by_scale, int left) {
+  uint32_t a[32], b[32];
+  float most = -INFINITY;
+  tm_load32(a, s_at);
+#pragma unroll 1
+  for (int chunk = 0; chunk < kKeys / 32; chunk += 2) {
+    tm_wait_ld();
+    tm_load32(b, s_at + 32 * (chunk + 1));
+    most = fmaxf(most, top_score<MASK>(a, scales + 32 * chunk, by_scale, left - 32 * chunk));
+    tm_wait_ld();
+    if (chunk + 2 < kKeys / 32) tm_load32(a, s_at + 32 * (chunk + 2));
+    most = fmaxf(most, top_score<MASK>(b, scales + 32 * (chunk + 1), by_scale, left - 32 * (chunk + 1)));
+  }
+  return most;
+}
+template <bool MASK>
+__device__ __forceinline__ float step_weights(uint32_t s_at, uint32_t scales, float by_scale, float m, float l, int left) {
+  uint32_t a[32], b[32], w[16];
+  tm_load32(a, s_at);
+#pragma unroll 1
+  for (int chunk = 0; chunk < kKeys / 32; chunk += 2) {
+    tm_wait_ld();
+    tm_load32(b, s_at + 32 * (chunk + 1));
+    l = weights_of<MASK>(a, w, scales + 32 * chunk, by_scale, m, l, left - 32 * chunk);
+    tm_wait_ld();                                          // b is read before its first columns are written over
+    tm_store16(s_at + 16 * chunk, w);
+    if (chunk + 2 < kKeys / 32) tm_load32(a, s_at + 32 * (chunk + 2));
+    l = weights_of<MASK>(b, w, scales + 32 * (chunk + 1), by_scale, m, l, left - 32 * (chunk + 1));
+    tm_store16(s_at + 16 * (chunk + 1), w);
   }
   return l;
 }
@@ -396,21 +434,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
           const uint32_t scales = smem + Sh::kScales + static_cast<uint32_t>((place.unit + (j - place.k0) - share) % kMeta) * (kGranules * 16);
           const int left = (j + 1) * kKeys > seen_first ? seen - j * kKeys : kKeys;  // keys of the step that the row sees
           const bool mask = __any_sync(kFull, left < kKeys);
-          // the largest score: raw sums within a granule, which has one factor that is not negative
-          float most = -INFINITY;
-          {
-            uint32_t a[32], b[32];
-            tm_load32(a, s_at);
-#pragma unroll 1
-            for (int chunk = 0; chunk < kKeys / 32; chunk += 2) {
-              tm_wait_ld();
-              tm_load32(b, s_at + 32 * (chunk + 1));
-              most = fmaxf(most, top_score(a, scales + 32 * chunk, by_scale, mask, left - 32 * chunk));
-              tm_wait_ld();
-              if (chunk + 2 < kKeys / 32) tm_load32(a, s_at + 32 * (chunk + 2));
-              most = fmaxf(most, top_score(b, scales + 32 * (chunk + 1), by_scale, mask, left - 32 * (chunk + 1)));
-            }
-          }
+          const float most = mask ? step_top<true>(s_at, scales, by_scale, left) : step_top<false>(s_at, scales, by_scale, left);
           const bool up = have ? most > m + 8.0f : most > -INFINITY;
           if (__any_sync(kFull, up)) {
             float by = 1.0f;
@@ -435,22 +459,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
               tm_wait_st();
             }
           }
-          // weights: those of 32 scores take the place of 16
-          {
-            uint32_t a[32], b[32], w[16];
-            tm_load32(a, s_at);
-#pragma unroll 1
-            for (int chunk = 0; chunk < kKeys / 32; chunk += 2) {
-              tm_wait_ld();
-              tm_load32(b, s_at + 32 * (chunk + 1));
-              l = weights_of(a, w, scales + 32 * chunk, by_scale, m, l, mask, left - 32 * chunk);
-              tm_wait_ld();                                // b is read before its first columns are written over
-              tm_store16(s_at + 16 * chunk, w);
-              if (chunk + 2 < kKeys / 32) tm_load32(a, s_at + 32 * (chunk + 2));
-              l = weights_of(b, w, scales + 32 * (chunk + 1), by_scale, m, l, mask, left - 32 * (chunk + 1));
-              tm_store16(s_at + 16 * (chunk + 1), w);
-            }
-          }
+          l = mask ? step_weights<true>(s_at, scales, by_scale, m, l, left) : step_weights<false>(s_at, scales, by_scale, m, l, left);
           tm_wait_st();
           tm_fence_before();
           bar_arrive(bars + 8 * (kPReady + t));
