@@ -58,14 +58,9 @@ __device__ __forceinline__ void tm_load32(uint32_t (&v)[32], uint32_t at) {
       : TSQ_R8(v, 0), TSQ_R8(v, 8), TSQ_R8(v, 16), TSQ_R8(v, 24)
       : "r"(at));
 }
-__device__ __forceinline__ void tm_store32(uint32_t at, const uint32_t* v) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
-      "%32};" ::"r"(at),
-      TSQ_W8(v, 0), TSQ_W8(v, 8), TSQ_W8(v, 16), TSQ_W8(v, 24)
-      : "memory");
+__device__ __forceinline__ void tm_load16(uint32_t (&v)[16], uint32_t at) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];" : TSQ_R8(v, 0), TSQ_R8(v, 8) : "r"(at));
 }
-
 __device__ __forceinline__ void tm_store16(uint32_t at, const uint32_t (&v)[16]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at), TSQ_W8(v, 0), TSQ_W8(v, 8) : "memory");
 }
@@ -82,7 +77,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 // Largest score of 32 keys (two granules, whose scales lie at `scales`; a granule has one factor that is not negative) in the form that the weights' exponent has; with MASK only the first `left` count.
 template <bool MASK>
-__device__ __forceinline__ float top_score(uint32_t (&s)[32], uint32_t scales, float by_scale, int left) {
+__device__ __forceinline__ float top_score(const uint32_t (&scores)[32], uint32_t scales, float by_scale, int left) {
+  uint32_t s[32];
+#pragma unroll
+  for (int e = 0; e < 32; ++e) s[e] = scores[e];
   if constexpr (MASK) {
 #pragma unroll
     for (int e = 0; e < 32; ++e) s[e] = e < left ? s[e] : 0xff800000u;
@@ -129,42 +127,6 @@ __device__ __forceinline__ float weights_of(const uint32_t (&s)[32], uint32_t (&
     float even, odd;
     unpack2f(sum, even, odd);
     l = __fmaf_rn(even + odd, f.z, l);
-  }
-  return l;
-}
-
-// The same over a step's 128 keys, each part read from tensor memory while the one before is worked on.  Weights take the place of scores: those of 32
-// that of 16.
-template <bool MASK>
-__device__ __forceinline__ float step_top(uint32_t s_at, uint32_t scales, float by_scale, int left) {
-  uint32_t a[32], b[32];
-  float most = -INFINITY;
-  tm_load32(a, s_at);
-#pragma unroll 1
-  for (int chunk = 0; chunk < kKeys / 32; chunk += 2) {
-    tm_wait_ld();
-    tm_load32(b, s_at + 32 * (chunk + 1));
-    most = fmaxf(most, top_score<MASK>(a, scales + 32 * chunk, by_scale, left - 32 * chunk));
-    tm_wait_ld();
-    if (chunk + 2 < kKeys / 32) tm_load32(a, s_at + 32 * (chunk + 2));
-    most = fmaxf(most, top_score<MASK>(b, scales + 32 * (chunk + 1), by_scale, left - 32 * (chunk + 1)));
-  }
-  return most;
-}
-template <bool MASK>
-__device__ __forceinline__ float step_weights(uint32_t s_at, uint32_t scales, float by_scale, float m, float l, int left) {
-  uint32_t a[32], b[32], w[16];
-  tm_load32(a, s_at);
-#pragma unroll 1
-  for (int chunk = 0; chunk < kKeys / 32; chunk += 2) {
-    tm_wait_ld();
-    tm_load32(b, s_at + 32 * (chunk + 1));
-    l = weights_of<MASK>(a, w, scales + 32 * chunk, by_scale, m, l, left - 32 * chunk);
-    tm_wait_ld();                                          // b is read before its first columns are written over
-    tm_store16(s_at + 16 * chunk, w);
-    if (chunk + 2 < kKeys / 32) tm_load32(a, s_at + 32 * (chunk + 2));
-    l = weights_of<MASK>(b, w, scales + 32 * (chunk + 1), by_scale, m, l, left - 32 * (chunk + 1));
-    tm_store16(s_at + 16 * (chunk + 1), w);
   }
   return l;
 }
@@ -248,14 +210,19 @@ struct Shared {
   static constexpr int kBars = kScales + kMeta * kGranules * 16;
   static constexpr int kBytes = kBars + 256;
 };
-enum Bar { kKFull = 0, kKFree = 2, kVFull = 4, kVFree = 6, kSFull = 8, kPReady = 10, kODone = 12, kQFull = 14, kBarCount = 16 };
+// Barriers: buffers of keys and values; a half step's scores, weights and sums, by group and half; a tile's queries, by group.
+enum Bar { kKFull = 0, kKFree = 2, kVFull = 4, kVFree = 6, kSFull = 8, kPReady = 12, kODone = 16, kQFull = 20, kBarCount = 22 };
+__host__ __device__ constexpr uint32_t arrivals_of(int bar) {  // threads, or one for the products of each group
+  return bar < kKFree || (bar >= kVFull && bar < kVFree) || (bar >= kPReady && bar < kODone) || bar >= kQFull ? 128u : bar < kSFull ? 2u : 1u;
+}
 
 // A CTA's two groups of 128 threads have 128 query rows each, a thread a row; a tile is the 256 rows of one (request, key head) that follow one another, the group's query
 // heads of a token side by side, so that widened codes serve both groups and all heads.  Per step of 128 tokens:
 //   widening group  codes from global memory (a step ahead in registers) to binary16 (exact) in shared memory, two buffers each for keys and values
-//   product warp    S = Q K^T into tensor memory for each group, then O += P V with P from tensor memory
+//   product warps   one for each group: S = Q K^T into tensor memory, then O += P V with P from tensor memory
 //   softmax groups  S out of tensor memory, w = 2^(S * scale + log2 s_v - m) to binary16 in S's place, sums in binary32
-// While one group works on its scores the tensor cores have the other's products.  m is a reference that follows the row's maximum only when a
+// Scores come in halves of 64 keys, each with its place in tensor memory: while a group works on one, its products fill the other, and the other group's run besides.
+// m is a reference that follows the row's maximum only when a
 // score is more than 2^8 above it: then the step is done again and O is scaled in tensor memory.  Every CTA takes the same number of steps whatever the requests'
 // lengths are; tiles that several CTAs have a part of are added up through the workspace by the one that comes last, in the order of the steps.
 // Bound by the exponentials and by what surrounds them: 16 of them per SM and clock are 1024 clocks for a group's step, as long as its two products take.
@@ -288,7 +255,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
     s_found = 0;
     s_begin = 0;
     const uint32_t bars = smem + Sh::kBars;
-    for (int i = 0; i < kBarCount; ++i) bar_init(bars + 8 * i, i < kKFree || (i >= kVFull && i < kVFree) || (i >= kPReady && i < kODone) || i >= kQFull ? 128u : 1u);
+#pragma unroll
+    for (int i = 0; i < kBarCount; ++i) bar_init(bars + 8 * i, arrivals_of(i));
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_proxy_async_smem();
   }
@@ -389,82 +357,115 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
     const uint32_t lanes = static_cast<uint32_t>(warp % 4) << 21;  // lane 32 * (warp % 4) in the upper half of an address
     const uint32_t s_at = tmem + lanes + 128 * t, o_at = tmem + lanes + 256 + D * t;
     uint32_t count = 0;                                    // steps of this group so far
-    do {
+    // the thread's row of a tile, brought to binary16 by a power of two; the inverse is returned
+    auto load_query = [&](const Place& at) {
+      const long long row0 = static_cast<long long>(at.tile) * kTilesRows + 128 * t;
+      float factor = 1.0f;
+      if (row0 >= at.rows || at.limit(t, p) <= at.k0) return factor;
+      const long long in = row0 + row;
+      const bool live = in < at.rows;
+      const int token = static_cast<int>((live ? in : row0) / p.group), query_head = at.head * p.group + static_cast<int>((live ? in : row0) % p.group);
+      const uint16_t* const from = static_cast<const uint16_t*>(p.q) + (at.r.start + token) * p.q_stride + static_cast<long long>(query_head) * D;
+      uint32_t top = 0u;
+      uint4 v[D / 8];
+#pragma unroll
+      for (int k = 0; k < D / 8; ++k) v[k] = live ? reinterpret_cast<const uint4*>(from)[k] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+      for (int k = 0; k < D / 8; ++k)
+        top = __vmaxu2(__vmaxu2(top, v[k].x & 0x7fff7fffu), __vmaxu2(v[k].y & 0x7fff7fffu, __vmaxu2(v[k].z & 0x7fff7fffu, v[k].w & 0x7fff7fffu)));
+      const float power = row_power(Elem<BF16>::pattern_f32(max(top & 0xffffu, top >> 16)), factor);
+      const float sign = p.scale_log2 < 0.0f ? -power : power;  // the scores' factors are not negative
+      unsigned char* const q_at = smem_at + Sh::kQ + t * Sh::kOperand + row * 128;
+#pragma unroll
+      for (int k = 0; k < D / 8; ++k) {
+        const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+        uint32_t h[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = pack_half2(Elem<BF16>::lo_f32(w[e]) * sign, Elem<BF16>::hi_f32(w[e]) * sign);
+        *reinterpret_cast<uint4*>(q_at + (k / 8) * kHalf + (((k % 8) ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+      }
+      fence_proxy_async_smem();
+      bar_arrive(bars + 8 * (kQFull + t));
+      return factor;
+    };
+    float factor = load_query(place);
+    Place next = place;
+    bool more = true;
+    for (; more && ok; place = next) {
       const int limit = place.limit(t, p);
       const long long row0 = static_cast<long long>(place.tile) * kTilesRows + 128 * t;
-      if (row0 >= place.rows) continue;
-      const int rows = static_cast<int>(min(128ll, place.rows - row0));
+      const bool mine = row0 < place.rows, any = mine && limit > place.k0;  // the group has rows of the tile; the CTA has steps that they see
+      const int rows = mine ? static_cast<int>(min(128ll, place.rows - row0)) : 1;
       const bool live = row < rows;
       const long long at = row0 + min(row, rows - 1);
       const int token = static_cast<int>(at / p.group), query_head = place.head * p.group + static_cast<int>(at % p.group);
-      const bool any = limit > place.k0;                   // the CTA has steps that this half of the tile sees
       float m = 0.0f, l = 0.0f;
       bool have = false;
       if (any) {
-        // the row, brought to binary16 by a power of two
-        const uint16_t* const from = static_cast<const uint16_t*>(p.q) + (place.r.start + token) * p.q_stride + static_cast<long long>(query_head) * D;
-        uint32_t top = 0u;
-        uint4 v[D / 8];
-#pragma unroll
-        for (int k = 0; k < D / 8; ++k) {
-          v[k] = live ? reinterpret_cast<const uint4*>(from)[k] : make_uint4(0u, 0u, 0u, 0u);
-          const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) top = max(top, max(w[e] & 0x7fffu, (w[e] >> 16) & 0x7fffu));
-        }
-        float factor;
-        const float power = row_power(Elem<BF16>::pattern_f32(top), factor);
-        const float sign = p.scale_log2 < 0.0f ? -power : power;  // the scores' factors below are not negative
-        unsigned char* const q_at = smem_at + Sh::kQ + t * Sh::kOperand;
-#pragma unroll
-        for (int k = 0; k < D / 8; ++k) {
-          const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-          uint32_t h[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) h[e] = pack_half2(Elem<BF16>::lo_f32(w[e]) * sign, Elem<BF16>::hi_f32(w[e]) * sign);
-          *reinterpret_cast<uint4*>(q_at + (k / 8) * kHalf + row * 128 + (((k % 8) ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
-        }
-        fence_proxy_async_smem();
-        bar_arrive(bars + 8 * (kQFull + t));
         const float by_scale = factor * fabsf(p.scale_log2);
         const int seen = place.r.seen(token), seen_first = place.r.seen(static_cast<int>(row0 / p.group));
-        for (int j = place.k0; j < limit; ++j, ++count) {
-          if (!wait(kSFull + t, count & 1u)) break;
-          tm_fence_after();
-          const uint32_t scales = smem + Sh::kScales + static_cast<uint32_t>((place.unit + (j - place.k0) - share) % kMeta) * (kGranules * 16);
-          const int left = (j + 1) * kKeys > seen_first ? seen - j * kKeys : kKeys;  // keys of the step that the row sees
-          const bool mask = __any_sync(kFull, left < kKeys);
-          const float most = mask ? step_top<true>(s_at, scales, by_scale, left) : step_top<false>(s_at, scales, by_scale, left);
-          const bool up = have ? most > m + 8.0f : most > -INFINITY;
-          if (__any_sync(kFull, up)) {
-            float by = 1.0f;
-            if (up) {
-              by = have ? exp2_fast(m - most) : 0.0f;
-              m = most;
-              have = true;
-            }
-            l *= by;
-            if (j > place.k0) {                            // the sums so far follow the reference
-              if (!wait(kODone + t, (count - 1u) & 1u)) break;
-              tm_fence_after();
+        uint32_t scales = static_cast<uint32_t>(place.unit - share) % kMeta;
+        for (int j = place.k0; j < limit; ++j, ++count, scales = (scales + 1) % kMeta) {
+          const bool mask = (j + 1) * kKeys > seen_first;  // as far as the group's first row sees
 #pragma unroll 1
-              for (int d = 0; d < D; d += 32) {
-                uint32_t o[32];
-                tm_load32(o, o_at + d);
-                tm_wait_ld();
-#pragma unroll
-                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
-                tm_store32(o_at + d, o);
+          for (int h = 0; h < 2; ++h) {
+            if (!wait(kSFull + 2 * t + h, count & 1u)) break;
+            tm_fence_after();
+            const uint32_t at_half = s_at + 64 * h, factors = smem + Sh::kScales + (scales * kGranules + 4 * h) * 16;
+            const int left = seen - j * kKeys - 64 * h;    // keys of the half that the row sees
+            uint32_t a[32], b[32], w[16];
+            tm_load32(a, at_half);
+            tm_load32(b, at_half + 32);
+            tm_wait_ld();
+            const float most = mask ? fmaxf(top_score<true>(a, factors, by_scale, left), top_score<true>(b, factors + 32, by_scale, left - 32))
+                                    : fmaxf(top_score<false>(a, factors, by_scale, 64), top_score<false>(b, factors + 32, by_scale, 64));
+            const bool up = have ? most > m + 8.0f : most > -INFINITY;
+            if (__any_sync(kFull, up)) {
+              float by = 1.0f;
+              if (up) {
+                by = have ? exp2_fast(m - most) : 0.0f;
+                m = most;
+                have = true;
               }
-              tm_wait_st();
+              l *= by;
+              if (j > place.k0 || h > 0) {                 // the sums so far follow the reference
+                if (!wait(kODone + 2 * t + (h ^ 1), (h > 0 ? count : count - 1u) & 1u)) break;
+                tm_fence_after();
+#pragma unroll 1
+                for (int d = 0; d < D; d += 16) {
+                  uint32_t o[16];
+                  tm_load16(o, o_at + d);
+                  tm_wait_ld();
+#pragma unroll
+                  for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
+                  tm_store16(o_at + d, o);
+                }
+              }
             }
+            // weights take the place of scores, which have all been read: those of 32 that of 16
+            if (mask) {
+              l = weights_of<true>(a, w, factors, by_scale, m, l, left);
+              tm_store16(at_half, w);
+              l = weights_of<true>(b, w, factors + 32, by_scale, m, l, left - 32);
+            } else {
+              l = weights_of<false>(a, w, factors, by_scale, m, l, 64);
+              tm_store16(at_half, w);
+              l = weights_of<false>(b, w, factors + 32, by_scale, m, l, 64);
+            }
+            tm_store16(at_half + 16, w);
+            tm_wait_st();
+            tm_fence_before();
+            bar_arrive(bars + 8 * (kPReady + 2 * t + h));
           }
-          l = mask ? step_weights<true>(s_at, scales, by_scale, m, l, left) : step_weights<false>(s_at, scales, by_scale, m, l, left);
-          tm_wait_st();
-          tm_fence_before();
-          bar_arrive(bars + 8 * (kPReady + t));
+          if (!ok) break;
         }
-        if (!wait(kODone + t, (count - 1u) & 1u)) break;
+      }
+      // the next tile's queries, while the last products are on their way: those with the scores have all ended
+      more = next.next(p);
+      if (more && ok) factor = load_query(next);
+      if (!mine || !ok) continue;
+      if (any) {
+        if (!wait(kODone + 2 * t + 1, (count - 1u) & 1u)) break;
         tm_fence_after();
       }
       // ---- the row, or its part ----
@@ -548,7 +549,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
           }
         }
       }
-    } while (ok && place.next(p));
+    }
   } else if (warp < 12) {
     // ---- codes to binary16 ----
     regs_down<kWidenRegs>();
@@ -634,63 +635,81 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
   } else {
     regs_down<kProductRegs>();
   }
-  if (warp == 12) {
-    // ---- products ----
-    constexpr uint32_t kScores = product_of(kKeys, false), kSums = product_of(D, true);
-    uint32_t n = 0, count[2] = {0u, 0u}, tiles[2] = {0u, 0u};
-    do {
-      const int limit[2] = {place.limit(0, p), place.limit(1, p)};
-      for (int j = place.k0; j <= place.k1 && ok; ++j) {
-        const uint32_t buffer = n & 1u, before = (n - 1u) & 1u;
+  if (warp == 12 || warp == 13) {
+    // ---- products: a warp for each group ----
+    const int t = warp - 12;
+    constexpr uint32_t kScores = product_of(kKeys / 2, false), kSums = product_of(D, true);
+    const uint32_t o_at = tmem + 256 + D * t;
+    const uint64_t queries = operand(smem + Sh::kQ + t * Sh::kOperand, 16, 1024);
+    uint32_t n = 0, count = 0, tiles = 0;                  // steps; steps and tiles of the group
+    // scores of 64 of the keys in buffer `buffer`
+    auto scores = [&](uint32_t buffer, int h) {
+      tm_fence_after();
+      if (lane == 0) {
+        const uint64_t keys = operand(smem + Sh::kK + buffer * Sh::kOperand + h * (kHalf / 2), 16, 1024);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if (j > place.k0 && j - 1 < limit[t]) {          // the sums of the step before
-            if (!wait(kVFull + before, ((n - 1u) >> 1) & 1u) || !wait(kPReady + t, (count[t] - 1u) & 1u)) break;
-            tm_fence_after();
-            if (lane == 0) {
-              const uint32_t v_at = smem + Sh::kV + before * Sh::kOperand;
-#pragma unroll
-              for (int k = 0; k < kKeys / 16; ++k)
-                product_ts(tmem + 256 + D * t, tmem + 128 * t + 8 * k, operand(v_at + 2048 * k, kHalf, 1024), kSums, j - 1 > place.k0 || k > 0);
-              tm_commit(bars + 8 * (kODone + t));
-            }
-            __syncwarp();
-          }
-          if (j < limit[t]) {
-            if (j == place.k0 && !wait(kQFull + t, tiles[t] & 1u)) break;
-            if (!wait(kKFull + buffer, (n >> 1) & 1u)) break;
-            if (count[t] > 0 && !wait(kODone + t, (count[t] - 1u) & 1u)) break;  // the weights in the scores' place have been used
-            tm_fence_after();
-            if (lane == 0) {
-              const uint32_t q_at = smem + Sh::kQ + t * Sh::kOperand, k_at = smem + Sh::kK + buffer * Sh::kOperand;
-#pragma unroll
-              for (int k = 0; k < D / 16; ++k) {
-                const uint32_t off = (k / 4) * kHalf + (k % 4) * 32;
-                product_ss(tmem + 128 * t, operand(q_at + off, 16, 1024), operand(k_at + off, 16, 1024), kScores, k > 0);
-              }
-              tm_commit(bars + 8 * (kSFull + t));
-            }
-            __syncwarp();
-            ++count[t];
-          }
+        for (int k = 0; k < D / 16; ++k) {
+          constexpr uint32_t kUnit = 16;                   // bytes that a descriptor's address counts
+          const uint32_t off = ((k / 4) * kHalf + (k % 4) * 32) / kUnit;
+          product_ss(tmem + 128 * t + 64 * h, queries + off, keys + off, kScores, k > 0);
         }
-        if (lane == 0) {
-          if (j < place.k1) tm_commit(bars + 8 * (kKFree + buffer));
-          if (j > place.k0) tm_commit(bars + 8 * (kVFree + before));
-        }
-        __syncwarp();
-        if (j < place.k1) ++n;
+        tm_commit(bars + 8 * (kSFull + 2 * t + h));
+        if (h == 1) tm_commit(bars + 8 * (kKFree + buffer));
       }
+      __syncwarp();
+    };
+    do {
+      const int limit = place.limit(t, p);
+      int j = place.k0;
+      if (j < limit) {
+        if (!wait(kQFull + t, tiles & 1u) || !wait(kKFull + (n & 1u), (n >> 1) & 1u)) break;
+        ++tiles;
+        for (int h = 0; h < 2; ++h) {
+          // the weights in the scores' place have been used
+          if (count > 0 && !wait(kODone + 2 * t + h, (count - 1u) & 1u)) break;
+          scores(n & 1u, h);
+        }
+      }
+      for (; j < limit && ok; ++j) {
+        const uint32_t buffer = n & 1u;
+        if (!wait(kVFull + buffer, (n >> 1) & 1u)) break;
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+          if (!wait(kPReady + 2 * t + h, count & 1u)) break;
+          tm_fence_after();
+          if (lane == 0) {
+            const uint64_t values = operand(smem + Sh::kV + buffer * Sh::kOperand + h * (kHalf / 2), kHalf, 1024);
 #pragma unroll
-      for (int t = 0; t < 2; ++t) tiles[t] += limit[t] > place.k0 ? 1u : 0u;
+            for (int k = 0; k < kKeys / 32; ++k)           // 16 tokens: 2048 bytes
+              product_ts(o_at, tmem + 128 * t + 64 * h + 8 * k, values + 128 * k, kSums, j > place.k0 || h > 0 || k > 0);
+            tm_commit(bars + 8 * (kODone + 2 * t + h));
+            if (h == 1) tm_commit(bars + 8 * (kVFree + buffer));
+          }
+          __syncwarp();
+          if (j + 1 < limit) {
+            if (h == 0 && !wait(kKFull + (buffer ^ 1u), ((n + 1u) >> 1) & 1u)) break;
+            if (!wait(kODone + 2 * t + h, count & 1u)) break;
+            scores(buffer ^ 1u, h);
+          }
+        }
+        ++n;
+        ++count;
+      }
+      // steps that only the other group has: the buffers are not waited for on this one's account
+      for (; j < place.k1 && ok; ++j, ++n) {
+        const uint32_t buffer = n & 1u, phase = (n >> 1) & 1u;
+        if (!wait(kKFull + buffer, phase)) break;
+        if (lane == 0) bar_arrive(bars + 8 * (kKFree + buffer));
+        if (!wait(kVFull + buffer, phase)) break;
+        if (lane == 0) bar_arrive(bars + 8 * (kVFree + buffer));
+        __syncwarp();
+      }
     } while (ok && place.next(p));
     // everything issued has ended before the tensor memory is given back
-    if (lane == 0) {
-      for (int t = 0; t < 2; ++t) {
-        if (count[t] > 0) {
-          bar_wait(bars + 8 * (kSFull + t), (count[t] - 1u) & 1u);
-          bar_wait(bars + 8 * (kODone + t), (count[t] - 1u) & 1u);
-        }
+    if (count > 0) {
+      for (int h = 0; h < 2; ++h) {
+        bar_wait(bars + 8 * (kSFull + 2 * t + h), (count - 1u) & 1u);
+        bar_wait(bars + 8 * (kODone + 2 * t + h), (count - 1u) & 1u);
       }
     }
     __syncwarp();
