@@ -13,6 +13,7 @@ constexpr int kGranules = kKeys / 16;        // parts of a step that lie within 
 constexpr int kThreads = 4 * 128;            // two softmax warpgroups, one that widens codes, one whose first warp issues the products
 // Registers: 128 a thread at launch, dealt out again among the four: 2 * 168 + 112 + 64 = 4 * 128.
 constexpr int kSoftmaxRegs = 168, kWidenRegs = 112, kProductRegs = 64;
+constexpr int kTileSteps = 3;                // what beginning and ending a tile costs, in steps
 constexpr int kMeta = 4;                     // steps whose scales are kept
 constexpr uint32_t kPolls = 1u << 20;        // of a wait inside the CTA: tens of milliseconds at least, where a sound one takes microseconds
 
@@ -161,35 +162,44 @@ __device__ __forceinline__ int steps_of(const Request& r, long long rows, long l
   return seen > 0 ? (seen - 1) / kKeys + 1 : 1;
 }
 
-// Where a CTA is in its share of the work.  Order: request, key head, tile of rows, step.
+// Where a CTA is in its share of the work.  Order: request, key head, tile of rows, step; in front of a tile's steps lie kTileSteps units that stand for
+// what beginning and ending it costs.
 struct Place {
   int request, head, tile;
   Request r;
   long long rows;                 // rows of the request times the group
   int steps;                      // of the tile
-  int k0, k1;                     // steps that the CTA takes of it
-  unsigned long long unit, end;   // the first of them; where the CTA's share ends
+  int from, upto;                 // units that the CTA takes of it,
+  int k0, k1;                     // and steps
+  int before;                     // steps that the CTA has had before
+  unsigned long long unit, end;   // the first unit; where the CTA's share ends
 
   __device__ __forceinline__ void take(const AttentionParams& p) {
     steps = steps_of(r, rows, static_cast<long long>(tile) * kTilesRows, p);
-    k1 = static_cast<int>(min(static_cast<unsigned long long>(steps), k0 + (end - unit)));
+    upto = static_cast<int>(min(static_cast<unsigned long long>(steps + kTileSteps), from + (end - unit)));
+    k0 = max(0, from - kTileSteps);
+    k1 = max(0, upto - kTileSteps);
   }
+  // the next tile of which the CTA has steps
   __device__ __forceinline__ bool next(const AttentionParams& p) {
-    unit += k1 - k0;
-    if (unit >= end) return false;
-    k0 = 0;
-    if (static_cast<long long>(++tile) * kTilesRows >= rows) {
-      tile = 0;
-      if (++head == p.kv_heads) {
-        head = 0;
-        do {
-          if (++request >= p.requests) return false;
-          r = request_of(p, request);
-        } while (r.rows == 0);
-        rows = static_cast<long long>(r.rows) * p.group;
+    do {
+      unit += upto - from;
+      before += k1 - k0;
+      if (unit >= end) return false;
+      from = 0;
+      if (static_cast<long long>(++tile) * kTilesRows >= rows) {
+        tile = 0;
+        if (++head == p.kv_heads) {
+          head = 0;
+          do {
+            if (++request >= p.requests) return false;
+            r = request_of(p, request);
+          } while (r.rows == 0);
+          rows = static_cast<long long>(r.rows) * p.group;
+        }
       }
-    }
-    take(p);
+      take(p);
+    } while (k1 == k0);
     return true;
   }
   // steps of the half of the tile (128 rows) that group t has: as far as its last row sees, 0 where it has no row
@@ -245,7 +255,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
     const Request r = request_of(p, i);
     const long long rows = static_cast<long long>(r.rows) * p.group;
     unsigned long long sum = 0;
-    for (long long row0 = static_cast<long long>(lane) * kTilesRows; row0 < rows; row0 += 32ll * kTilesRows) sum += steps_of(r, rows, row0, p);
+    for (long long row0 = static_cast<long long>(lane) * kTilesRows; row0 < rows; row0 += 32ll * kTilesRows) sum += steps_of(r, rows, row0, p) + kTileSteps;
 #pragma unroll
     for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(kFull, sum, d);
     if (lane == 0) s_units[i] = sum;                       // of one key head
@@ -296,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
     }
     __syncthreads();
   }
-  const unsigned long long ctas = total < gridDim.x ? total : gridDim.x;
+  const unsigned int ctas = total < gridDim.x ? static_cast<unsigned int>(total) : gridDim.x;
   {
     place.request = s_found;
     place.r = request_of(p, place.request);
@@ -308,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
     int tile = 0;
     for (;;) {
       const long long row0 = static_cast<long long>(tile + lane) * kTilesRows;
-      const int n = row0 < place.rows ? steps_of(place.r, place.rows, row0, p) : 0;
+      const int n = row0 < place.rows ? steps_of(place.r, place.rows, row0, p) + kTileSteps : 0;
       int upto = n;
 #pragma unroll
       for (int d = 1; d < 32; d *= 2) {
@@ -331,8 +341,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
       }
     }
     place.tile = tile;
-    place.k0 = static_cast<int>(rest);
+    place.from = static_cast<int>(rest);
+    place.before = 0;
     place.take(p);
+    if (place.k1 == place.k0 && !place.next(p)) return;
   }
   if (warp == 12) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem)) : "memory");
@@ -343,7 +355,6 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
   tm_fence_after();
   const uint32_t tmem = s_tmem, bars = smem + Sh::kBars;
   bool ok = true;
-  const unsigned long long share = place.unit;             // the CTA's first step
   // a wait that runs out ends the warp's work, and the others' waits run out in turn
   auto wait = [&](int bar, uint32_t parity) {
     ok = __all_sync(kFull, ok && bar_wait(bars + 8 * bar, parity));
@@ -404,7 +415,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
       if (any) {
         const float by_scale = factor * fabsf(p.scale_log2);
         const int seen = place.r.seen(token), seen_first = place.r.seen(static_cast<int>(row0 / p.group));
-        uint32_t scales = static_cast<uint32_t>(place.unit - share) % kMeta;
+        uint32_t scales = static_cast<uint32_t>(place.before) % kMeta;
         for (int j = place.k0; j < limit; ++j, ++count, scales = (scales + 1) % kMeta) {
           const bool mask = (j + 1) * kKeys > seen_first;  // as far as the group's first row sees
 #pragma unroll 1
@@ -506,8 +517,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
         }
         tm_fence_before();
       }
-      const unsigned long long tile_begin = place.unit - place.k0;
-      const int first = static_cast<int>(((tile_begin + 1) * ctas - 1) / total), last = static_cast<int>(((tile_begin + place.steps) * ctas - 1) / total);
+      const unsigned long long tile_begin = place.unit - place.from + kTileSteps;  // its first step
+      const int first = owner_of(tile_begin, total, ctas), last = owner_of(tile_begin + place.steps - 1, total, ctas);
       __threadfence();
       __syncwarp();
       unsigned int done = 0u;                              // a warp's rows by themselves
