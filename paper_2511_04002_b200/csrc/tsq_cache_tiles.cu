@@ -45,8 +45,8 @@ __device__ __forceinline__ void tm_fence_before() { asm volatile("tcgen05.fence:
 __device__ __forceinline__ void tm_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tm_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tm_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ void tm_commit(uint32_t leader, uint32_t bar) {
+  asm volatile("{\n\t.reg .pred e;\n\tsetp.ne.u32 e, %1, 0;\n\t@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(leader) : "memory");
 }
 
 #define TSQ_R8(v, i) "=r"(v[i]), "=r"(v[i + 1]), "=r"(v[i + 2]), "=r"(v[i + 3]), "=r"(v[i + 4]), "=r"(v[i + 5]), "=r"(v[i + 6]), "=r"(v[i + 7])
@@ -143,16 +143,26 @@ __device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t leading, uint3
 __host__ __device__ constexpr uint32_t product_of(int columns, bool b_mn_major) {
   return 1u << 4 | (b_mn_major ? 1u << 16 : 0u) | static_cast<uint32_t>(columns / 8) << 17 | (128u / 16u) << 24;
 }
-__device__ __forceinline__ void product_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(what),
-               "r"(static_cast<uint32_t>(add))
-               : "memory");
+// The whole warp comes here and `leader` is set in one thread of it: a guard on the instruction instead of a branch around it leaves the operands' arithmetic to
+// the warp's uniform registers, from which the instruction takes them.
+__device__ __forceinline__ void product_ss(uint32_t leader, uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 e, %5, 0;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b),
+      "r"(what), "r"(static_cast<uint32_t>(add)), "r"(leader)
+      : "memory");
 }
-__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(what),
-               "r"(static_cast<uint32_t>(add))
-               : "memory");
+__device__ __forceinline__ void product_ts(uint32_t leader, uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 e, %5, 0;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b),
+      "r"(what), "r"(static_cast<uint32_t>(add)), "r"(leader)
+      : "memory");
 }
+__device__ __forceinline__ uint32_t elected() {
+  uint32_t e;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+  return e;
+}
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(kFull, v, 0); }
 
 // ---- work ----------------------------------------------------------------------------------------
 
@@ -648,26 +658,22 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
   }
   if (warp == 12 || warp == 13) {
     // ---- products: a warp for each group ----
-    const int t = warp - 12;
+    const int t = static_cast<int>(uniform(warp - 12));
+    const uint32_t leader = elected(), base = uniform(smem), bar = uniform(bars), tm = uniform(tmem);
     constexpr uint32_t kScores = product_of(kKeys / 2, false), kSums = product_of(D, true);
-    const uint32_t o_at = tmem + 256 + D * t;
-    const uint64_t queries = operand(smem + Sh::kQ + t * Sh::kOperand, 16, 1024);
     uint32_t n = 0, count = 0, tiles = 0;                  // steps; steps and tiles of the group
     // scores of 64 of the keys in buffer `buffer`
     auto scores = [&](uint32_t buffer, int h) {
       tm_fence_after();
-      if (lane == 0) {
-        const uint64_t keys = operand(smem + Sh::kK + buffer * Sh::kOperand + h * (kHalf / 2), 16, 1024);
+      const uint64_t queries = operand(base + Sh::kQ + t * Sh::kOperand, 16, 1024), keys = operand(base + Sh::kK + buffer * Sh::kOperand + h * (kHalf / 2), 16, 1024);
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          constexpr uint32_t kUnit = 16;                   // bytes that a descriptor's address counts
-          const uint32_t off = ((k / 4) * kHalf + (k % 4) * 32) / kUnit;
-          product_ss(tmem + 128 * t + 64 * h, queries + off, keys + off, kScores, k > 0);
-        }
-        tm_commit(bars + 8 * (kSFull + 2 * t + h));
-        if (h == 1) tm_commit(bars + 8 * (kKFree + buffer));
+      for (int k = 0; k < D / 16; ++k) {
+        constexpr uint32_t kUnit = 16;                     // bytes that a descriptor's address counts
+        const uint32_t off = ((k / 4) * kHalf + (k % 4) * 32) / kUnit;
+        product_ss(leader, tm + 128 * t + 64 * h, queries + off, keys + off, kScores, k > 0);
       }
-      __syncwarp();
+      tm_commit(leader, bar + 8 * (kSFull + 2 * t + h));
+      if (h == 1) tm_commit(leader, bar + 8 * (kKFree + buffer));
     };
     do {
       const int limit = place.limit(t, p);
@@ -678,25 +684,23 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
         for (int h = 0; h < 2; ++h) {
           // the weights in the scores' place have been used
           if (count > 0 && !wait(kODone + 2 * t + h, (count - 1u) & 1u)) break;
-          scores(n & 1u, h);
+          scores(uniform(n & 1u), h);
         }
       }
       for (; j < limit && ok; ++j) {
-        const uint32_t buffer = n & 1u;
+        const uint32_t buffer = uniform(n & 1u);
         if (!wait(kVFull + buffer, (n >> 1) & 1u)) break;
-#pragma unroll 1
+#pragma unroll
         for (int h = 0; h < 2; ++h) {
           if (!wait(kPReady + 2 * t + h, count & 1u)) break;
           tm_fence_after();
-          if (lane == 0) {
-            const uint64_t values = operand(smem + Sh::kV + buffer * Sh::kOperand + h * (kHalf / 2), kHalf, 1024);
+          const uint64_t values = operand(base + Sh::kV + buffer * Sh::kOperand + h * (kHalf / 2), kHalf, 1024);
+          const uint32_t add = uniform(j > place.k0 || h > 0);
 #pragma unroll
-            for (int k = 0; k < kKeys / 32; ++k)           // 16 tokens: 2048 bytes
-              product_ts(o_at, tmem + 128 * t + 64 * h + 8 * k, values + 128 * k, kSums, j > place.k0 || h > 0 || k > 0);
-            tm_commit(bars + 8 * (kODone + 2 * t + h));
-            if (h == 1) tm_commit(bars + 8 * (kVFree + buffer));
-          }
-          __syncwarp();
+          for (int k = 0; k < kKeys / 32; ++k)             // 16 tokens: 2048 bytes
+            product_ts(leader, tm + 256 + D * t, tm + 128 * t + 64 * h + 8 * k, values + 128 * k, kSums, add != 0u || k > 0);
+          tm_commit(leader, bar + 8 * (kODone + 2 * t + h));
+          if (h == 1) tm_commit(leader, bar + 8 * (kVFree + buffer));
           if (j + 1 < limit) {
             if (h == 0 && !wait(kKFull + (buffer ^ 1u), ((n + 1u) >> 1) & 1u)) break;
             if (!wait(kODone + 2 * t + h, count & 1u)) break;
