@@ -10,9 +10,9 @@ namespace {
 
 constexpr int kKeys = 128;                   // tokens of a step
 constexpr int kGranules = kKeys / 16;        // parts of a step that lie within one page
-constexpr int kThreads = 4 * 128;            // two softmax warpgroups, one that widens codes, one whose first warp issues the products
-// Registers: 128 a thread at launch, dealt out again among the four: 2 * 168 + 112 + 64 = 4 * 128.
-constexpr int kSoftmaxRegs = 168, kWidenRegs = 112, kProductRegs = 64;
+constexpr int kThreads = 5 * 128;            // two softmax warpgroups, two that widen codes, one whose first two warps issue the products
+// Registers: 96 a thread at launch, dealt out again among the five: 2 * 136 + 2 * 80 + 48 = 5 * 96.
+constexpr int kSoftmaxRegs = 136, kWidenRegs = 80, kProductRegs = 48;
 constexpr int kTileSteps = 3;                // what beginning and ending a tile costs, in steps
 constexpr int kMeta = 4;                     // steps whose scales are kept
 constexpr uint32_t kPolls = 1u << 20;        // of a wait inside the CTA: tens of milliseconds at least, where a sound one takes microseconds
@@ -238,7 +238,7 @@ __host__ __device__ constexpr uint32_t arrivals_of(int bar) {  // threads, or on
 
 // A CTA's two groups of 128 threads have 128 query rows each, a thread a row; a tile is the 256 rows of one (request, key head) that follow one another, the group's query
 // heads of a token side by side, so that widened codes serve both groups and all heads.  Per step of 128 tokens:
-//   widening group  codes from global memory (a step ahead in registers) to binary16 (exact) in shared memory, two buffers each for keys and values
+//   widening groups one for the keys, one for the values: codes from global memory (a step ahead in registers) to binary16 (exact) in shared memory, two buffers each
 //   product warps   one for each group: S = Q K^T into tensor memory, then O += P V with P from tensor memory
 //   softmax groups  S out of tensor memory, w = 2^(S * scale + log2 s_v - m) to binary16 in S's place, sums in binary32
 // Scores come in halves of 64 keys, each with its place in tensor memory: while a group works on one, its products fill the other, and the other group's run besides.
@@ -356,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
     place.take(p);
     if (place.k1 == place.k0 && !place.next(p)) return;
   }
-  if (warp == 12) {
+  if (warp == 16) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -571,17 +571,22 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
         }
       }
     }
-  } else if (warp < 12) {
-    // ---- codes to binary16 ----
+  } else if (warp < 16) {
+    // ---- codes to binary16: a warpgroup for the keys, one for the values ----
     regs_down<kWidenRegs>();
     constexpr int kChunks = D / 16;                        // 16-byte chunks of a token's codes
     constexpr int kItems = kKeys * kChunks / 128;          // per thread and step
-    const int w = warp - 8, in_group = tid - 256;
+    const bool values = warp >= 12;
+    const int w = warp % 4, in_group = tid % 128;
+    const int8_t* const codes = values ? p.v_codes : p.k_codes;
+    const int full = values ? kVFull : kKFull, free = values ? kVFree : kKFree;
     // eight neighbouring lanes write four chunks of two neighbouring tokens: the swizzle puts those in different banks
     const int token0 = D == 128 ? w * 4 + (lane >> 4) * 2 + ((lane >> 2) & 1) : w * 8 + (lane >> 2);
     const int chunk = D == 128 ? (lane & 3) | ((lane >> 3) & 1) << 2 : lane & 3;
+    unsigned char* const to = smem_at + (values ? Sh::kV : Sh::kK) + (chunk / 4) * kHalf;
+    const bool has_scale = !values && in_group < kGranules;  // the keys' group leaves the scales too, a thread for each granule
     uint32_t n = 0;                                        // steps so far
-    uint4 k[kItems], v[kItems];
+    uint4 raw[kItems];
     float4 scale = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     // pages of the next step's granules; -1 where there is none
     int pages[kItems], scale_page = -1;
@@ -593,72 +598,59 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
     auto fetch_pages = [&](int j) {
 #pragma unroll
       for (int it = 0; it < kItems; ++it) pages[it] = page_at(j, (token0 + it * (128 / kChunks)) / 16);
-      if (in_group < kGranules) scale_page = page_at(j, in_group);
+      if (has_scale) scale_page = page_at(j, in_group);
     };
-    auto fetch = [&](int j, const int8_t* codes, uint4 (&into)[kItems]) {
+    auto fetch = [&](int j) {
 #pragma unroll
       for (int it = 0; it < kItems; ++it) {
         const int token = j * kKeys + token0 + it * (128 / kChunks);
-        into[it] = make_uint4(0u, 0u, 0u, 0u);
+        raw[it] = make_uint4(0u, 0u, 0u, 0u);
         if (static_cast<unsigned>(pages[it]) < static_cast<unsigned>(p.pages))
-          into[it] = *(reinterpret_cast<const uint4*>(codes + (((static_cast<long long>(pages[it]) * p.kv_heads + place.head) << p.page_shift) +
-                                                               (token & ((1 << p.page_shift) - 1))) * D) + chunk);
+          raw[it] = *(reinterpret_cast<const uint4*>(codes + (((static_cast<long long>(pages[it]) * p.kv_heads + place.head) << p.page_shift) +
+                                                              (token & ((1 << p.page_shift) - 1))) * D) + chunk);
       }
-    };
-    auto fetch_scale = [&]() {
-      if (in_group >= kGranules) return;
-      scale = make_float4(0.0f, -INFINITY, 0.0f, 0.0f);    // nothing of a page that is not there is seen
-      if (static_cast<unsigned>(scale_page) < static_cast<unsigned>(p.pages)) {
-        const long long page_head = static_cast<long long>(scale_page) * p.kv_heads + place.head;
-        const float vs = fmaxf(p.v_scale[page_head], kLeastScale);
-        scale = make_float4(p.k_scale[page_head], __log2f(vs), 1.0f / vs, 0.0f);
-      }
-    };
-    auto widen = [&](const uint4 (&from)[kItems], unsigned char* to) {
-#pragma unroll
-      for (int it = 0; it < kItems; ++it) {
-        const int token = token0 + it * (128 / kChunks);
-        const uint32_t u[4] = {from[it].x ^ 0x80808080u, from[it].y ^ 0x80808080u, from[it].z ^ 0x80808080u, from[it].w ^ 0x80808080u};
-        unsigned char* const at = to + (chunk / 4) * kHalf + token * 128;
-        const int c = 2 * (chunk % 4), x = token & 7;
-        *reinterpret_cast<uint4*>(at + ((c ^ x) << 4)) = make_uint4(widen_lo(u[0]), widen_hi(u[0]), widen_lo(u[1]), widen_hi(u[1]));
-        *reinterpret_cast<uint4*>(at + (((c + 1) ^ x) << 4)) = make_uint4(widen_lo(u[2]), widen_hi(u[2]), widen_lo(u[3]), widen_hi(u[3]));
+      if (has_scale) {
+        scale = make_float4(0.0f, -INFINITY, 0.0f, 0.0f);  // nothing of a page that is not there is seen
+        if (static_cast<unsigned>(scale_page) < static_cast<unsigned>(p.pages)) {
+          const long long page_head = static_cast<long long>(scale_page) * p.kv_heads + place.head;
+          const float vs = fmaxf(p.v_scale[page_head], kLeastScale);
+          scale = make_float4(p.k_scale[page_head], __log2f(vs), 1.0f / vs, 0.0f);
+        }
       }
     };
     int j = place.k0;
     bool more = true;
     fetch_pages(j);
-    fetch_scale();
-    fetch(j, p.k_codes, k);
-    fetch(j, p.v_codes, v);
+    fetch(j);
     while (more) {
       if (++j >= place.k1) {                               // the step behind this one
         more = place.next(p);
         j = place.k0;
       }
       if (more) fetch_pages(j);
-      if (!wait(kKFree + (n & 1u), ((n >> 1) & 1u) ^ 1u)) break;
-      if (in_group < kGranules) reinterpret_cast<float4*>(smem_at + Sh::kScales)[(n % kMeta) * kGranules + in_group] = scale;
-      widen(k, smem_at + Sh::kK + (n & 1u) * Sh::kOperand);
-      fence_proxy_async_smem();
-      bar_arrive(bars + 8 * (kKFull + (n & 1u)));
-      if (more) {
-        fetch(j, p.k_codes, k);
-        fetch_scale();
+      const uint32_t buffer = n & 1u;
+      if (!wait(free + buffer, ((n >> 1) & 1u) ^ 1u)) break;
+      if (has_scale) reinterpret_cast<float4*>(smem_at + Sh::kScales)[(n % kMeta) * kGranules + in_group] = scale;
+#pragma unroll
+      for (int it = 0; it < kItems; ++it) {
+        const int token = token0 + it * (128 / kChunks);
+        const uint32_t u[4] = {raw[it].x ^ 0x80808080u, raw[it].y ^ 0x80808080u, raw[it].z ^ 0x80808080u, raw[it].w ^ 0x80808080u};
+        unsigned char* const at = to + buffer * Sh::kOperand + token * 128;
+        const int c = 2 * (chunk % 4), x = token & 7;
+        *reinterpret_cast<uint4*>(at + ((c ^ x) << 4)) = make_uint4(widen_lo(u[0]), widen_hi(u[0]), widen_lo(u[1]), widen_hi(u[1]));
+        *reinterpret_cast<uint4*>(at + (((c + 1) ^ x) << 4)) = make_uint4(widen_lo(u[2]), widen_hi(u[2]), widen_lo(u[3]), widen_hi(u[3]));
       }
-      if (!wait(kVFree + (n & 1u), ((n >> 1) & 1u) ^ 1u)) break;
-      widen(v, smem_at + Sh::kV + (n & 1u) * Sh::kOperand);
       fence_proxy_async_smem();
-      bar_arrive(bars + 8 * (kVFull + (n & 1u)));
-      if (more) fetch(j, p.v_codes, v);
+      bar_arrive(bars + 8 * (full + buffer));
+      if (more) fetch(j);
       ++n;
     }
   } else {
     regs_down<kProductRegs>();
   }
-  if (warp == 12 || warp == 13) {
+  if (warp == 16 || warp == 17) {
     // ---- products: a warp for each group ----
-    const int t = static_cast<int>(uniform(warp - 12));
+    const int t = static_cast<int>(uniform(warp - 16));
     const uint32_t leader = elected(), base = uniform(smem), bar = uniform(bars), tm = uniform(tmem);
     constexpr uint32_t kScores = product_of(kKeys / 2, false), kSums = product_of(D, true);
     uint32_t n = 0, count = 0, tiles = 0;                  // steps; steps and tiles of the group
@@ -733,7 +725,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
   tm_fence_before();
   __syncthreads();
   tm_fence_after();
-  if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  if (warp == 16) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   if (tid == 0 && s_failed != 0u) atomicExch(p.status, static_cast<unsigned>(TSQ_ERR_TIMEOUT));
 }
 
