@@ -12,7 +12,7 @@ constexpr int kKeys = 128;                   // tokens of a step
 constexpr int kGranules = kKeys / 16;        // parts of a step that lie within one page
 constexpr int kThreads = 5 * 128;            // two softmax warpgroups, two that widen codes, one whose first two warps issue the products
 // Registers: 96 a thread at launch, dealt out again among the five: 2 * 136 + 2 * 80 + 48 = 5 * 96.
-constexpr int kSoftmaxRegs = 136, kWidenRegs = 80, kProductRegs = 48;
+constexpr int kSoftmaxRegs = 136, kWidenRegs = 80, kProductRegs = 48, kLaunchRegs = 96;
 constexpr int kTileSteps = 3;                // what beginning and ending a tile costs, in steps
 constexpr int kMeta = 4;                     // steps whose scales are kept
 constexpr uint32_t kPolls = 1u << 20;        // of a wait inside the CTA: tens of milliseconds at least, where a sound one takes microseconds
@@ -20,8 +20,10 @@ constexpr uint32_t kPolls = 1u << 20;        // of a wait inside the CTA: tens o
 // ---- barriers, tensor memory, products -----------------------------------------------------------
 
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+// One arrival for the warp, behind what its threads have done (and fenced, where another proxy is to see it).
 __device__ __forceinline__ void bar_arrive(uint32_t bar) {
-  asm volatile("{\n\t.reg .b64 s;\n\tmbarrier.arrive.shared::cta.b64 s, [%0];\n\t}" ::"r"(bar) : "memory");
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) asm volatile("{\n\t.reg .b64 s;\n\tmbarrier.arrive.shared::cta.b64 s, [%0];\n\t}" ::"r"(bar) : "memory");
 }
 // Whether the phase of that parity has ended; false after kPolls polls.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
@@ -39,6 +41,18 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
 
 template <int N>
 __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+// The end of a role: back to the launch's registers, so that the code behind the roles may use any of those, whichever role a warp comes from.  (Behind roles of
+// different counts nothing keeps a value out of the registers that the smallest role has given away.)  The warps of a warpgroup meet between two setmaxnreg.
+template <int N>
+__device__ __forceinline__ void regs_back(int group, bool failed, uint32_t* s_failed) {
+  if (failed) *s_failed = 1u;
+  asm volatile("bar.sync %0, 128;" ::"r"(group + 1) : "memory");
+  if constexpr (N > kLaunchRegs) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLaunchRegs));
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kLaunchRegs));
+  }
+}
 template <int N>
 __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 __device__ __forceinline__ void tm_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -61,6 +75,13 @@ __device__ __forceinline__ void tm_load32(uint32_t (&v)[32], uint32_t at) {
 }
 __device__ __forceinline__ void tm_load16(uint32_t (&v)[16], uint32_t at) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];" : TSQ_R8(v, 0), TSQ_R8(v, 8) : "r"(at));
+}
+__device__ __forceinline__ void tm_store32(uint32_t at, const uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
+      "%32};" ::"r"(at),
+      TSQ_W8(v, 0), TSQ_W8(v, 8), TSQ_W8(v, 16), TSQ_W8(v, 24)
+      : "memory");
 }
 __device__ __forceinline__ void tm_store16(uint32_t at, const uint32_t (&v)[16]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at), TSQ_W8(v, 0), TSQ_W8(v, 8) : "memory");
@@ -103,9 +124,9 @@ __device__ __forceinline__ float top_score(const uint32_t (&scores)[32], uint32_
   }
   return most;
 }
-// Their weights in binary16, two to a word; returns the sum l and theirs over the values' scale.
+// Weights of 64 keys in binary16, two to a word; returns their sum over the values' scale.
 template <bool MASK>
-__device__ __forceinline__ float weights_of(const uint32_t (&s)[32], uint32_t (&w)[16], uint32_t scales, float by_scale, float m, float l, int left) {
+__device__ __forceinline__ void weights_of_32(const uint32_t (&s)[32], uint32_t* w, uint32_t scales, float by_scale, float m, float& l, int left) {
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
     const float4 f = shared_float4(scales + 16 * g);
@@ -129,7 +150,19 @@ __device__ __forceinline__ float weights_of(const uint32_t (&s)[32], uint32_t (&
     unpack2f(sum, even, odd);
     l = __fmaf_rn(even + odd, f.z, l);
   }
-  return l;
+}
+template <bool MASK>
+__device__ __forceinline__ float weights_of(const uint32_t (&a)[32], const uint32_t (&b)[32], uint32_t (&w)[32], uint32_t scales, float by_scale, float m, int left) {
+  float sum = 0.0f;
+  weights_of_32<MASK>(a, w, scales, by_scale, m, sum, left);
+  weights_of_32<MASK>(b, w + 16, scales + 32, by_scale, m, sum, left - 32);
+  return sum;
+}
+__device__ __forceinline__ float top_weight(const uint32_t (&w)[32]) {
+  __half2 t = Elem<false>::as2(w[0]);
+#pragma unroll
+  for (int e = 1; e < 32; ++e) t = __hmax2(t, Elem<false>::as2(w[e]));
+  return fmaxf(__low2float(t), __high2float(t));
 }
 
 // Shared-memory descriptors of 128-byte swizzled operands: rows of 128 bytes, eight rows to a 1024-byte atom.
@@ -232,8 +265,8 @@ struct Shared {
 };
 // Barriers: buffers of keys and values; a half step's scores, weights and sums, by group and half; a tile's queries, by group.
 enum Bar { kKFull = 0, kKFree = 2, kVFull = 4, kVFree = 6, kSFull = 8, kPReady = 12, kODone = 16, kQFull = 20, kBarCount = 22 };
-__host__ __device__ constexpr uint32_t arrivals_of(int bar) {  // threads, or one for the products of each group
-  return bar < kKFree || (bar >= kVFull && bar < kVFree) || (bar >= kPReady && bar < kODone) || bar >= kQFull ? 128u : bar < kSFull ? 2u : 1u;
+__host__ __device__ constexpr uint32_t arrivals_of(int bar) {  // a group's warps, or one for the products of each group
+  return bar < kKFree || (bar >= kVFull && bar < kVFree) || (bar >= kPReady && bar < kODone) || bar >= kQFull ? 4u : bar < kSFull ? 2u : 1u;
 }
 
 // A CTA's two groups of 128 threads have 128 query rows each, a thread a row; a tile is the 256 rows of one (request, key head) that follow one another, the group's query
@@ -421,7 +454,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
       const long long at = row0 + min(row, rows - 1);
       const int token = static_cast<int>(at / p.group), query_head = place.head * p.group + static_cast<int>(at % p.group);
       float m = 0.0f, l = 0.0f;
-      bool have = false;
+      bool have = false, settled = false;                  // the row has a reference; every row of the warp has one
       if (any) {
         const float by_scale = factor * fabsf(p.scale_log2);
         const int seen = place.r.seen(token), seen_first = place.r.seen(static_cast<int>(row0 / p.group));
@@ -434,20 +467,27 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
             tm_fence_after();
             const uint32_t at_half = s_at + 64 * h, factors = smem + Sh::kScales + (scales * kGranules + 4 * h) * 16;
             const int left = seen - j * kKeys - 64 * h;    // keys of the half that the row sees
-            uint32_t a[32], b[32], w[16];
+            uint32_t a[32], b[32], w[32];
             tm_load32(a, at_half);
             tm_load32(b, at_half + 32);
             tm_wait_ld();
-            const float most = mask ? fmaxf(top_score<true>(a, factors, by_scale, left), top_score<true>(b, factors + 32, by_scale, left - 32))
-                                    : fmaxf(top_score<false>(a, factors, by_scale, 64), top_score<false>(b, factors + 32, by_scale, 64));
-            const bool up = have ? most > m + 8.0f : most > -INFINITY;
-            if (__any_sync(kFull, up)) {
+            float sum = 0.0f;
+            // once a row has its reference its weights are formed at once, and again only if one of them came out above 2^8
+            bool again = !settled;
+            if (settled) {
+              sum = mask ? weights_of<true>(a, b, w, factors, by_scale, m, left) : weights_of<false>(a, b, w, factors, by_scale, m, 64);
+              again = __any_sync(kFull, top_weight(w) > 256.0f);
+            }
+            if (again) {
+              const float most = mask ? fmaxf(top_score<true>(a, factors, by_scale, left), top_score<true>(b, factors + 32, by_scale, left - 32))
+                                      : fmaxf(top_score<false>(a, factors, by_scale, 64), top_score<false>(b, factors + 32, by_scale, 64));
               float by = 1.0f;
-              if (up) {
+              if (have ? most > m + 8.0f : most > -INFINITY) {
                 by = have ? exp2_fast(m - most) : 0.0f;
                 m = most;
                 have = true;
               }
+              settled = __all_sync(kFull, have);
               l *= by;
               if (j > place.k0 || h > 0) {                 // the sums so far follow the reference
                 if (!wait(kODone + 2 * t + (h ^ 1), (h > 0 ? count : count - 1u) & 1u)) break;
@@ -462,18 +502,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                   tm_store16(o_at + d, o);
                 }
               }
+              sum = weights_of<true>(a, b, w, factors, by_scale, m, mask ? left : 64);
             }
-            // weights take the place of scores, which have all been read: those of 32 that of 16
-            if (mask) {
-              l = weights_of<true>(a, w, factors, by_scale, m, l, left);
-              tm_store16(at_half, w);
-              l = weights_of<true>(b, w, factors + 32, by_scale, m, l, left - 32);
-            } else {
-              l = weights_of<false>(a, w, factors, by_scale, m, l, 64);
-              tm_store16(at_half, w);
-              l = weights_of<false>(b, w, factors + 32, by_scale, m, l, 64);
-            }
-            tm_store16(at_half + 16, w);
+            l += sum;
+            tm_store32(at_half, w);                        // in the place of scores, which have all been read
             tm_wait_st();
             tm_fence_before();
             bar_arrive(bars + 8 * (kPReady + 2 * t + h));
@@ -571,6 +603,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
         }
       }
     }
+    regs_back<kSoftmaxRegs>(warp / 4, !ok, &s_failed);
   } else if (warp < 16) {
     // ---- codes to binary16: a warpgroup for the keys, one for the values ----
     regs_down<kWidenRegs>();
@@ -645,88 +678,89 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
       if (more) fetch(j);
       ++n;
     }
+    regs_back<kWidenRegs>(warp / 4, !ok, &s_failed);
   } else {
     regs_down<kProductRegs>();
-  }
-  if (warp == 16 || warp == 17) {
-    // ---- products: a warp for each group ----
-    const int t = static_cast<int>(uniform(warp - 16));
-    const uint32_t leader = elected(), base = uniform(smem), bar = uniform(bars), tm = uniform(tmem);
-    constexpr uint32_t kScores = product_of(kKeys / 2, false), kSums = product_of(D, true);
-    uint32_t n = 0, count = 0, tiles = 0;                  // steps; steps and tiles of the group
-    // scores of 64 of the keys in buffer `buffer`
-    auto scores = [&](uint32_t buffer, int h) {
-      tm_fence_after();
-      const uint64_t queries = operand(base + Sh::kQ + t * Sh::kOperand, 16, 1024), keys = operand(base + Sh::kK + buffer * Sh::kOperand + h * (kHalf / 2), 16, 1024);
+    if (warp < 18) {
+      // ---- products: a warp for each group ----
+      const int t = static_cast<int>(uniform(warp - 16));
+      const uint32_t leader = elected(), base = uniform(smem), bar = uniform(bars), tm = uniform(tmem);
+      constexpr uint32_t kScores = product_of(kKeys / 2, false), kSums = product_of(D, true);
+      uint32_t n = 0, count = 0, tiles = 0;                  // steps; steps and tiles of the group
+      // scores of 64 of the keys in buffer `buffer`
+      auto scores = [&](uint32_t buffer, int h) {
+        tm_fence_after();
+        const uint64_t queries = operand(base + Sh::kQ + t * Sh::kOperand, 16, 1024), keys = operand(base + Sh::kK + buffer * Sh::kOperand + h * (kHalf / 2), 16, 1024);
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k) {
-        constexpr uint32_t kUnit = 16;                     // bytes that a descriptor's address counts
-        const uint32_t off = ((k / 4) * kHalf + (k % 4) * 32) / kUnit;
-        product_ss(leader, tm + 128 * t + 64 * h, queries + off, keys + off, kScores, k > 0);
-      }
-      tm_commit(leader, bar + 8 * (kSFull + 2 * t + h));
-      if (h == 1) tm_commit(leader, bar + 8 * (kKFree + buffer));
-    };
-    do {
-      const int limit = place.limit(t, p);
-      int j = place.k0;
-      if (j < limit) {
-        if (!wait(kQFull + t, tiles & 1u) || !wait(kKFull + (n & 1u), (n >> 1) & 1u)) break;
-        ++tiles;
-        for (int h = 0; h < 2; ++h) {
-          // the weights in the scores' place have been used
-          if (count > 0 && !wait(kODone + 2 * t + h, (count - 1u) & 1u)) break;
-          scores(uniform(n & 1u), h);
+        for (int k = 0; k < D / 16; ++k) {
+          constexpr uint32_t kUnit = 16;                     // bytes that a descriptor's address counts
+          const uint32_t off = ((k / 4) * kHalf + (k % 4) * 32) / kUnit;
+          product_ss(leader, tm + 128 * t + 64 * h, queries + off, keys + off, kScores, k > 0);
         }
-      }
-      for (; j < limit && ok; ++j) {
-        const uint32_t buffer = uniform(n & 1u);
-        if (!wait(kVFull + buffer, (n >> 1) & 1u)) break;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (!wait(kPReady + 2 * t + h, count & 1u)) break;
-          tm_fence_after();
-          const uint64_t values = operand(base + Sh::kV + buffer * Sh::kOperand + h * (kHalf / 2), kHalf, 1024);
-          const uint32_t add = uniform(j > place.k0 || h > 0);
-#pragma unroll
-          for (int k = 0; k < kKeys / 32; ++k)             // 16 tokens: 2048 bytes
-            product_ts(leader, tm + 256 + D * t, tm + 128 * t + 64 * h + 8 * k, values + 128 * k, kSums, add != 0u || k > 0);
-          tm_commit(leader, bar + 8 * (kODone + 2 * t + h));
-          if (h == 1) tm_commit(leader, bar + 8 * (kVFree + buffer));
-          if (j + 1 < limit) {
-            if (h == 0 && !wait(kKFull + (buffer ^ 1u), ((n + 1u) >> 1) & 1u)) break;
-            if (!wait(kODone + 2 * t + h, count & 1u)) break;
-            scores(buffer ^ 1u, h);
+        tm_commit(leader, bar + 8 * (kSFull + 2 * t + h));
+        if (h == 1) tm_commit(leader, bar + 8 * (kKFree + buffer));
+      };
+      do {
+        const int limit = place.limit(t, p);
+        int j = place.k0;
+        if (j < limit) {
+          if (!wait(kQFull + t, tiles & 1u) || !wait(kKFull + (n & 1u), (n >> 1) & 1u)) break;
+          ++tiles;
+          for (int h = 0; h < 2; ++h) {
+            // the weights in the scores' place have been used
+            if (count > 0 && !wait(kODone + 2 * t + h, (count - 1u) & 1u)) break;
+            scores(uniform(n & 1u), h);
           }
         }
-        ++n;
-        ++count;
+        for (; j < limit && ok; ++j) {
+          const uint32_t buffer = uniform(n & 1u);
+          if (!wait(kVFull + buffer, (n >> 1) & 1u)) break;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (!wait(kPReady + 2 * t + h, count & 1u)) break;
+            tm_fence_after();
+            const uint64_t values = operand(base + Sh::kV + buffer * Sh::kOperand + h * (kHalf / 2), kHalf, 1024);
+            const uint32_t add = uniform(j > place.k0 || h > 0);
+#pragma unroll
+            for (int k = 0; k < kKeys / 32; ++k)             // 16 tokens: 2048 bytes
+              product_ts(leader, tm + 256 + D * t, tm + 128 * t + 64 * h + 8 * k, values + 128 * k, kSums, add != 0u || k > 0);
+            tm_commit(leader, bar + 8 * (kODone + 2 * t + h));
+            if (h == 1) tm_commit(leader, bar + 8 * (kVFree + buffer));
+            if (j + 1 < limit) {
+              if (h == 0 && !wait(kKFull + (buffer ^ 1u), ((n + 1u) >> 1) & 1u)) break;
+              if (!wait(kODone + 2 * t + h, count & 1u)) break;
+              scores(buffer ^ 1u, h);
+            }
+          }
+          ++n;
+          ++count;
+        }
+        // steps that only the other group has: the buffers are not waited for on this one's account
+        for (; j < place.k1 && ok; ++j, ++n) {
+          const uint32_t buffer = n & 1u, phase = (n >> 1) & 1u;
+          if (!wait(kKFull + buffer, phase)) break;
+          bar_arrive(bars + 8 * (kKFree + buffer));
+          if (!wait(kVFull + buffer, phase)) break;
+          bar_arrive(bars + 8 * (kVFree + buffer));
+          __syncwarp();
+        }
+      } while (ok && place.next(p));
+      // everything issued has ended before the tensor memory is given back
+      if (count > 0) {
+        for (int h = 0; h < 2; ++h) {
+          bar_wait(bars + 8 * (kSFull + 2 * t + h), (count - 1u) & 1u);
+          bar_wait(bars + 8 * (kODone + 2 * t + h), (count - 1u) & 1u);
+        }
       }
-      // steps that only the other group has: the buffers are not waited for on this one's account
-      for (; j < place.k1 && ok; ++j, ++n) {
-        const uint32_t buffer = n & 1u, phase = (n >> 1) & 1u;
-        if (!wait(kKFull + buffer, phase)) break;
-        if (lane == 0) bar_arrive(bars + 8 * (kKFree + buffer));
-        if (!wait(kVFull + buffer, phase)) break;
-        if (lane == 0) bar_arrive(bars + 8 * (kVFree + buffer));
-        __syncwarp();
-      }
-    } while (ok && place.next(p));
-    // everything issued has ended before the tensor memory is given back
-    if (count > 0) {
-      for (int h = 0; h < 2; ++h) {
-        bar_wait(bars + 8 * (kSFull + 2 * t + h), (count - 1u) & 1u);
-        bar_wait(bars + 8 * (kODone + 2 * t + h), (count - 1u) & 1u);
-      }
+      __syncwarp();
     }
-    __syncwarp();
+    regs_back<kProductRegs>(4, !ok, &s_failed);
   }
-  if (!ok) s_failed = 1u;
   tm_fence_before();
   __syncthreads();
   tm_fence_after();
-  if (warp == 16) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
-  if (tid == 0 && s_failed != 0u) atomicExch(p.status, static_cast<unsigned>(TSQ_ERR_TIMEOUT));
+  if (threadIdx.x / 32 == 16) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(*static_cast<volatile uint32_t*>(&s_tmem)) : "memory");
+  if (threadIdx.x == 0 && s_failed != 0u) atomicExch(p.status, static_cast<unsigned>(TSQ_ERR_TIMEOUT));
 }
 
 template <bool BF16, int D>
