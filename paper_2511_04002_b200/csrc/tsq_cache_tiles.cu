@@ -57,7 +57,6 @@ template <int N>
 __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 __device__ __forceinline__ void tm_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tm_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tm_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tm_commit(uint32_t leader, uint32_t bar) {
   asm volatile("{\n\t.reg .pred e;\n\tsetp.ne.u32 e, %1, 0;\n\t@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(leader) : "memory");
@@ -72,6 +71,13 @@ __device__ __forceinline__ void tm_load32(uint32_t (&v)[32], uint32_t at) {
       "[%32];"
       : TSQ_R8(v, 0), TSQ_R8(v, 8), TSQ_R8(v, 16), TSQ_R8(v, 24)
       : "r"(at));
+}
+// What is computed from loaded registers has to stay behind the wait: they pass through it.
+#define TSQ_RW8(v, i) "+r"(v[i]), "+r"(v[i + 1]), "+r"(v[i + 2]), "+r"(v[i + 3]), "+r"(v[i + 4]), "+r"(v[i + 5]), "+r"(v[i + 6]), "+r"(v[i + 7])
+__device__ __forceinline__ void tm_wait_ld(uint32_t (&v)[16]) { asm volatile("tcgen05.wait::ld.sync.aligned;" : TSQ_RW8(v, 0), TSQ_RW8(v, 8)::"memory"); }
+__device__ __forceinline__ void tm_wait_ld(uint32_t (&v)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : TSQ_RW8(v, 0), TSQ_RW8(v, 8)::"memory");
+  asm volatile("" : TSQ_RW8(v, 16), TSQ_RW8(v, 24)::"memory");
 }
 __device__ __forceinline__ void tm_load16(uint32_t (&v)[16], uint32_t at) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];" : TSQ_R8(v, 0), TSQ_R8(v, 8) : "r"(at));
@@ -470,7 +476,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
             uint32_t a[32], b[32], w[32];
             tm_load32(a, at_half);
             tm_load32(b, at_half + 32);
-            tm_wait_ld();
+            tm_wait_ld(a);
+            tm_wait_ld(b);
             float sum = 0.0f;
             // once a row has its reference its weights are formed at once, and again only if one of them came out above 2^8
             bool again = !settled;
@@ -496,7 +503,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                 for (int d = 0; d < D; d += 16) {
                   uint32_t o[16];
                   tm_load16(o, o_at + d);
-                  tm_wait_ld();
+                  tm_wait_ld(o);
 #pragma unroll
                   for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
                   tm_store16(o_at + d, o);
@@ -529,7 +536,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
         for (int d = 0; d < D; d += 32) {
           uint32_t o[32];
           tm_load32(o, o_at + d);
-          tm_wait_ld();
+          tm_wait_ld(o);
           if (live) {
 #pragma unroll
             for (int e = 0; e < 32; e += 8) {
@@ -553,7 +560,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
         for (int d = 0; d < D; d += 32) {
           uint32_t o[32];
           tm_load32(o, o_at + d);
-          tm_wait_ld();
+          tm_wait_ld(o);
 #pragma unroll
           for (int e = 0; e < 32; ++e) slot[128 * (2 + d + e)] = __uint_as_float(o[e]);
         }
@@ -567,33 +574,37 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
       if (lane == 0) done = atomicInc(p.counters + 8 * first + warp, static_cast<unsigned>(last - first));
       if (__shfl_sync(kFull, done, 0) == static_cast<unsigned>(last - first)) {
         __threadfence();
+        // two parts and 32 dimensions at a time, without a branch between the loads, so that all of them are on their way; behind the last part its data again, not counted
+        const auto part_at = [&](int n) { return p.partials + (4ll * min(n, last) + 2 * t + (min(n, last) == first ? 1 : 0)) * kSlot + row; };
         float top = -INFINITY, all = 0.0f;
-        for (int n = first; n <= last; ++n) {
-          const float* const part = p.partials + (4ll * n + 2 * t + (n == first ? 1 : 0)) * kSlot + row;
-          top = fmaxf(top, __ldcg(part));
-        }
-        for (int n = first; n <= last; ++n) {
-          const float* const part = p.partials + (4ll * n + 2 * t + (n == first ? 1 : 0)) * kSlot + row;
-          const float mine = __ldcg(part);
-          if (mine != -INFINITY) all = __fmaf_rn(__ldcg(part + 128), exp2_fast(mine - top), all);
-        }
-        const float by = all == 0.0f ? 0.0f : 1.0f / all;
+#pragma unroll 4
+        for (int n = first; n <= last; ++n) top = fmaxf(top, __ldcg(part_at(n)));
 #pragma unroll 1
-        for (int d = 0; d < D; d += 16) {
-          float o[16];
+        for (int d = 0; d < D; d += 32) {
+          float o[32];
+          all = 0.0f;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) o[e] = 0.0f;
-          for (int n = first; n <= last; ++n) {
-            const float* const part = p.partials + (4ll * n + 2 * t + (n == first ? 1 : 0)) * kSlot + row;
-            const float mine = __ldcg(part);
-            if (mine == -INFINITY) continue;
-            const float w = exp2_fast(mine - top);
+          for (int e = 0; e < 32; ++e) o[e] = 0.0f;
+#pragma unroll 1
+          for (int n = first; n <= last; n += 2) {
+            const float *const p0 = part_at(n), *const p1 = part_at(n + 1);
+            const float m0 = __ldcg(p0), m1 = n < last ? __ldcg(p1) : -INFINITY, l0 = __ldcg(p0 + 128), l1 = __ldcg(p1 + 128);
+            float x0[32], x1[32];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = __fmaf_rn(__ldcg(part + 128 * (2 + d + e)), w, o[e]);
+            for (int e = 0; e < 32; ++e) {
+              x0[e] = __ldcg(p0 + 128 * (2 + d + e));
+              x1[e] = __ldcg(p1 + 128 * (2 + d + e));
+            }
+            // a part of maximum -Inf has seen nothing: what stands in its slot does not count, whatever it is
+            const float w0 = m0 == -INFINITY ? 0.0f : exp2_fast(m0 - top), w1 = m1 == -INFINITY ? 0.0f : exp2_fast(m1 - top);
+            all += (m0 == -INFINITY ? 0.0f : l0 * w0) + (m1 == -INFINITY ? 0.0f : l1 * w1);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] += (m0 == -INFINITY ? 0.0f : x0[e] * w0) + (m1 == -INFINITY ? 0.0f : x1[e] * w1);
           }
+          const float by = all == 0.0f ? 0.0f : 1.0f / all;
           if (live) {
 #pragma unroll
-            for (int e = 0; e < 16; e += 8) {
+            for (int e = 0; e < 32; e += 8) {
               uint32_t w[4];
 #pragma unroll
               for (int k = 0; k < 4; ++k) w[k] = Elem<BF16>::pack_rn(o[e + 2 * k] * by, o[e + 2 * k + 1] * by);
