@@ -466,7 +466,11 @@ cudaError_t launch_store(const StoreParams& p, int shift, int grid, cudaStream_t
 }
 
 // Workspace: 16 bytes with the status, the counters of either kernel, the slots of sums.
-bool few_query_rows(long long max_query, int group) { return max_query * group <= kRowsTile; }
+// Which kernel: by the query rows that a key head's codes serve at most.  The row kernel reads the codes again for every 16 rows; the tile kernel takes
+// 256 at once, at a step's price whether they are there or not.  us, rows / tiles (bf16, heads of 128, codes in HBM): 16 requests of 8000 keys, 8 key heads,
+// 24 and 32 rows 119 / 158, 48 rows 170 / 158, 64 rows 213 / 158; 64 of 2000 keys 24 rows 123 / 176, 48 rows 176 / 178; 1 of 100000 keys 32 rows 113 / 158, 64 rows 180 / 160;
+// 16 of 3000 keys, 40 key heads, 20 rows 209 / 285, 40 rows 301 / 291.
+bool few_query_rows(long long max_query, int group) { return max_query * group <= kFewQueryRows; }
 size_t workspace_head(int sms) { return static_cast<size_t>(align16(16ull + 4ull * sms * std::max(kRowsCtasPerSm * kRowsCounters, kTilesCounters))); }
 size_t workspace_size(int sms, int head_dim, bool few) {
   const unsigned long long rows = few ? 1ull * kRowsCtasPerSm * kRowsSlots * kRowsTile : 128ull * kTilesSlots;
