@@ -37,7 +37,7 @@ __device__ __forceinline__ Request request_of(const AttentionParams& p, int i) {
   const long long length = max(p.lengths[i], 0);
   r.start = begin;
   r.rows = static_cast<int>(min(end - begin, static_cast<long long>(p.max_query)));
-  r.keys = static_cast<int>(min(length, static_cast<long long>(p.table_pages) << p.page_shift));
+  r.keys = static_cast<int>(min(min(length, static_cast<long long>(p.table_pages) << p.page_shift), 0x7ffff000ll));  // a step further stays an int
   r.before = length - (end - begin);
   return r;
 }

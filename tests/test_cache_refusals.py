@@ -80,6 +80,12 @@ def test_no_cache_and_no_place_for_the_answer():
     assert L.tsq_cache_workspace_init(None, 1 << 30, None) == L.tsq_cache_workspace_init(PTR + 8, 1 << 30, None) == INVALID
 
 
+def test_workspace_status_wants_a_workspace_and_a_place():
+    out = C.c_uint32(9)
+    assert B.lib().tsq_cache_workspace_status(None, C.byref(out), None) == B.lib().tsq_cache_workspace_status(PTR, None, None) == INVALID
+    assert B.lib().tsq_cache_workspace_status(PTR + 4, C.byref(out), None) == INVALID and out.value == 9
+
+
 def slots(page=16, held=PTR, added=PTR, requests=3, free=PTR, n_free=4, start=PTR, lengths=PTR, table=PTR, width=5, out=PTR, tokens=9, taken=PTR):
     return B.lib().tsq_cache_slots(page, held, added, requests, free, n_free, start, lengths, table, width, out, tokens, taken, None)
 

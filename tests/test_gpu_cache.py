@@ -125,6 +125,14 @@ def test_store_of_a_batch_of_single_tokens():
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16])
+def test_store_of_a_prompt_in_blocks(dtype):
+    # several tokens for each CTA: runs that begin and end anywhere in a CTA's block, and rows without a slot
+    s = Setup(dtype, [1500, 700], kv_heads=8, head_dim=128, page=32, seed=25)
+    slots = s.slots_of(0, 3, 1500) + [-1] * 5 + s.slots_of(1, 650, 700) + [-1]
+    check_store(s, s.rows(len(slots), 8), s.rows(len(slots), 8), slots)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
 def test_store_of_values_that_are_no_numbers_zeros_and_extremes(dtype):
     s = Setup(dtype, [48, 20], kv_heads=2, head_dim=64, page=16, seed=5)
     x = s.rows(68, 2)
@@ -324,6 +332,118 @@ def test_on_another_stream_and_in_graphs_that_share_a_workspace(added):
     s.cache.attention(q, starts, lengths, s.table, want, ws, added)
     torch.cuda.synchronize()
     assert torch.equal(outs[1], want)
+
+
+@pytest.mark.parametrize("D,P,H,group,held,added", [
+    (64, 16, 1, 2, [40000], [1]), (128, 64, 1, 1, [9000], [1]), (64, 32, 2, 5, [20000, 3], [3, 1]), (128, 128, 1, 8, [12000, 64, 1], [2, 1, 1]),      # up to 592 parts of a tile
+    (64, 64, 1, 1, [20000], [40]), (128, 16, 1, 5, [5000, 10], [30, 8]), (64, 128, 1, 64, [9000], [1]), (128, 32, 2, 3, [4000, 130], [100, 130])])
+def test_long_requests_whose_tiles_many_shares_have_parts_of(D, P, H, group, held, added):
+    check_attention(Setup(F16, held, H, D, P, seed=20), added, group)
+
+
+@pytest.mark.parametrize("group,most", [(1, 1), (4, 2), (2, 30)])
+def test_many_short_requests(group, most):
+    # more requests than a CTA has threads, some without a token, some without a row, at the ends too
+    r = random.Random(most)
+    n = 1500
+    held = [0] + [r.choice([0, 1, 2, 17, 40, 65, 200]) for _ in range(n - 2)] + [0]
+    added = [min(h, r.choice([0, 1, 1, most])) for h in held]
+    s = Setup(BF16, held, 1, 64, 16, seed=21)
+    starts = [0]
+    for a in added:
+        starts.append(starts[-1] + a)
+    q = s.rows(starts[-1] + 2, group, 1.5)
+    out = torch.full_like(q, 5.0)
+    ws = s.cache.workspace(q.shape[0], group, n, most)
+    s.cache.attention(q, s.ints(starts), s.ints(held), s.table, out, ws, most)
+    some = sorted(r.sample(range(n), 150))                              # the reference is slow: rows of 150 of them, and that every row is finite
+    for i in some:
+        part = Setup.__new__(Setup)
+        part.__dict__ = dict(s.__dict__, table=s.table[i:i + 1])
+        want, tol = attention_ref(part, q[starts[i]:starts[i + 1]], [0, added[i]], [held[i]], 64 ** -0.5)
+        assert bool(((out[starts[i]:starts[i + 1]].double().cpu() - want).abs() <= tol).all()), i
+    assert bool(out.isfinite().all()) and bool((out[starts[-1]:] == 5.0).all()) and s.cache.workspace_status(ws) == 0
+
+
+@pytest.mark.parametrize("added", [1, 50])
+def test_two_calls_at_once(added):
+    """Two streams, a workspace each: calls that may run at the same time, on whatever part of the GPU the other leaves."""
+    held = [3000, 700, 90]
+    s = Setup(F16, held, 2, 64 if added == 1 else 128, 32, seed=22)
+    T = 3 * added
+    starts, lengths = s.ints([0, added, 2 * added, T]), s.ints(held)
+    qs = [s.rows(T, 8) for _ in range(2)]
+    wss = [s.cache.workspace(T, 8, 3, added) for _ in range(2)]
+    want, got, streams = [], [], [torch.cuda.Stream() for _ in range(2)]
+    for q, ws in zip(qs, wss):
+        o = torch.zeros_like(q)
+        s.cache.attention(q, starts, lengths, s.table, o, ws, added)
+        want.append(o)
+        got.append([torch.zeros_like(q) for _ in range(6)])
+    torch.cuda.synchronize()
+    for k in range(6):
+        for q, ws, o, st in zip(qs, wss, got, streams):
+            s.cache.attention(q, starts, lengths, s.table, o[k], ws, added, stream=st)
+    torch.cuda.synchronize()
+    for w, o in zip(want, got):
+        assert all(torch.equal(x, w) for x in o)
+    assert [s.cache.workspace_status(ws) for ws in wss] == [0, 0]
+
+
+def test_one_workspace_for_calls_of_either_kind_in_turn():
+    held = [2000, 300]
+    s = Setup(BF16, held, 1, 64, 16, seed=23)
+    ws = s.cache.workspace(400, 4, 2, 200)                              # the larger of the two
+    for added in (1, 200, 3, 100, 1):
+        q = s.rows(2 * added, 4)
+        args = (q, s.ints([0, added, 2 * added]), s.ints(held), s.table)
+        out, want = torch.zeros_like(q), torch.zeros_like(q)
+        s.cache.attention(*args, out, ws, added)
+        s.cache.attention(*args, want, s.cache.workspace(2 * added, 4, 2, added), added)
+        assert torch.equal(out, want)
+
+
+def test_refusals_through_the_binding():
+    s = Setup(F16, [40], 2, 64, 16, seed=24)
+    q, out = s.rows(1, 4), s.rows(1, 4)
+    args = (s.ints([0, 1]), s.ints([40]), s.table)
+    ws = s.cache.workspace(1, 4, 1, 1)
+    for bad in (dict(q=q.to(BF16)), dict(q=q[..., :32]), dict(q=q.cpu()), dict(out=out[:, :2]), dict(ws=ws.view(torch.int32)), dict(max_query="x")):
+        a = dict(q=q, out=out, ws=ws, max_query=1)
+        a.update(bad)
+        with pytest.raises((AssertionError, TypeError)):
+            s.cache.attention(a["q"], *args, a["out"], a["ws"], a["max_query"])
+    for bad in (dict(ws=ws[:-16]), dict(max_query=0), dict(scale=math.nan)):
+        a = dict(ws=ws, max_query=1, scale=None)
+        a.update(bad)
+        with pytest.raises(B.TsqError):
+            s.cache.attention(q, *args, out, a["ws"], a["max_query"], scale=a["scale"])
+    with pytest.raises(B.TsqError):                                     # five query heads for two key heads
+        s.cache.attention(s.rows(1, 5), *args, s.rows(1, 5), ws, 1)
+    with pytest.raises(AssertionError):
+        s.cache.store(s.rows(3, 2), s.rows(3, 2), s.ints([1, 2]))
+    with pytest.raises(AssertionError):
+        s.cache.load(s.ints([[1], [2]]), s.rows(2, 2), s.rows(2, 2))
+    with pytest.raises(AssertionError):
+        B.cache_slots(16, s.ints([1, 2]), s.ints([1]), s.free, s.ints([0, 0, 0]), s.ints([0, 0]), s.ints([[0], [0]]), s.ints([0, 0]), s.ints([0]))
+    with pytest.raises(AssertionError):
+        B.Cache(F16, s.k_codes, s.v_codes[:1], s.k_scale, s.v_scale)
+
+
+def test_arrays_that_begin_anywhere():
+    # slots, tables and lengths are only aligned to their four bytes
+    whole = [torch.full((n + 1,), -9, dtype=torch.int32, device="cuda") for n in (4, 3, 21, 300, 1)]
+    start, lengths, table, slots, taken = (w[1:] for w in whole)
+    table = table.view(3, 7)
+    held, added = [5, 0, 30], [100, 64, 1]
+    free = torch.arange(50, 80, dtype=torch.int32, device="cuda")[1:]
+    ints = lambda v: torch.tensor([0] + v, dtype=torch.int32, device="cuda")[1:]  # noqa: E731
+    first = [[3] + [-9] * 6, [-9] * 7, [1, 2] + [-9] * 5]
+    table.copy_(torch.tensor(first))
+    B.cache_slots(16, ints(held), ints(added), free, start, lengths, table, slots, taken)
+    want = slots_ref(16, held, added, free.cpu().tolist(), first, 300)
+    assert [start.tolist(), lengths.tolist(), table.tolist(), slots.tolist(), int(taken)] == list(want)
+    assert all(int(w[0]) == -9 for w in whole)
 
 
 @pytest.mark.parametrize("added", [1, 20])
