@@ -132,9 +132,9 @@ __device__ __forceinline__ float top_score(const uint32_t (&scores)[32], uint32_
   }
   return most;
 }
-// Weights of 64 keys in binary16, two to a word; returns their sum over the values' scale.
+// Weights of 64 keys in binary16, two to a word; returns their sum over the values' scale.  most: the largest sum of a granule's weights, and so no less than any weight.
 template <bool MASK>
-__device__ __forceinline__ void weights_of_32(const uint32_t (&s)[32], uint32_t* w, uint32_t scales, float by_scale, float m, float& l, int left) {
+__device__ __forceinline__ void weights_of_32(const uint32_t (&s)[32], uint32_t* w, uint32_t scales, float by_scale, float m, float& l, float& most, int left) {
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
     const float4 f = shared_float4(scales + 16 * g);
@@ -156,21 +156,18 @@ __device__ __forceinline__ void weights_of_32(const uint32_t (&s)[32], uint32_t*
     }
     float even, odd;
     unpack2f(sum, even, odd);
+    most = fmaxf(most, even + odd);
     l = __fmaf_rn(even + odd, f.z, l);
   }
 }
 template <bool MASK>
-__device__ __forceinline__ float weights_of(const uint32_t (&a)[32], const uint32_t (&b)[32], uint32_t (&w)[32], uint32_t scales, float by_scale, float m, int left) {
+__device__ __forceinline__ float weights_of(const uint32_t (&a)[32], const uint32_t (&b)[32], uint32_t (&w)[32], uint32_t scales, float by_scale, float m, float& most,
+                                            int left) {
   float sum = 0.0f;
-  weights_of_32<MASK>(a, w, scales, by_scale, m, sum, left);
-  weights_of_32<MASK>(b, w + 16, scales + 32, by_scale, m, sum, left - 32);
+  most = 0.0f;
+  weights_of_32<MASK>(a, w, scales, by_scale, m, sum, most, left);
+  weights_of_32<MASK>(b, w + 16, scales + 32, by_scale, m, sum, most, left - 32);
   return sum;
-}
-__device__ __forceinline__ float top_weight(const uint32_t (&w)[32]) {
-  __half2 t = Elem<false>::as2(w[0]);
-#pragma unroll
-  for (int e = 1; e < 32; ++e) t = __hmax2(t, Elem<false>::as2(w[e]));
-  return fmaxf(__low2float(t), __high2float(t));
 }
 
 // Shared-memory descriptors of 128-byte swizzled operands: rows of 128 bytes, eight rows to a 1024-byte atom.
@@ -283,8 +280,8 @@ __host__ __device__ constexpr uint32_t arrivals_of(int bar) {  // a group's warp
 //   product warps   one for each group: S = Q K^T into tensor memory, then O += P V with P from tensor memory
 //   softmax groups  S out of tensor memory, w = 2^(S * scale + log2 s_v - m) to binary16 in S's place, sums in binary32
 // Scores come in halves of 64 keys, each with its place in tensor memory: while a group works on one, its products fill the other, and the other group's run besides.
-// m is a reference that follows the row's maximum only when a
-// score is more than 2^8 above it: then the step is done again and O is scaled in tensor memory.  Every CTA takes the same number of steps whatever the requests'
+// m is a reference that follows the row's maximum only when
+// weights come out above 2^12: then the half is done again and O is scaled in tensor memory.  Every CTA takes the same number of steps whatever the requests'
 // lengths are; tiles that several CTAs have a part of are added up through the workspace by the one that comes last, in the order of the steps.
 // Bound by the exponentials and by what surrounds them: 16 of them per SM and clock are 1024 clocks for a group's step, as long as its two products take.
 template <bool BF16, int D>
@@ -490,12 +487,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
             tm_load32(b, at_half + 32);
             tm_wait_ld(a);
             tm_wait_ld(b);
-            float sum = 0.0f;
-            // once a row has its reference its weights are formed at once, and again only if one of them came out above 2^8
+            float sum = 0.0f, most_weight = 0.0f;
+            // once a row has its reference its weights are formed at once, and again only if sixteen neighbours' sum came out above 2^12: no weight is above that in
+            // binary16, which goes to 65504
             bool again = !settled;
             if (settled) {
-              sum = mask ? weights_of<true>(a, b, w, factors, by_scale, m, left) : weights_of<false>(a, b, w, factors, by_scale, m, 64);
-              again = __any_sync(kFull, top_weight(w) > 256.0f);
+              sum = mask ? weights_of<true>(a, b, w, factors, by_scale, m, most_weight, left) : weights_of<false>(a, b, w, factors, by_scale, m, most_weight, 64);
+              again = __any_sync(kFull, most_weight > 4096.0f);
             }
             if (again) {
               const float most = mask ? fmaxf(top_score<true>(a, factors, by_scale, left), top_score<true>(b, factors + 32, by_scale, left - 32))
@@ -521,7 +519,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                   tm_store16(o_at + d, o);
                 }
               }
-              sum = weights_of<true>(a, b, w, factors, by_scale, m, mask ? left : 64);
+              sum = weights_of<true>(a, b, w, factors, by_scale, m, most_weight, mask ? left : 64);
             }
             l += sum;
             tm_store32(at_half, w);                        // in the place of scores, which have all been read
@@ -644,31 +642,27 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
     uint32_t n = 0;                                        // steps so far
     uint4 raw[kItems];
     float4 scale = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    // pages of the next step's granules; -1 where there is none
-    int pages[kItems], scale_page = -1;
-    auto page_at = [&](int j, int granule) {
-      const int token = j * kKeys + 16 * granule;
-      if (token >= place.r.keys) return -1;
-      return p.table[static_cast<long long>(place.request) * p.table_pages + (token >> p.page_shift)];
-    };
+    // lane g has the page of granule g of the next step, -1 where there is none; the others have its offset from there
+    int page = -1;
+    const int8_t* const from = codes + (token0 % 16) * D + chunk * 16;
     auto fetch_pages = [&](int j) {
-#pragma unroll
-      for (int it = 0; it < kItems; ++it) pages[it] = page_at(j, (token0 + it * (128 / kChunks)) / 16);
-      if (has_scale) scale_page = page_at(j, in_group);
+      const int token = j * kKeys + 16 * lane;
+      page = -1;
+      if (lane < kGranules && token < place.r.keys) page = p.table[static_cast<long long>(place.request) * p.table_pages + (token >> p.page_shift)];
     };
     auto fetch = [&](int j) {
+      const bool there = static_cast<unsigned>(page) < static_cast<unsigned>(p.pages);
+      const long long page_head = static_cast<long long>(page) * p.kv_heads + place.head;
+      const long long at = there ? ((page_head << p.page_shift) + ((j * kKeys + 16 * lane) & ((1 << p.page_shift) - 1))) * D : -1;
 #pragma unroll
       for (int it = 0; it < kItems; ++it) {
-        const int token = j * kKeys + token0 + it * (128 / kChunks);
+        const long long off = __shfl_sync(kFull, at, D == 128 ? it : 2 * it + w / 2);
         raw[it] = make_uint4(0u, 0u, 0u, 0u);
-        if (static_cast<unsigned>(pages[it]) < static_cast<unsigned>(p.pages))
-          raw[it] = *(reinterpret_cast<const uint4*>(codes + (((static_cast<long long>(pages[it]) * p.kv_heads + place.head) << p.page_shift) +
-                                                              (token & ((1 << p.page_shift) - 1))) * D) + chunk);
+        if (off >= 0) raw[it] = *reinterpret_cast<const uint4*>(from + off);
       }
       if (has_scale) {
         scale = make_float4(0.0f, -INFINITY, 0.0f, 0.0f);  // nothing of a page that is not there is seen
-        if (static_cast<unsigned>(scale_page) < static_cast<unsigned>(p.pages)) {
-          const long long page_head = static_cast<long long>(scale_page) * p.kv_heads + place.head;
+        if (there) {
           const float vs = fmaxf(p.v_scale[page_head], kLeastScale);
           scale = make_float4(p.k_scale[page_head], __log2f(vs), 1.0f / vs, 0.0f);
         }
