@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(kSlotThreads) slots_kernel(const SlotParams p)
 
 // ---- quantising into the cache -------------------------------------------------------------------
 
-constexpr int kStoreItems = 4;            // 16-byte chunks of a thread
+constexpr int kStoreItems = 8;            // 16-byte chunks of a thread
 __host__ __device__ constexpr int store_threads(int d, int page) { return d * page / (8 * kStoreItems) > 64 ? d * page / (8 * kStoreItems) : 64; }
 constexpr int kStoreBlock = 64;           // most tokens whose runs one CTA looks after
 constexpr float kScaleFloor = 9.094947017729282e-13f;  // 2^-40
