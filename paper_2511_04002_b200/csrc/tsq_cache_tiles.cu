@@ -13,7 +13,7 @@ constexpr int kGranules = kKeys / 16;        // parts of a step that lie within 
 constexpr int kThreads = 5 * 128;            // two softmax warpgroups, two that widen codes, one whose first two warps issue the products
 // Registers: 96 a thread at launch, dealt out again among the five: 2 * 136 + 2 * 80 + 48 = 5 * 96.
 constexpr int kSoftmaxRegs = 136, kWidenRegs = 80, kProductRegs = 48, kLaunchRegs = 96;
-constexpr int kTileSteps = 3;                // what beginning and ending a tile costs, in steps
+constexpr int kTileSteps = 4;                // what beginning and ending a tile costs, in steps
 // Most parts of a tile, on the average: adding a part up takes 1.7 us, a step 2.3 us (one tile of 235 steps in 148 parts 300 us, in 16 80 us).
 constexpr unsigned long long kMostParts = 16;
 constexpr int kMeta = 4;                     // steps whose scales are kept
