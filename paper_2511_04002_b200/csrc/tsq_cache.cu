@@ -511,8 +511,11 @@ tsq_status_t tsq_cache_slots(int32_t page_tokens, const int32_t* held, const int
   p.table_pages = table_pages;
   p.page_shift = page_shift(page_tokens);
   const size_t smem = 4ull * (2ull * static_cast<size_t>(requests) + 1ull);
-  if (smem > 48 * 1024 && cudaFuncSetAttribute(slots_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
-    return launched(cudaErrorInvalidValue);
+  static std::atomic<unsigned long long> done{0};
+  if (smem > 48 * 1024) {
+    const cudaError_t e = allow_shared(slots_kernel, 4 * (2 * kMaxRequests + 1), done);
+    if (e != cudaSuccess) return launched(e);
+  }
   const int grid = tokens > 0 ? static_cast<int>((tokens + kSlotTokens - 1) / kSlotTokens) : 1;
   return launched(launch_overlapped(slots_kernel, grid, kSlotThreads, smem, static_cast<cudaStream_t>(cuda_stream), p));
 }

@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "tsq.h"
 
 namespace tsq {
@@ -12,6 +14,19 @@ namespace tsq {
 void count_launch();  // tsq_kernel_launch_count
 
 constexpr int kMaxRequests = 8192;
+
+// Lets a kernel have so much dynamic shared memory on the current device; asked for once per kernel and device (`done`: a bit for each of the first 64).
+template <typename K>
+cudaError_t allow_shared(K kernel, int bytes, std::atomic<unsigned long long>& done) {
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = device >= 0 && device < 64 ? 1ull << device : 0ull;
+  if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
 
 struct AttentionParams {
   const void* q;

@@ -535,7 +535,8 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
 template <bool BF16, int D, int NT>
 cudaError_t launch(const AttentionParams& p, int sms, cudaStream_t stream) {
   using L = Layout<D, NT>;
-  const cudaError_t e = cudaFuncSetAttribute(attention_rows_kernel<BF16, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
+  static std::atomic<unsigned long long> done{0};
+  const cudaError_t e = allow_shared(attention_rows_kernel<BF16, D, NT>, L::kBytes, done);
   if (e != cudaSuccess) return e;
   return launch_overlapped(attention_rows_kernel<BF16, D, NT>, sms * L::kCtasPerSm, kThreads, static_cast<size_t>(L::kBytes), stream, p);
 }

@@ -784,7 +784,8 @@ template <bool BF16, int D>
 cudaError_t launch(const AttentionParams& p, int ctas, cudaStream_t stream) {
   constexpr int bytes = Shared<D>::kBytes + 1024;
   static_assert(Shared<D>::kScales >= 8 * kMaxRequests, "the unit counts fit in front of the scales");
-  const cudaError_t e = cudaFuncSetAttribute(attention_tiles_kernel<BF16, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  static std::atomic<unsigned long long> done{0};
+  const cudaError_t e = allow_shared(attention_tiles_kernel<BF16, D>, bytes, done);
   if (e != cudaSuccess) return e;
   return launch_overlapped(attention_tiles_kernel<BF16, D>, ctas, kThreads, bytes, stream, p);
 }

@@ -226,6 +226,24 @@ def test_pages_outside_the_cache_are_not_seen(added):
 
 
 @pytest.mark.parametrize("added", [1, 40])
+def test_a_table_without_entries(added):
+    s = Setup(F16, [100], 1, 64, 16, seed=26)
+    q = s.rows(added, 2)
+    out = torch.full_like(q, 5.0)
+    s.cache.attention(q, s.ints([0, added]), s.ints([100]), s.table[:, :0].contiguous(), out, s.cache.workspace(added, 2, 1, added), added)
+    assert bool((out == 0).all())
+
+
+def test_slots_of_the_most_requests():
+    n = 8192
+    held, added = [i * 7 % 50 for i in range(n)], [i * 5 % 3 for i in range(n)]
+    need = sum((h + a + 15) // 16 - (h + 15) // 16 for h, a in zip(held, added))
+    free, table = list(range(70000, 70000 + need)), [[9 * i + e if 16 * e < held[i] else -5 for e in range(4)] for i in range(n)]
+    got, want = run_slots(16, held, added, free, table, sum(added) + 1), slots_ref(16, held, added, free, table, sum(added) + 1)
+    assert [got[0], got[1], got[2], got[3], got[4][0]] == list(want)
+
+
+@pytest.mark.parametrize("added", [1, 40])
 def test_lengths_past_the_table_end_with_it(added):
     s = Setup(F16, [100, 64], 1, 64, 16, seed=10)
     table = s.table[:, :5].contiguous()
