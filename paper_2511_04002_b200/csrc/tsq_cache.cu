@@ -185,6 +185,12 @@ __device__ __forceinline__ uint32_t codes_of(uint64_t x01, uint64_t x23) {
   return __byte_perm(__byte_perm(t0, t1, 0x0040), __byte_perm(t2, t3, 0x0040), 0x5410);
 }
 
+// The larger magnitudes of two packed pairs as patterns; NaN if there is one, and with it above every number's pattern.  a holds magnitudes.
+template <bool BF16>
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+  return Elem<BF16>::bits(__hmax2_nan(Elem<BF16>::as2(a), __habs2(Elem<BF16>::as2(b))));
+}
+
 // One CTA per head, keys or values, and block of tokens: for every run (tokens of one page) that begins in the block, the run's rows are read once into
 // registers, the largest finite |x| is reduced on the 15-bit patterns, and the codes are formed from the registers.  The rows of the block are read while
 // the slots are still on their way; a run that begins with the block, the usual one, then only needs the rows past it.  A page that was begun earlier has its codes
@@ -248,10 +254,10 @@ __global__ void __launch_bounds__(store_threads(D, P)) store_kernel(const StoreP
       uint32_t pair = 0u;                                              // largest 15-bit patterns of the lower and the upper halves
 #pragma unroll
       for (int it = 0; it < kItems; ++it) {
-        if ((it * kStoreThreads + tid) / kRowChunks >= n) v[it] = make_uint4(0u, 0u, 0u, 0u);
-        pair = __vmaxu2(__vmaxu2(pair, v[it].x & 0x7fff7fffu), __vmaxu2(v[it].y & 0x7fff7fffu, __vmaxu2(v[it].z & 0x7fff7fffu, v[it].w & 0x7fff7fffu)));
+        if (it * kStoreThreads + tid >= n * kRowChunks) v[it] = make_uint4(0u, 0u, 0u, 0u);
+        pair = larger<BF16>(larger<BF16>(larger<BF16>(larger<BF16>(pair, v[it].x), v[it].y), v[it].z), v[it].w);
       }
-      uint32_t top = max(pair & 0xffffu, pair >> 16);
+      uint32_t top = max(pair & 0x7fffu, (pair >> 16) & 0x7fffu);
       const bool finite = top < Elem<BF16>::kInfPattern;               // this thread's values
       if (!finite) {
         top = 0u;
@@ -356,48 +362,52 @@ __global__ void __launch_bounds__(kLoadThreads) load_kernel(const LoadParams p) 
   const long long t0 = static_cast<long long>(blockIdx.x) * p.block;
   const int tokens = static_cast<int>(min(static_cast<long long>(p.block), p.tokens - t0));
   const int mine = static_cast<int>(threadIdx.x) / all;                    // 0 where a token's chunks are more than the threads
+  const uint32_t page_bytes = static_cast<uint32_t>(p.heads << p.page_shift) * D;  // of the keys' codes; below 2^24
+  const int place_mask = (1 << p.page_shift) - 1;
   wait_for_prior_grids();
   if (mine >= together) return;
   for (int chunk = static_cast<int>(threadIdx.x) - mine * all; chunk < all; chunk += kLoadThreads) {
     const bool values = chunk >= row;
     const int of_row = values ? chunk - row : chunk, head = of_row / (D / 8);
-    const int8_t* const codes = (values ? p.v_codes : p.k_codes) + (of_row % (D / 8)) * 8;
+    const int8_t* const codes = (values ? p.v_codes : p.k_codes) + (static_cast<long long>(head) << p.page_shift) * D + (of_row % (D / 8)) * 8;
     const float* const scales = (values ? p.v_scale : p.k_scale) + head;
-    const long long stride = values ? p.v_stride : p.k_stride;
-    uint16_t* const to = (values ? p.v : p.k) + t0 * stride + of_row * 8;
-    for (int first = mine; first < tokens; first += kLoadItems * together) {
+    const long long stride = (values ? p.v_stride : p.k_stride) * together;  // from one of the thread's tokens to the next
+    uint16_t* to = (values ? p.v : p.k) + (t0 + mine) * (values ? p.v_stride : p.k_stride) + of_row * 8;
+    const int32_t* slots = p.slots + t0 + mine;
+    for (int left = tokens - mine; left > 0; left -= kLoadItems * together) {
       uint32_t slot[kLoadItems];
       uint2 code[kLoadItems];
       float scale[kLoadItems];
 #pragma unroll
       for (int n = 0; n < kLoadItems; ++n) {
-        const int t = first + n * together;
-        slot[n] = t < tokens ? static_cast<uint32_t>(p.slots[t0 + t]) : 0xffffffffu;
+        slot[n] = n * together < left ? static_cast<uint32_t>(*slots) : 0xffffffffu;
+        slots += together;
       }
 #pragma unroll
       for (int n = 0; n < kLoadItems; ++n) {
-        code[n] = make_uint2(0u, 0u);
+        code[n] = make_uint2(0x80808080u, 0x80808080u);   // code 0, sign bit inverted
         scale[n] = 0.0f;
         if (slot[n] < p.n_slots) {
-          const long long page = static_cast<long long>(slot[n] >> p.page_shift) * p.heads;
-          code[n] = __ldcs(reinterpret_cast<const uint2*>(codes + (((page + head) << p.page_shift) + (slot[n] & ((1u << p.page_shift) - 1u))) * D));
-          scale[n] = scales[page];
+          const uint32_t page = slot[n] >> p.page_shift;
+          code[n] = __ldcs(reinterpret_cast<const uint2*>(codes + static_cast<unsigned long long>(page) * page_bytes + (slot[n] & place_mask) * D));
+          code[n].x ^= 0x80808080u;
+          code[n].y ^= 0x80808080u;
+          scale[n] = scales[static_cast<unsigned long long>(page) * static_cast<uint32_t>(p.heads)];
         }
       }
 #pragma unroll
       for (int n = 0; n < kLoadItems; ++n) {
-        const int t = first + n * together;
-        if (t >= tokens) break;
-        const uint32_t w[2] = {code[n].x ^ 0x80808080u, code[n].y ^ 0x80808080u};
+        if (n * together >= left) break;
         uint32_t out[4];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           float x[4];
-          widen4(w[k], scale[n], x);
+          widen4(k == 0 ? code[n].x : code[n].y, scale[n], x);
           out[2 * k] = Elem<BF16>::pack_rn(x[0], x[1]);
           out[2 * k + 1] = Elem<BF16>::pack_rn(x[2], x[3]);
         }
-        __stcs(reinterpret_cast<uint4*>(to + t * stride), make_uint4(out[0], out[1], out[2], out[3]));
+        __stcs(reinterpret_cast<uint4*>(to), make_uint4(out[0], out[1], out[2], out[3]));
+        to += stride;
       }
     }
   }
