@@ -156,6 +156,24 @@ def test_rows_of_a_wider_tensor():
     assert torch.equal(k[:, 3:5], want) and torch.equal(k[:, :3], before[:, :3]) and torch.equal(k[:, 5:], before[:, 5:])
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_rows_that_begin_between_32_byte_boundaries(D):
+    s = Setup(BF16, [90], kv_heads=3, head_dim=D, page=16, seed=27)
+    slots = s.slots_of(0, 0, 90)
+    one, two = (torch.zeros(90 * 3 * D + 16, dtype=BF16, device="cuda") for _ in range(2))
+    k, v = one[8:8 + 90 * 3 * D].view(90, 3, D), two[16:].view(90, 3, D)
+    want_k, want_v = torch.zeros_like(k), torch.zeros_like(v)
+    s.cache.load(s.ints(slots), want_k.contiguous(), want_v)
+    x = s.rows(90, 3)
+    k.copy_(x)
+    check_store(s, k, x, slots)
+    s.cache.load(s.ints(slots), k, v)
+    at = s.ints(slots).long()
+    for got, codes, scale in ((k, s.k_codes, s.k_scale), (v, s.v_codes, s.v_scale)):
+        assert torch.equal(got, (codes[at // s.P, :, at % s.P].float() * scale[at // s.P][..., None]).to(BF16))
+    assert bool((one[:8] == 0).all()) and bool((one[8 + 90 * 3 * D:] == 0).all()) and bool((two[:16] == 0).all())
+
+
 # ---- attention ----
 
 def check_attention(s, added, group, scale=None, lengths=None, table=None, q=None, pad=3, max_query=None, **kw):
