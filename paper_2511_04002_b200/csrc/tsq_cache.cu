@@ -622,7 +622,8 @@ static tsq_status_t check_attention_sizes(const tsq_cache_t* cache, int64_t toke
   const tsq_status_t fine = check_cache(cache);
   if (fine != TSQ_OK) return fine;
   if (tokens < 0 || tokens > kMaxSlots || requests < 0 || max_query < 1 || q_heads < 1 || q_heads % cache->kv_heads != 0) return TSQ_ERR_INVALID_ARG;
-  return q_heads / cache->kv_heads > 64 || requests > kMaxRequests ? TSQ_ERR_UNSUPPORTED : TSQ_OK;
+  const int group = q_heads / cache->kv_heads;
+  return group > 64 || requests > kMaxRequests || tokens * group > kMaxSlots ? TSQ_ERR_UNSUPPORTED : TSQ_OK;
 }
 
 tsq_status_t tsq_cache_workspace(const tsq_cache_t* cache, int64_t tokens, int32_t q_heads, int32_t requests, int32_t max_query, size_t* workspace_bytes) {

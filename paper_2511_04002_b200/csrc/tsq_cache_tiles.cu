@@ -170,6 +170,21 @@ __device__ __forceinline__ float weights_of(const uint32_t (&a)[32], const uint3
   return sum;
 }
 
+// 32 bytes at once where they are a sector, which neighbouring threads' rows do not share.
+__device__ __forceinline__ void load_sector(uint4& a, uint4& b, const void* at) {
+  asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w)
+               : "l"(at));
+}
+__device__ __forceinline__ void store_sector(void* at, const uint32_t (&w)[8], bool whole) {
+  if (whole) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(at), TSQ_W8(w, 0) : "memory");
+  } else {
+    static_cast<uint4*>(at)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    static_cast<uint4*>(at)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+}
+
 // Shared-memory descriptors of 128-byte swizzled operands: rows of 128 bytes, eight rows to a 1024-byte atom.
 // K-major (queries, keys): atoms follow one another down the rows.  MN-major (values: a row is a token, its 64 dimensions contiguous): atoms follow
 // one another along the tokens, the second 64 dimensions lie kHalf bytes behind.
@@ -205,8 +220,8 @@ __device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(kFu
 // ---- work ----------------------------------------------------------------------------------------
 
 // Steps of the tile of 256 rows that begins at row0: by the keys its last row sees, one at least.
-__device__ __forceinline__ int steps_of(const Request& r, long long rows, long long row0, const AttentionParams& p) {
-  const int seen = r.seen(static_cast<int>((min(rows, row0 + kTilesRows) - 1) / p.group));
+__device__ __forceinline__ int steps_of(const Request& r, uint32_t rows, uint32_t row0, const AttentionParams& p) {
+  const int seen = r.seen(static_cast<int>((min(rows, row0 + kTilesRows) - 1u) / static_cast<uint32_t>(p.group)));
   return seen > 0 ? (seen - 1) / kKeys + 1 : 1;
 }
 
@@ -215,7 +230,7 @@ __device__ __forceinline__ int steps_of(const Request& r, long long rows, long l
 struct Place {
   int request, head, tile;
   Request r;
-  long long rows;                 // rows of the request times the group
+  uint32_t rows;                  // rows of the request times the group, below 2^31 (tsq_cache_attention)
   int steps;                      // of the tile
   int from, upto;                 // units that the CTA takes of it,
   int k0, k1;                     // and steps
@@ -223,7 +238,7 @@ struct Place {
   unsigned long long unit, end;   // the first unit; where the CTA's share ends
 
   __device__ __forceinline__ void take(const AttentionParams& p) {
-    steps = steps_of(r, rows, static_cast<long long>(tile) * kTilesRows, p);
+    steps = steps_of(r, rows, static_cast<uint32_t>(tile) * kTilesRows, p);
     upto = static_cast<int>(min(static_cast<unsigned long long>(steps + kTileSteps), from + (end - unit)));
     k0 = max(0, from - kTileSteps);
     k1 = max(0, upto - kTileSteps);
@@ -235,7 +250,7 @@ struct Place {
       before += k1 - k0;
       if (unit >= end) return false;
       from = 0;
-      if (static_cast<long long>(++tile) * kTilesRows >= rows) {
+      if (static_cast<uint32_t>(++tile) * kTilesRows >= rows) {
         tile = 0;
         if (++head == p.kv_heads) {
           head = 0;
@@ -243,7 +258,7 @@ struct Place {
             if (++request >= p.requests) return false;
             r = request_of(p, request);
           } while (r.rows == 0);
-          rows = static_cast<long long>(r.rows) * p.group;
+          rows = static_cast<uint32_t>(r.rows) * static_cast<uint32_t>(p.group);
         }
       }
       take(p);
@@ -252,9 +267,9 @@ struct Place {
   }
   // steps of the half of the tile (128 rows) that group t has: as far as its last row sees, 0 where it has no row
   __device__ __forceinline__ int limit(int t, const AttentionParams& p) const {
-    const long long row0 = static_cast<long long>(tile) * kTilesRows + 128 * t;
+    const uint32_t row0 = static_cast<uint32_t>(tile) * kTilesRows + 128u * t;
     if (row0 >= rows) return 0;
-    const int seen = r.seen(static_cast<int>((min(rows, row0 + 128) - 1) / p.group));
+    const int seen = r.seen(static_cast<int>((min(rows, row0 + 128u) - 1u) / static_cast<uint32_t>(p.group)));
     return min(k1, seen > 0 ? (seen - 1) / kKeys + 1 : 1);
   }
 };
@@ -302,9 +317,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
   unsigned long long* const s_units = reinterpret_cast<unsigned long long*>(smem_at);
   for (int i = warp; i < p.requests; i += kThreads / 32) {
     const Request r = request_of(p, i);
-    const long long rows = static_cast<long long>(r.rows) * p.group;
+    const uint32_t rows = static_cast<uint32_t>(r.rows) * static_cast<uint32_t>(p.group);
     unsigned long long sum = 0;
-    for (long long row0 = static_cast<long long>(lane) * kTilesRows; row0 < rows; row0 += 32ll * kTilesRows) sum += steps_of(r, rows, row0, p) + kTileSteps;
+    for (uint32_t row0 = static_cast<uint32_t>(lane) * kTilesRows; row0 < rows; row0 += 32u * kTilesRows) sum += steps_of(r, rows, row0, p) + kTileSteps;
 #pragma unroll
     for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(kFull, sum, d);
     if (lane == 0) s_units[i] = sum;                       // of one key head
@@ -369,14 +384,14 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
   {
     place.request = s_found;
     place.r = request_of(p, place.request);
-    place.rows = static_cast<long long>(place.r.rows) * p.group;
+    place.rows = static_cast<uint32_t>(place.r.rows) * static_cast<uint32_t>(p.group);
     const unsigned long long of_head = s_units[place.request], in = place.unit - s_begin;
     place.head = static_cast<int>(in / of_head);
     unsigned long long rest = in % of_head;                // steps of this head's tiles in front of `unit`
     // every warp by itself: 32 tiles at a time
     int tile = 0;
     for (;;) {
-      const long long row0 = static_cast<long long>(tile + lane) * kTilesRows;
+      const uint32_t row0 = static_cast<uint32_t>(tile + lane) * kTilesRows;
       const int n = row0 < place.rows ? steps_of(place.r, place.rows, row0, p) + kTileSteps : 0;
       int upto = n;
 #pragma unroll
@@ -393,7 +408,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
       }
       rest -= __shfl_sync(kFull, upto, 31);
       tile += 32;
-      if (static_cast<long long>(tile) * kTilesRows >= place.rows) {  // not reached: the request has the unit
+      if (static_cast<uint32_t>(tile) * kTilesRows >= place.rows) {  // not reached: the request has the unit
         tile = 0;
         rest = 0;
         break;
@@ -427,19 +442,31 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
     const uint32_t lanes = static_cast<uint32_t>(warp % 4) << 21;  // lane 32 * (warp % 4) in the upper half of an address
     const uint32_t s_at = tmem + lanes + 128 * t, o_at = tmem + lanes + 256 + D * t;
     uint32_t count = 0;                                    // steps of this group so far
+    const uint32_t group = static_cast<uint32_t>(p.group);
+    // whether rows lie on 32-byte boundaries
+    const bool q_sectors = ((reinterpret_cast<uintptr_t>(p.q) | static_cast<uintptr_t>(2 * p.q_stride)) & 31u) == 0;
+    const bool out_sectors = ((reinterpret_cast<uintptr_t>(p.out) | static_cast<uintptr_t>(2 * p.out_stride)) & 31u) == 0;
     // the thread's row of a tile, brought to binary16 by a power of two; the inverse is returned
     auto load_query = [&](const Place& at) {
-      const long long row0 = static_cast<long long>(at.tile) * kTilesRows + 128 * t;
+      const uint32_t row0 = static_cast<uint32_t>(at.tile) * kTilesRows + 128u * t;
       float factor = 1.0f;
       if (row0 >= at.rows || at.limit(t, p) <= at.k0) return factor;
-      const long long in = row0 + row;
-      const bool live = in < at.rows;
-      const int token = static_cast<int>((live ? in : row0) / p.group), query_head = at.head * p.group + static_cast<int>((live ? in : row0) % p.group);
+      const bool live = row0 + row < at.rows;
+      const uint32_t in = live ? row0 + row : row0, token = in / group, query_head = at.head * group + (in - token * group);
       const uint16_t* const from = static_cast<const uint16_t*>(p.q) + (at.r.start + token) * p.q_stride + static_cast<long long>(query_head) * D;
       uint32_t top = 0u;
       uint4 v[D / 8];
+      if (q_sectors) {                                     // whole sectors
 #pragma unroll
-      for (int k = 0; k < D / 8; ++k) v[k] = live ? reinterpret_cast<const uint4*>(from)[k] : make_uint4(0u, 0u, 0u, 0u);
+        for (int k = 0; k < D / 8; k += 2) load_sector(v[k], v[k + 1], from + 8 * k);
+      } else {
+#pragma unroll
+        for (int k = 0; k < D / 8; ++k) v[k] = reinterpret_cast<const uint4*>(from)[k];
+      }
+      if (!live) {
+#pragma unroll
+        for (int k = 0; k < D / 8; ++k) v[k] = make_uint4(0u, 0u, 0u, 0u);
+      }
 #pragma unroll
       for (int k = 0; k < D / 8; ++k)
         top = __vmaxu2(__vmaxu2(top, v[k].x & 0x7fff7fffu), __vmaxu2(v[k].y & 0x7fff7fffu, __vmaxu2(v[k].z & 0x7fff7fffu, v[k].w & 0x7fff7fffu)));
@@ -463,17 +490,16 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
     bool more = true;
     for (; more && ok; place = next) {
       const int limit = place.limit(t, p);
-      const long long row0 = static_cast<long long>(place.tile) * kTilesRows + 128 * t;
+      const uint32_t row0 = static_cast<uint32_t>(place.tile) * kTilesRows + 128u * t;
       const bool mine = row0 < place.rows, any = mine && limit > place.k0;  // the group has rows of the tile; the CTA has steps that they see
-      const int rows = mine ? static_cast<int>(min(128ll, place.rows - row0)) : 1;
+      const int rows = mine ? static_cast<int>(min(128u, place.rows - row0)) : 1;
       const bool live = row < rows;
-      const long long at = row0 + min(row, rows - 1);
-      const int token = static_cast<int>(at / p.group), query_head = place.head * p.group + static_cast<int>(at % p.group);
+      const uint32_t at = row0 + min(row, rows - 1), token = at / group, query_head = place.head * group + (at - token * group);
       float m = 0.0f, l = 0.0f;
       bool have = false, settled = false;                  // the row has a reference; every row of the warp has one
       if (any) {
         const float by_scale = factor * fabsf(p.scale_log2);
-        const int seen = place.r.seen(token), seen_first = place.r.seen(static_cast<int>(row0 / p.group));
+        const int seen = place.r.seen(static_cast<int>(token)), seen_first = place.r.seen(static_cast<int>(row0 / group));
         uint32_t scales = static_cast<uint32_t>(place.before) % kMeta;
         for (int j = place.k0; j < limit; ++j, ++count, scales = (scales + 1) % kMeta) {
           const bool mask = (j + 1) * kKeys > seen_first;  // as far as the group's first row sees
@@ -550,11 +576,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
           tm_wait_ld(o);
           if (live) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 8) {
-              uint32_t w[4];
+            for (int e = 0; e < 32; e += 16) {
+              uint32_t w[8];
 #pragma unroll
-              for (int k = 0; k < 4; ++k) w[k] = Elem<BF16>::pack_rn(__uint_as_float(o[e + 2 * k]) * by, __uint_as_float(o[e + 2 * k + 1]) * by);
-              *reinterpret_cast<uint4*>(to + d + e) = make_uint4(w[0], w[1], w[2], w[3]);
+              for (int k = 0; k < 8; ++k) w[k] = Elem<BF16>::pack_rn(__uint_as_float(o[e + 2 * k]) * by, __uint_as_float(o[e + 2 * k + 1]) * by);
+              store_sector(to + d + e, w, out_sectors);
             }
           }
         }
@@ -615,11 +641,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
           const float by = all == 0.0f ? 0.0f : 1.0f / all;
           if (live) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 8) {
-              uint32_t w[4];
+            for (int e = 0; e < 32; e += 16) {
+              uint32_t w[8];
 #pragma unroll
-              for (int k = 0; k < 4; ++k) w[k] = Elem<BF16>::pack_rn(o[e + 2 * k] * by, o[e + 2 * k + 1] * by);
-              *reinterpret_cast<uint4*>(to + d + e) = make_uint4(w[0], w[1], w[2], w[3]);
+              for (int k = 0; k < 8; ++k) w[k] = Elem<BF16>::pack_rn(o[e + 2 * k] * by, o[e + 2 * k + 1] * by);
+              store_sector(to + d + e, w, out_sectors);
             }
           }
         }

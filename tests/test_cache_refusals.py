@@ -59,7 +59,7 @@ def test_no_rows_are_nothing_to_do(call):
 
 @pytest.mark.parametrize("change,status", [
     (dict(heads=0), INVALID), (dict(heads=6), INVALID), (dict(heads=4 * 65, qs=4 * 65 * 128), UNSUPPORTED), (dict(requests=-1), INVALID), (dict(requests=8193), UNSUPPORTED),
-    (dict(most=0), INVALID), (dict(tokens=-1), INVALID)])
+    (dict(most=0), INVALID), (dict(tokens=-1), INVALID), (dict(tokens=2 ** 30), UNSUPPORTED)])
 def test_sizes_of_attention(change, status):
     assert attention(cache(), **change) == status and workspace(cache(), **{k: v for k, v in change.items() if k != "qs"}) == status
 
