@@ -299,7 +299,7 @@ __host__ __device__ constexpr uint32_t arrivals_of(int bar) {  // a group's warp
 // same number of steps whatever the requests' lengths are; tiles that several CTAs have a part of are added up through the workspace by the one that comes last, in the
 // order of the steps.
 // Bound by the chain scores -> weights -> sums -> scores of each group: about 4400 clocks a step where the products take 2050 and the exponentials, 16 per SM and clock, as many.
-// 8192 tokens, 32 query heads on 8 key heads: 639 us, 860 TFLOP/s (bf16 or fp16, heads of 128), at the 1.55 GHz that the power cap leaves.
+// 8192 tokens, 32 query heads on 8 key heads: 600 to 615 us, 900 TFLOP/s (bf16 or fp16, heads of 128), at the 1.55 GHz that the power cap leaves.
 template <bool BF16, int D>
 __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const AttentionParams p) {
   using Sh = Shared<D>;
@@ -669,27 +669,32 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
     uint32_t n = 0;                                        // steps so far
     uint4 raw[kItems];
     float4 scale = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    // lane g has the page of granule g of the next step, -1 where there is none; the others have its offset from there
-    int page = -1;
-    const int8_t* const from = codes + (token0 % 16) * D + chunk * 16;
+    // pages of the next step's granules, -1 where there is none: every thread reads those of its own tokens (one lane for each granule and shuffles: 16 requests of 8000 tokens,
+    // 64 rows 150 -> 217 us, 5 requests in chunks 366 -> 420, although fewer instructions)
+    int pages[kItems], scale_page = -1;
+    auto page_at = [&](int j, int granule) {
+      const int token = j * kKeys + 16 * granule;
+      if (token >= place.r.keys) return -1;
+      return p.table[static_cast<long long>(place.request) * p.table_pages + (token >> p.page_shift)];
+    };
     auto fetch_pages = [&](int j) {
-      const int token = j * kKeys + 16 * lane;
-      page = -1;
-      if (lane < kGranules && token < place.r.keys) page = p.table[static_cast<long long>(place.request) * p.table_pages + (token >> p.page_shift)];
+#pragma unroll
+      for (int it = 0; it < kItems; ++it) pages[it] = page_at(j, (token0 + it * (128 / kChunks)) / 16);
+      if (has_scale) scale_page = page_at(j, in_group);
     };
     auto fetch = [&](int j) {
-      const bool there = static_cast<unsigned>(page) < static_cast<unsigned>(p.pages);
-      const long long page_head = static_cast<long long>(page) * p.kv_heads + place.head;
-      const long long at = there ? ((page_head << p.page_shift) + ((j * kKeys + 16 * lane) & ((1 << p.page_shift) - 1))) * D : -1;
 #pragma unroll
       for (int it = 0; it < kItems; ++it) {
-        const long long off = __shfl_sync(kFull, at, D == 128 ? it : 2 * it + w / 2);
+        const int token = j * kKeys + token0 + it * (128 / kChunks);
         raw[it] = make_uint4(0u, 0u, 0u, 0u);
-        if (off >= 0) raw[it] = *reinterpret_cast<const uint4*>(from + off);
+        if (static_cast<unsigned>(pages[it]) < static_cast<unsigned>(p.pages))
+          raw[it] = *(reinterpret_cast<const uint4*>(codes + (((static_cast<long long>(pages[it]) * p.kv_heads + place.head) << p.page_shift) +
+                                                              (token & ((1 << p.page_shift) - 1))) * D) + chunk);
       }
       if (has_scale) {
         scale = make_float4(0.0f, -INFINITY, 0.0f, 0.0f);  // nothing of a page that is not there is seen
-        if (there) {
+        if (static_cast<unsigned>(scale_page) < static_cast<unsigned>(p.pages)) {
+          const long long page_head = static_cast<long long>(scale_page) * p.kv_heads + place.head;
           const float vs = fmaxf(p.v_scale[page_head], kLeastScale);
           scale = make_float4(p.k_scale[page_head], __log2f(vs), 1.0f / vs, 0.0f);
         }
