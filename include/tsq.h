@@ -331,7 +331,7 @@ tsq_status_t tsq_cache_load(const tsq_cache_t *cache, const int32_t *slots, int6
  * A page outside the cache in block_table, and what lies past table_pages, is not seen.  Codes and scales behind a request's last token are not used, whatever they hold.
  *   max_query    no request has more rows than this (>= 1); rows past it are left as they were
  *   requests     0 .. 8192, more are TSQ_ERR_UNSUPPORTED; so are tokens times q_heads / kv_heads of 2^31 and more
- *   scale        finite; 1 / sqrt(head_dim) is the usual one
+ *   scale        within +-2e38; 1 / sqrt(head_dim) is the usual one
  *   ws           DEVICE, of tsq_cache_workspace's size or larger, 16-byte aligned, initialised once by tsq_cache_workspace_init; one workspace
  *                serves one call at a time.  Calls of a step whose sizes are not above those that the size was asked for may share it
  * Offsets into the cache are 64-bit.  One kernel launch; the same inputs give the same bits.

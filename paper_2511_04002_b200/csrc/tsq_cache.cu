@@ -424,6 +424,7 @@ __global__ void __launch_bounds__(kLoadThreads) load_kernel(const LoadParams p) 
 // ---- host side -----------------------------------------------------------------------------------
 
 constexpr int kMaxSlots = 0x7fffffff;
+constexpr float kMostScale = 2.0e38f;  // times log2(e) still finite
 
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
@@ -653,7 +654,7 @@ tsq_status_t tsq_cache_attention(const tsq_cache_t* cache, const void* q, int64_
                                  void* out, int64_t out_stride, void* ws_dev, size_t ws_bytes, void* cuda_stream) {
   const tsq_status_t fine = check_attention_sizes(cache, tokens, q_heads, requests, max_query);
   if (fine != TSQ_OK) return fine;
-  if (table_pages < 0 || !(std::fabs(scale) <= 3.0e38f) || !ws_dev || !aligned(ws_dev, 16)) return TSQ_ERR_INVALID_ARG;
+  if (table_pages < 0 || !(std::fabs(scale) <= kMostScale) || !ws_dev || !aligned(ws_dev, 16)) return TSQ_ERR_INVALID_ARG;
   if (requests > 0 && (!query_start || !lengths || (table_pages > 0 && !block_table))) return TSQ_ERR_INVALID_ARG;
   if (!aligned(query_start, 4) || !aligned(lengths, 4) || !aligned(block_table, 4)) return TSQ_ERR_INVALID_ARG;
   if (!rows_fit(q, q_stride, tokens, q_heads, cache->head_dim) || !rows_fit(out, out_stride, tokens, q_heads, cache->head_dim)) return TSQ_ERR_INVALID_ARG;

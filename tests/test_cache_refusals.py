@@ -71,6 +71,11 @@ def test_arguments_of_attention(change):
     assert attention(cache(), **change) == INVALID
 
 
+@pytest.mark.parametrize("scale", [2.5e38, 3.0e38, -2.5e38, 3.4e38])
+def test_a_scale_that_is_infinite_in_binary_logarithms(scale):
+    assert attention(cache(), scale=scale) == INVALID
+
+
 def test_no_cache_and_no_place_for_the_answer():
     L = B.lib()
     n = C.c_size_t(0)
