@@ -132,19 +132,29 @@ __device__ __forceinline__ float top_score(const uint32_t (&scores)[32], uint32_
   }
   return most;
 }
-// Weights of 64 keys in binary16, two to a word; returns their sum over the values' scale.  most: the largest sum of a granule's weights, and so no less than any weight.
-template <bool MASK>
+// References up to this take part in the product's addend, f.y - m: that is off by up to 2^-5 there.  Beyond, it could be off by more than any weight may be in binary16
+// (from 2^27 on by 8 and more), so a score is formed as the reference was and the reference subtracted from it: the largest key's difference is 0 whatever m is.
+constexpr float kNearReference = 1048576.0f;  // 2^20
+
+// Weights of 32 keys in binary16, two to a word; their sum over the values' scale is added to l.  most: the largest sum of a granule's weights, and so no less than any weight.
+// FAR: references of any size; one that is near gives the same bits as without.
+template <bool MASK, bool FAR>
 __device__ __forceinline__ void weights_of_32(const uint32_t (&s)[32], uint32_t* w, uint32_t scales, float by_scale, float m, float& l, float& most, int left) {
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
     const float4 f = shared_float4(scales + 16 * g);
-    const float a = f.x * by_scale, b = f.y - m;
+    const bool far = FAR && fabsf(m) >= kNearReference;
+    const float a = f.x * by_scale, b = far ? f.y : f.y - m, less = far ? m : 0.0f;
     const uint64_t a2 = pack2f(a, a), b2 = pack2f(b, b);
     uint64_t sum = 0ull;                                   // of even and of odd keys
 #pragma unroll
     for (int e = 0; e < 16; e += 2) {
       float x0, x1;
       unpack2f(fma2(pack2u(s[16 * g + e], s[16 * g + e + 1]), a2, b2), x0, x1);
+      if constexpr (FAR) {
+        x0 -= less;
+        x1 -= less;
+      }
       if constexpr (MASK) {
         x0 = 16 * g + e < left ? x0 : -INFINITY;
         x1 = 16 * g + e + 1 < left ? x1 : -INFINITY;
@@ -160,13 +170,13 @@ __device__ __forceinline__ void weights_of_32(const uint32_t (&s)[32], uint32_t*
     l = __fmaf_rn(even + odd, f.z, l);
   }
 }
-template <bool MASK>
+template <bool MASK, bool FAR>
 __device__ __forceinline__ float weights_of(const uint32_t (&a)[32], const uint32_t (&b)[32], uint32_t (&w)[32], uint32_t scales, float by_scale, float m, float& most,
                                             int left) {
   float sum = 0.0f;
   most = 0.0f;
-  weights_of_32<MASK>(a, w, scales, by_scale, m, sum, most, left);
-  weights_of_32<MASK>(b, w + 16, scales + 32, by_scale, m, sum, most, left - 32);
+  weights_of_32<MASK, FAR>(a, w, scales, by_scale, m, sum, most, left);
+  weights_of_32<MASK, FAR>(b, w + 16, scales + 32, by_scale, m, sum, most, left - 32);
   return sum;
 }
 
@@ -496,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
       const bool live = row < rows;
       const uint32_t at = row0 + min(row, rows - 1), token = at / group, query_head = place.head * group + (at - token * group);
       float m = 0.0f, l = 0.0f;
-      bool have = false, settled = false;                  // the row has a reference; every row of the warp has one
+      bool have = false, settled = false;                  // the row has a reference; every row of the warp has one below kNearReference
       if (any) {
         const float by_scale = factor * fabsf(p.scale_log2);
         const int seen = place.r.seen(static_cast<int>(token)), seen_first = place.r.seen(static_cast<int>(row0 / group));
@@ -519,7 +529,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
             // binary16, which goes to 65504
             bool again = !settled;
             if (settled) {
-              sum = mask ? weights_of<true>(a, b, w, factors, by_scale, m, most_weight, left) : weights_of<false>(a, b, w, factors, by_scale, m, most_weight, 64);
+              sum = mask ? weights_of<true, false>(a, b, w, factors, by_scale, m, most_weight, left) : weights_of<false, false>(a, b, w, factors, by_scale, m, most_weight, 64);
               again = __any_sync(kFull, most_weight > 4096.0f);
             }
             if (again) {
@@ -531,7 +541,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                 m = most;
                 have = true;
               }
-              settled = __all_sync(kFull, have);
+              settled = __all_sync(kFull, have && fabsf(m) < kNearReference);
               l *= by;
               if (j > place.k0 || h > 0) {                 // the sums so far follow the reference
                 if (!wait(kODone + 2 * t + (h ^ 1), (h > 0 ? count : count - 1u) & 1u)) break;
@@ -546,7 +556,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                   tm_store16(o_at + d, o);
                 }
               }
-              sum = weights_of<true>(a, b, w, factors, by_scale, m, most_weight, mask ? left : 64);
+              sum = weights_of<true, true>(a, b, w, factors, by_scale, m, most_weight, mask ? left : 64);
             }
             l += sum;
             tm_store32(at_half, w);                        // in the place of scores, which have all been read

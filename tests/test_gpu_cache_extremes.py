@@ -1,0 +1,34 @@
+"""Attention over the paged 8-bit cache at the ends of its arguments' ranges."""
+import pytest
+import torch
+
+from tests._cache import HALF_STEP, Setup
+
+pytestmark = pytest.mark.gpu
+F16, BF16 = torch.float16, torch.bfloat16
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("added", [1, 40])
+@pytest.mark.parametrize("log2_scale", [0, 10, 14, 18, 22, 30, 60, 100])
+@pytest.mark.parametrize("winner,others,sign", [(127, 40, 1), (127, 40, -1), (60, 127, 1)])
+def test_scores_far_from_zero(dtype, added, log2_scale, winner, others, sign):
+    """One key's score is above the others' by more than 2^8 at any of these scales, at 60 against 127 with every score below zero: a row is that
+    key's value.  The weight of it may be off by half a step of binary16, as all weights; where binary32 has no place left for fractions of a score,
+    it still is the one weight."""
+    held = 400
+    s = Setup(dtype, [held], 2, 64, 16, seed=31)
+    g = torch.Generator().manual_seed(5)
+    every = s.table[0, :(held + 15) // 16].long()
+    s.k_scale[every] = 0.031
+    for where in [0, 70, 200, held - added]:                            # every row sees them
+        s.k_codes[every] = -others if others > winner else torch.randint(-others, others, s.k_codes[every].shape, generator=g).to(torch.int8).cuda()
+        s.k_codes[int(s.table[0, where // 16]), :, where % 16] = (-winner if others > winner else winner)
+        q = torch.rand((added, 6, 1), generator=g) * 3 + 2              # each row in its own place of its binade
+        q = (q * sign).to(dtype).expand(added, 6, 64).contiguous().cuda()
+        out = torch.full_like(q, 5.0)
+        ws = s.cache.workspace(added, 6, 1, added)
+        s.cache.attention(q, s.ints([0, added]), s.ints([held]), s.table, out, ws, added, scale=sign * 2.0 ** log2_scale)
+        page = int(s.table[0, where // 16])
+        want = (s.v_codes[page, :, where % 16].double() * s.v_scale[page].double()[:, None]).repeat_interleave(3, 0)[None]
+        assert bool(((out.double() - want).abs() <= (2.0 ** -11 + HALF_STEP[dtype] + 2.0 ** -16) * want.abs() + 2.0 ** -24).all()), (where, out[0, :, :4], want[0, :, :4])
