@@ -80,12 +80,11 @@ __device__ __forceinline__ uint32_t less_1152(uint32_t pair) {
 __device__ __forceinline__ uint32_t widen_lo(uint32_t u) { return less_1152(__byte_perm(u, 0x64646464u, 0x4140)); }
 __device__ __forceinline__ uint32_t widen_hi(uint32_t u) { return less_1152(__byte_perm(u, 0x64646464u, 0x4342)); }
 
-// Power of two that brings a row whose largest magnitude is `top` to just below 2^15 (2^112 at most), and the inverse.  Both stay in binary32's normal range; a row that is zero or not
-// finite is left alone.
+// Power of two that brings a row whose largest magnitude is `top` to just below 2^15 (2^112 at most, which brings the least bfloat16 numbers to 2^-21, a binary16 number), and the
+// inverse.  Both stay in binary32's normal range; a row that is not finite is left alone.
 __device__ __forceinline__ float row_power(float top, float& inverse) {
   const int e = static_cast<int>(__float_as_uint(top) >> 23);              // biased exponent; 0: below the normal range
-  const bool plain = e > 0 && e < 255;
-  const int up = plain ? min(14 - (e - 127), 112) : 0;
+  const int up = e < 255 ? min(14 - (e - 127), 112) : 0;
   inverse = __uint_as_float(static_cast<uint32_t>(127 - up) << 23);
   return __uint_as_float(static_cast<uint32_t>(127 + up) << 23);
 }

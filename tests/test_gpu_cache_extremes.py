@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from tests._cache import HALF_STEP, Setup
+from tests.test_gpu_cache import check_attention
 
 pytestmark = pytest.mark.gpu
 F16, BF16 = torch.float16, torch.bfloat16
@@ -32,3 +33,12 @@ def test_scores_far_from_zero(dtype, added, log2_scale, winner, others, sign):
         page = int(s.table[0, where // 16])
         want = (s.v_codes[page, :, where % 16].double() * s.v_scale[page].double()[:, None]).repeat_interleave(3, 0)[None]
         assert bool(((out.double() - want).abs() <= (2.0 ** -11 + HALF_STEP[dtype] + 2.0 ** -16) * want.abs() + 2.0 ** -24).all()), (where, out[0, :, :4], want[0, :, :4])
+
+
+@pytest.mark.parametrize("added", [1, 40])
+def test_queries_below_bfloat16_s_normal_range(added):
+    s = Setup(BF16, [130, 77], 2, 64, 16, seed=32)
+    g = torch.Generator().manual_seed(6)
+    q = (torch.randn((2 * added, 4, 64), generator=g, dtype=torch.float64) * 2.0 ** -128).to(BF16).cuda()
+    assert 0.0 < float(q.double().abs().max()) < 2.0 ** -125
+    check_attention(s, [added, added], 2, q=q, pad=0, scale=2.0 ** 127)
