@@ -325,7 +325,8 @@ tsq_status_t tsq_cache_load(const tsq_cache_t *cache, const int32_t *slots, int6
  * 64 times; query head h reads key head h / (q_heads / kv_heads).  Request i owns the rows query_start[i] .. query_start[i + 1) and has lengths[i]
  * tokens in the cache, its own of this step among them; its row j is the token at position lengths[i] - n_i + j and sees the positions up to its own:
  *   out = sum_p softmax_p(scale * <q, k_p>) v_p
- * A value scale below 2^-60 counts as 2^-60; the scales of the value pages that a row sees may differ by a factor of 2^80.
+ * A value scale below 2^-60 counts as 2^-60; the scales of the value pages that a row sees may differ by a factor of 2^80.  A scale that is NaN makes the rows NaN that see a
+ * key of its page and head, and no others; negative ones are not allowed: what the rows that see them come out as is undefined.
  * Rows that see no key (n_i > lengths[i]) are written as zeros, rows behind the last request's are left as they were.  Scores, the softmax's
  * sum and the accumulators are binary32; weights are rounded to binary16, relative to the largest of their row times its page's scale.
  * A page outside the cache in block_table, and what lies past table_pages, is not seen.  Codes and scales behind a request's last token are not used, whatever they hold.

@@ -10,6 +10,10 @@ namespace tsq {
 // Weights are 2^(score + log2 s_v - m) and the softmax's sum takes them over s_v: both have to stay in binary32's range for every page that counts.  A values' scale below
 // this counts as this (tsq_cache_store's are 2^-40 at least): what its codes add is under 2^-53, and a page may lie 2^80 below another of the row before its keys leave the sum.
 constexpr float kLeastScale = 8.673617379884035e-19f;  // 2^-60
+// Its logarithm and its inverse.  A scale that is NaN makes the weights of its keys NaN by the logarithm, and with them the rows that see one; the inverse stays a number,
+// since it also multiplies the weight 0 of rows that see none.
+__device__ __forceinline__ float log2_of_scale(float s) { return s != s ? s : __log2f(fmaxf(s, kLeastScale)); }
+__device__ __forceinline__ float inverse_of_scale(float s) { return 1.0f / fmaxf(s, kLeastScale); }
 
 // A request as the kernels read it: every number is brought into the range of the arrays first.
 struct Request {

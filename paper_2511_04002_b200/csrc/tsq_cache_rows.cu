@@ -235,8 +235,7 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
       };
       // score factor, log2 and inverse of the values' scale of a batch's steps
       auto put_scales = [&](int b) {
-        const float v = fmaxf(vs, kLeastScale);
-        asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(scales + ((b & 1) * 32 + lane) * 16), "f"(ks * p.scale_log2), "f"(__log2f(v)), "f"(1.0f / v), "f"(0.0f)
+        asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(scales + ((b & 1) * 32 + lane) * 16), "f"(ks * p.scale_log2), "f"(log2_of_scale(vs)), "f"(inverse_of_scale(vs)), "f"(0.0f)
                      : "memory");
       };
       auto issue = [&](int step) {

@@ -705,8 +705,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
         scale = make_float4(0.0f, -INFINITY, 0.0f, 0.0f);  // nothing of a page that is not there is seen
         if (static_cast<unsigned>(scale_page) < static_cast<unsigned>(p.pages)) {
           const long long page_head = static_cast<long long>(scale_page) * p.kv_heads + place.head;
-          const float vs = fmaxf(p.v_scale[page_head], kLeastScale);
-          scale = make_float4(p.k_scale[page_head], __log2f(vs), 1.0f / vs, 0.0f);
+          const float vs = p.v_scale[page_head];
+          scale = make_float4(p.k_scale[page_head], log2_of_scale(vs), inverse_of_scale(vs), 0.0f);
         }
       }
     };

@@ -1,4 +1,6 @@
 """Attention over the paged 8-bit cache at the ends of its arguments' ranges."""
+import math
+
 import pytest
 import torch
 
@@ -42,3 +44,21 @@ def test_queries_below_bfloat16_s_normal_range(added):
     q = (torch.randn((2 * added, 4, 64), generator=g, dtype=torch.float64) * 2.0 ** -128).to(BF16).cuda()
     assert 0.0 < float(q.double().abs().max()) < 2.0 ** -125
     check_attention(s, [added, added], 2, q=q, pad=0, scale=2.0 ** 127)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("added,first", [(1, 322), (5, 320), (40, 304)])   # of the page, in the first request: its earlier rows do not see it
+@pytest.mark.parametrize("of", ["k_scale", "v_scale"])
+def test_a_page_whose_scale_is_no_number_spoils_the_rows_that_see_it(dtype, added, first, of):
+    s = Setup(dtype, [323, 90], 2, 128, 16, seed=33)
+    T = 2 * added
+    q = s.rows(T, 6)
+    args = (s.ints([0, added, T]), s.ints([323, 90]), s.table)
+    ws = s.cache.workspace(T, 6, 2, added)
+    clean, out = torch.zeros_like(q), torch.zeros_like(q)
+    s.cache.attention(q, *args, clean, ws, added)
+    getattr(s, of)[int(s.table[0, first // 16]), 1] = math.nan
+    s.cache.attention(q, *args, out, ws, added)
+    spoilt = torch.zeros((T, 6), dtype=torch.bool, device="cuda")
+    spoilt[max(0, first - (323 - added)):added, 3:] = True
+    assert torch.equal(out.isnan().all(-1), spoilt) and torch.equal(out.isnan().any(-1), spoilt) and torch.equal(out[~spoilt], clean[~spoilt])
