@@ -293,10 +293,10 @@ struct Shared {
   static constexpr int kBars = kScales + kMeta * kGranules * 16;
   static constexpr int kBytes = kBars + 256;
 };
-// Barriers: buffers of keys and values; a half step's scores, weights and sums, by group and half; a tile's queries, by group.
-enum Bar { kKFull = 0, kKFree = 2, kVFull = 4, kVFree = 6, kSFull = 8, kPReady = 12, kODone = 16, kQFull = 20, kBarCount = 22 };
+// Barriers: buffers of keys and values; a half step's scores, weights and sums, by group and half; a tile's queries, by group; the end of a group's products.
+enum Bar { kKFull = 0, kKFree = 2, kVFull = 4, kVFree = 6, kSFull = 8, kPReady = 12, kODone = 16, kQFull = 20, kEnd = 22, kBarCount = 24 };
 __host__ __device__ constexpr uint32_t arrivals_of(int bar) {  // a group's warps, or one for the products of each group
-  return bar < kKFree || (bar >= kVFull && bar < kVFree) || (bar >= kPReady && bar < kODone) || bar >= kQFull ? 4u : bar < kSFull ? 2u : 1u;
+  return bar < kKFree || (bar >= kVFull && bar < kVFree) || (bar >= kPReady && bar < kODone) || (bar >= kQFull && bar < kEnd) ? 4u : bar >= kKFree && bar < kSFull ? 2u : 1u;
 }
 
 // A CTA's two groups of 128 threads have 128 query rows each, a thread a row; a tile is the 256 rows of one (request, key head) that follow one another, the group's query
@@ -746,9 +746,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
       const uint32_t leader = elected(), base = uniform(smem), bar = uniform(bars), tm = uniform(tmem);
       constexpr uint32_t kScores = product_of(kKeys / 2, false), kSums = product_of(D, true);
       uint32_t n = 0, count = 0, tiles = 0;                  // steps; steps and tiles of the group
+      bool issued = false;
       // scores of 64 of the keys in buffer `buffer`
       auto scores = [&](uint32_t buffer, int h) {
         tm_fence_after();
+        issued = true;
         const uint64_t queries = operand(base + Sh::kQ + t * Sh::kOperand, 16, 1024), keys = operand(base + Sh::kK + buffer * Sh::kOperand + h * (kHalf / 2), 16, 1024);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
@@ -804,14 +806,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
           __syncwarp();
         }
       } while (ok && place.next(p));
-      // everything issued has ended before the tensor memory is given back
-      if (count > 0) {
-        for (int h = 0; h < 2; ++h) {
-          bar_wait(bars + 8 * (kSFull + 2 * t + h), (count - 1u) & 1u);
-          bar_wait(bars + 8 * (kODone + 2 * t + h), (count - 1u) & 1u);
-        }
+      // everything issued has ended before the tensor memory is given back, wherever the loops were left: a commit stands for all of the thread's products before it
+      if (issued) {
+        tm_commit(leader, bar + 8 * (kEnd + t));
+        if (!bar_wait(bars + 8 * (kEnd + t), 0u)) ok = false;
       }
-      __syncwarp();
+      ok = __all_sync(kFull, ok);
     }
     regs_back<kProductRegs>(4, !ok, &s_failed);
   }
