@@ -342,7 +342,8 @@ tsq_status_t tsq_cache_workspace(const tsq_cache_t *cache, int64_t tokens, int32
 tsq_status_t tsq_cache_workspace_init(void *ws_dev, size_t ws_bytes, void *cuda_stream);
 /*
  * TSQ_OK, or TSQ_ERR_TIMEOUT if a wait inside an attention call's kernel ran out since the workspace was initialised (every wait is for the call's own work: it
- * cannot in a sound call).  Synchronises `cuda_stream`; `status` is HOST.
+ * cannot in a sound call).  The output of the call that it ran out in is undefined; calls behind it leave theirs as it was, until tsq_cache_workspace_init.
+ * Synchronises `cuda_stream`; `status` is HOST.
  */
 tsq_status_t tsq_cache_workspace_status(const void *ws_dev, uint32_t *status, void *cuda_stream);
 tsq_status_t tsq_cache_attention(const tsq_cache_t *cache, const void *q, int64_t q_stride, int32_t q_heads, int64_t tokens,

@@ -38,8 +38,8 @@ struct AttentionParams {
   int32_t requests, table_pages, pages, kv_heads, group, max_query;
   int32_t page_shift;                      // log2 of the page's tokens
   float scale_log2;                        // scale * log2(e)
-  unsigned int* status;                    // of the workspace
-  unsigned int* counters;                  // 0 between calls
+  unsigned int* status;                    // of the workspace; not TSQ_OK: a wait ran out since it was initialised, and no call uses it
+  unsigned int* counters;                  // 0 between calls, as long as the status is TSQ_OK
   float* partials;                         // sums of tiles that several CTAs have a part of
 };
 

@@ -143,11 +143,13 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ unsigned long long s_scan[kWarps];
   __shared__ int s_found;
+  __shared__ unsigned int s_status;
   __shared__ unsigned long long s_begin;
   __shared__ unsigned int s_last;
   launch_dependents();
   wait_for_prior_grids();
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, c = lane % 4;
+  const unsigned int status = *static_cast<volatile unsigned int*>(p.status);  // one thread's is used, behind a barrier: on its way with the requests
 
   // the CTA's share, and the request that has its first unit: every thread sums its requests' units, and the one whose sums reach past the first unit tells the others
   unsigned long long total, unit, unit_end;
@@ -169,6 +171,7 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
     if (lane == 31) s_scan[warp] = in;
     if (tid == 0) {
       s_found = 0;
+      s_status = status;
       s_begin = 0;
     }
     __syncthreads();
@@ -180,7 +183,7 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
       total += s_scan[w];
     }
     ctas = total < gridDim.x ? static_cast<unsigned int>(total) : gridDim.x;
-    if (blockIdx.x >= ctas) return;
+    if (blockIdx.x >= ctas || s_status != TSQ_OK) return;
     unit = scaled(blockIdx.x, total, ctas);
     unit_end = scaled(blockIdx.x + 1, total, ctas);
     if (at <= unit && unit < at + mine) {

@@ -315,11 +315,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
   using Sh = Shared<D>;
   extern __shared__ unsigned char smem_raw[];
   __shared__ unsigned long long s_scan[kThreads / 32], s_begin, s_tiles[kThreads / 32];
-  __shared__ uint32_t s_tmem, s_failed;
+  __shared__ uint32_t s_tmem, s_failed, s_status;
   __shared__ int s_found;
   launch_dependents();
   wait_for_prior_grids();
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  if (tid == kThreads - 1) s_status = *static_cast<volatile unsigned int*>(p.status);  // in the last warp, which has the fewest requests
   const uint32_t smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
   unsigned char* const smem_at = smem_raw + (smem - smem_addr(smem_raw));
 
@@ -378,7 +379,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
       tiles += s_tiles[w];
     }
     ctas = static_cast<unsigned int>(min(static_cast<unsigned long long>(gridDim.x), min(total, kMostParts * tiles)));
-    if (blockIdx.x >= ctas) return;
+    if (blockIdx.x >= ctas || s_status != TSQ_OK) return;
     place.unit = scaled(blockIdx.x, total, ctas);
     place.end = scaled(blockIdx.x + 1, total, ctas);
     for (int i = i0; i < i1; ++i) {
