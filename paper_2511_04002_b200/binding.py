@@ -287,11 +287,18 @@ class Cache:
         self.workspace_init(ws)
         return ws
 
+    def _check_workspace(self, ws: torch.Tensor) -> None:
+        assert ws.is_cuda and ws.device.index == self.device and ws.dtype == torch.uint8 and ws.is_contiguous(), \
+            "ws must be a contiguous uint8 CUDA tensor on the cache's device"
+
     def workspace_init(self, ws: torch.Tensor, stream=None) -> None:
+        self._check_workspace(ws)
         with torch.cuda.device(self.device):
             _check(lib().tsq_cache_workspace_init(ws.data_ptr(), ws.numel(), _stream(stream)), "tsq_cache_workspace_init")
 
     def workspace_status(self, ws: torch.Tensor, stream=None) -> int:
+        self._check_workspace(ws)
+        assert ws.numel() >= 16, "ws is no workspace"
         out = C.c_uint32(0)
         with torch.cuda.device(self.device):
             _check(lib().tsq_cache_workspace_status(ws.data_ptr(), C.byref(out), _stream(stream)), "tsq_cache_workspace_status")

@@ -102,3 +102,12 @@ def slots(page=16, held=PTR, added=PTR, requests=3, free=PTR, n_free=4, start=PT
     (dict(tokens=2 ** 31), INVALID), (dict(taken=None), INVALID), (dict(held=PTR + 2), INVALID), (dict(table=PTR + 1), INVALID)])
 def test_slots(change, status):
     assert slots(**change) == status
+
+
+@pytest.mark.parametrize("call", ["workspace_init", "workspace_status"])
+def test_workspaces_on_the_host(call):
+    import torch
+    of = B.Cache.__new__(B.Cache)                                       # a cache's tensors need a device
+    of.device = 0
+    with pytest.raises(AssertionError):
+        getattr(of, call)(torch.zeros(1 << 20, dtype=torch.uint8))

@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from paper_2511_04002_b200 import binding as B
 from tests._cache import Setup
 
 pytestmark = pytest.mark.gpu
@@ -32,3 +33,14 @@ def test_a_workspace_whose_wait_ran_out_is_not_used_before_an_init(added):
         s.cache.attention(*args, out, ws, added)
         assert torch.equal(out, want)
     assert s.cache.workspace_status(ws) == 0
+
+
+@pytest.mark.parametrize("call", ["workspace_init", "workspace_status"])
+def test_tensors_that_are_no_workspace(call):
+    s = Setup(F16, [40], 2, 64, 16, seed=35)
+    ws = s.cache.workspace(1, 4, 1, 1)
+    one = torch.zeros(1, dtype=torch.uint8, device="cuda")
+    for bad in (ws.cpu(), ws.view(torch.int32), ws.view(torch.float32), ws[::2], one.expand(1 << 24), ws[:0]):
+        with pytest.raises((AssertionError, B.TsqError)):
+            getattr(s.cache, call)(bad)
+    getattr(s.cache, call)(ws)
