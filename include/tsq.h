@@ -263,7 +263,7 @@ double tsq_model_best_rate(double rate_lo, double rate_hi, double bandwidth, dou
  *
  * A cache is described by a HOST struct that the caller fills in; the library keeps nothing of it.
  *   dtype        type of the 16-bit rows that are stored, loaded and attended with
- *   kv_heads     >= 1
+ *   kv_heads     1 .. 1024 (more are TSQ_ERR_UNSUPPORTED)
  *   head_dim     64 or 128 (else TSQ_ERR_UNSUPPORTED)
  *   page_tokens  tokens of a page: 16, 32, 64 or 128 (else TSQ_ERR_UNSUPPORTED)
  *   pages        >= 1; pages * page_tokens < 2^31
@@ -328,7 +328,9 @@ tsq_status_t tsq_cache_load(const tsq_cache_t *cache, const int32_t *slots, int6
  * A value scale below 2^-60 counts as 2^-60; the scales of the value pages that a row sees may differ by a factor of 2^80.  A scale that is NaN makes the rows NaN that see a
  * key of its page and head, and no others; negative ones are not allowed: what the rows that see them come out as is undefined.
  * Rows that see no key (n_i > lengths[i]) are written as zeros, rows behind the last request's are left as they were.  Scores, the softmax's
- * sum and the accumulators are binary32; weights are rounded to binary16, relative to the largest of their row times its page's scale.
+ * sum and the accumulators are binary32; weights are rounded to binary16, relative to the largest of their row times its page's scale.  The products of scale * log2(e) with a
+ * page's key scale, with a row's largest query and with both have to stay in binary32's range, as the scores have.  bfloat16 queries are taken in binary16 relative to the
+ * largest of their row and query head: exact down to 2^-31 of it, with fewer bits below, 0 under 2^-39.
  * A page outside the cache in block_table, and what lies past table_pages, is not seen.  Codes and scales behind a request's last token are not used, whatever they hold.
  *   max_query    no request has more rows than this (>= 1); rows past it are left as they were
  *   requests     0 .. 8192, more are TSQ_ERR_UNSUPPORTED; so are tokens times q_heads / kv_heads of 2^31 and more

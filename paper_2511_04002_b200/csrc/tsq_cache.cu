@@ -1,5 +1,5 @@
 // The paged 8-bit key/value cache: argument checks and launches of its calls, and the kernels that build block tables and slots, quantise keys
-// and values into the cache and read them back.  Attention: tsq_cache_rows.cu.
+// and values into the cache and read them back.  Attention: tsq_cache_rows.cu for few query rows, tsq_cache_tiles.cu for many.
 
 #include <algorithm>
 #include <atomic>
@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(kLoadThreads) load_kernel(const LoadParams p) 
   const long long t0 = static_cast<long long>(blockIdx.x) * p.block;
   const int tokens = static_cast<int>(min(static_cast<long long>(p.block), p.tokens - t0));
   const int mine = static_cast<int>(threadIdx.x) / all;                    // 0 where a token's chunks are more than the threads
-  const uint32_t page_bytes = static_cast<uint32_t>(p.heads << p.page_shift) * D;  // of the keys' codes; below 2^24
+  const uint32_t page_bytes = static_cast<uint32_t>(p.heads << p.page_shift) * D;  // of the keys' codes; 2^24 at most
   const int place_mask = (1 << p.page_shift) - 1;
   wait_for_prior_grids();
   if (mine >= together) return;

@@ -131,8 +131,9 @@ struct Layout {
 // Codes go from HBM to shared memory by asynchronous copies and are widened to binary16 in registers (exact).  Both products have the codes as their 16-row
 // operand and the query rows as columns, eight to a product: S^T = K Q^T, O^T += V^T P^T, where P^T is S^T transposed by 8 x 8 blocks.  The order of the
 // head's dimensions in the products is free: thread c of a token's four takes D / 4 neighbouring ones, so a token is read as 16-byte chunks.  Scores: q
-// scaled by a power of two per row (exact), code products summed in binary32, times the page's scale.  With the values' scale s_v of the page, weights are
-// w = 2^(score + log2 s_v - m), rounded to binary16 for the product with the values' codes, and the softmax's sum takes w / s_v.
+// scaled by a power of two per row (binary16 queries exactly, bfloat16 ones down to 2^-31 of the row's largest), code products summed in binary32, times the page's
+// scale.  With the values' scale s_v of the page, weights are w = 2^(score + log2 s_v - m), rounded to binary16 for the product with the values' codes, and the softmax's
+// sum takes w / s_v.
 // Bound by HBM where the cache is long (64 requests of 500 to 8000 tokens, 558 MB: 99 to 102 us, 5.5 TB/s), by the chain lengths -> table -> codes -> sums where it is short (one of
 // 1001 tokens: 10 us).
 template <bool BF16, int D, int NT>
