@@ -309,7 +309,7 @@ __host__ __device__ constexpr uint32_t arrivals_of(int bar) {  // a group's warp
 // same number of steps whatever the requests' lengths are; tiles that several CTAs have a part of are added up through the workspace by the one that comes last, in the
 // order of the steps.
 // Bound by the chain scores -> weights -> sums -> scores of each group: about 4400 clocks a step where the products take 2050 and the exponentials, 16 per SM and clock, as many.
-// 8192 tokens, 32 query heads on 8 key heads: 600 to 630 us, 870 to 910 TFLOP/s (bf16 or fp16, heads of 128), at the 1.55 GHz that the power cap leaves.
+// 8192 tokens, 32 query heads on 8 key heads: 600 to 634 us, 865 to 910 TFLOP/s (bf16 or fp16, heads of 128), at the 1.55 GHz that the power cap leaves.
 template <bool BF16, int D>
 __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const AttentionParams p) {
   using Sh = Shared<D>;
