@@ -353,6 +353,57 @@ tsq_status_t tsq_cache_attention(const tsq_cache_t *cache, const void *q, int64_
                                  const int32_t *block_table, int32_t table_pages, float scale, void *out,
                                  int64_t out_stride, void *ws_dev, size_t ws_bytes, void *cuda_stream);
 
+/*
+ * The paged 4-bit key/value cache: half the bytes of the 8-bit one for each token, with a scale and a zero-point for each token and head (the range of Eq. "Proposed" on signed values at
+ * 4 bits, taken over the token's row of one head).  Pages, slots, block tables (tsq_cache_slots), strides, streams, workspaces (tsq_cache_workspace_init, tsq_cache_workspace_status) and
+ * errors are those of the 8-bit cache; the differences:
+ *   k_codes, v_codes  DEVICE, [pages][kv_heads][page_tokens][head_dim / 2], 16-byte aligned: two codes 0 .. 15 to a byte, the even dimension's in the lower half
+ *   k_grid, v_grid    DEVICE, [pages][kv_heads][page_tokens], 16-byte aligned: the scale, a bfloat16 number >= 0, in the lower half of a word, the zero-point, a signed 16-bit number within
+ *                     +-1000, in the upper half.  A code stands for (code + zero-point) * scale
+ */
+typedef struct {
+  tsq_dtype_t dtype;
+  int32_t kv_heads, head_dim, page_tokens;
+  int64_t pages;
+  uint8_t *k_codes, *v_codes;
+  uint32_t *k_grid, *v_grid;
+} tsq_cache4_t;
+
+/*
+ * Quantise a step's keys and values into the cache, as tsq_cache_store.  Rows go by themselves: slots may come in any order, and nothing but a row's own codes and words is written; a slot
+ * that comes twice in a call is left with codes and word of its rows in an undefined mixture.  With lo and hi the least and the largest finite number of a row, within +-2^126 (0 where none is finite):
+ *   scale  s = max((hi - lo) / 15, max(|lo|, |hi|) / 128, 2^-40), in IEEE binary32 (round-to-nearest-even), then up to the next number of seven significant bits
+ *   zero-point z = round(lo / s); codes max(0, min(15, round(x / s) - z)), infinities the last or the first, NaN 0; round takes halves away from zero, quotients are exact
+ * One kernel launch.
+ */
+tsq_status_t tsq_cache4_store(const tsq_cache4_t *cache, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                              int64_t tokens, const int32_t *slots, void *cuda_stream);
+
+/*
+ * Read tokens back, as tsq_cache_load: (code + zero-point) * scale in binary32, rounded once to the cache's dtype and not beyond its largest finite number (a scale that is NaN gives NaN); 0 for a
+ * slot outside the cache.  One kernel launch.
+ */
+tsq_status_t tsq_cache4_load(const tsq_cache4_t *cache, const int32_t *slots, int64_t tokens, void *k, int64_t k_stride,
+                             void *v, int64_t v_stride, void *cuda_stream);
+
+/*
+ * Attention of a step's queries over the cache, as tsq_cache_attention, with scales and zero-points by token.
+ *   causal   1: row j of request i is the token at position lengths[i] - n_i + j and sees the positions up to its own.  0: every row of request i sees all of its lengths[i] tokens, whatever
+ *            n_i is (a decoder's queries over an encoder's states, which were stored once).  Anything else is TSQ_ERR_INVALID_ARG
+ * A value scale below 2^-60 counts as 2^-60 in the weights' scaling and as what it is in the value; the scales of the values that a row sees may differ by a factor of 2^80.  A token whose key or
+ * value scale is NaN or infinite makes the rows NaN that see it, and no others.  With up to 32 query rows (max_query times q_heads / kv_heads) products with codes are exact and scales
+ * come in in binary32.  With more, values and keys are brought to binary16 relative to the largest number that 16 neighbouring tokens can stand for, exactly as long as a token's codes reach down
+ * to 0 or across it and its scale has seven significant bits and is no less than 2^-32 of that number; otherwise they are rounded once, or lose bits below 2^-35 of it.  The ranges that tsq_cache_attention
+ * asks of scale, key scales and queries hold for the tokens' key scales; queries lie within +-2^120.
+ * The workspace is of tsq_cache4_workspace's size or larger; one may be shared with calls over an 8-bit cache that it is large enough for.
+ */
+tsq_status_t tsq_cache4_workspace(const tsq_cache4_t *cache, int64_t tokens, int32_t q_heads, int32_t requests, int32_t max_query,
+                                  size_t *workspace_bytes);
+tsq_status_t tsq_cache4_attention(const tsq_cache4_t *cache, const void *q, int64_t q_stride, int32_t q_heads, int64_t tokens,
+                                  const int32_t *query_start, const int32_t *lengths, int32_t requests, int32_t max_query,
+                                  const int32_t *block_table, int32_t table_pages, float scale, int32_t causal, void *out,
+                                  int64_t out_stride, void *ws_dev, size_t ws_bytes, void *cuda_stream);
+
 /* Number of kernels the library has launched in this process (all plans, all streams). */
 uint64_t tsq_kernel_launch_count(void);
 

@@ -2,7 +2,7 @@
 
 Every step of encode and decode runs inside the CUDA library; torch is used for device
 memory and streams.  Function names mirror the C entry points.  The calls of a decode step,
-encode and decode and those of the paged cache, go through the extension module built from
+encode and decode and those of the paged caches, go through the extension module built from
 csrc/tsq_torch.cpp (5 us less host time per call than ctypes); everything else goes through ctypes.
 """
 from __future__ import annotations
@@ -25,6 +25,7 @@ EXPORTS = ["tsq_plan", "tsq_plan_variant", "tsq_plan_sizes", "tsq_workspace_init
            "tsq_workspace_status", "tsq_encode_host", "tsq_decode_host", "tsq_kernel_launch_count",
            "tsq_plan_destroy", "tsq_status_string",
            "tsq_cache_slots", "tsq_cache_store", "tsq_cache_load", "tsq_cache_workspace", "tsq_cache_workspace_init", "tsq_cache_workspace_status", "tsq_cache_attention",
+           "tsq_cache4_store", "tsq_cache4_load", "tsq_cache4_workspace", "tsq_cache4_attention",
            "tsq_model_kv_bits", "tsq_model_io_bits", "tsq_model_outage", "tsq_model_latency", "tsq_model_best_rate"]
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtsq.so")
@@ -50,6 +51,11 @@ class _Info(C.Structure):
 class _CacheStruct(C.Structure):
     _fields_ = [("dtype", C.c_int), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_tokens", C.c_int32), ("pages", C.c_int64),
                 ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class _Cache4Struct(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_tokens", C.c_int32), ("pages", C.c_int64),
+                ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_grid", C.c_void_p), ("v_grid", C.c_void_p)]
 
 
 def lib() -> C.CDLL:
@@ -84,7 +90,7 @@ def lib() -> C.CDLL:
                  "tsq_workspace_status", "tsq_encode_host", "tsq_decode_host"):
         getattr(L, name).restype = C.c_int
     d, i32 = C.c_double, C.c_int32
-    cache, ip = C.POINTER(_CacheStruct), C.c_void_p
+    cache, cache4, ip = C.POINTER(_CacheStruct), C.POINTER(_Cache4Struct), C.c_void_p
     L.tsq_cache_slots.argtypes = [i32, ip, ip, i32, ip, i32, ip, ip, ip, i32, ip, i64, ip, vp]
     L.tsq_cache_store.argtypes = [cache, vp, i64, vp, i64, i64, ip, vp]
     L.tsq_cache_load.argtypes = [cache, ip, i64, vp, i64, vp, i64, vp]
@@ -92,8 +98,12 @@ def lib() -> C.CDLL:
     L.tsq_cache_workspace_init.argtypes = [vp, sz, vp]
     L.tsq_cache_workspace_status.argtypes = [vp, C.POINTER(C.c_uint32), vp]
     L.tsq_cache_attention.argtypes = [cache, vp, i64, i32, i64, ip, ip, i32, i32, ip, i32, C.c_float, vp, i64, vp, sz, vp]
+    L.tsq_cache4_store.argtypes = [cache4, vp, i64, vp, i64, i64, ip, vp]
+    L.tsq_cache4_load.argtypes = [cache4, ip, i64, vp, i64, vp, i64, vp]
+    L.tsq_cache4_workspace.argtypes = [cache4, i64, i32, i32, i32, C.POINTER(sz)]
+    L.tsq_cache4_attention.argtypes = [cache4, vp, i64, i32, i64, ip, ip, i32, i32, ip, i32, C.c_float, i32, vp, i64, vp, sz, vp]
     for name in ("tsq_cache_slots", "tsq_cache_store", "tsq_cache_load", "tsq_cache_workspace", "tsq_cache_workspace_init", "tsq_cache_workspace_status",
-                 "tsq_cache_attention"):
+                 "tsq_cache_attention", "tsq_cache4_store", "tsq_cache4_load", "tsq_cache4_workspace", "tsq_cache4_attention"):
         getattr(L, name).restype = C.c_int
     L.tsq_model_kv_bits.argtypes = [i64, i32, i32, i32, i64, d, d]
     L.tsq_model_io_bits.argtypes = [i64, i32, i32, i32, i64, d, d, i32]
@@ -235,50 +245,25 @@ class Plan:
         _check(st, "tsq_decode_host")
 
 
-class Cache:
-    """The paged 8-bit key/value cache (tsq_cache_t) over four tensors of the caller's: codes int8 [pages, kv_heads, page_tokens, head_dim] and scales
-    float32 [pages, kv_heads], for keys and for values.  Methods are the C calls tsq_cache_* with pointers filled in; they run on the tensors' device,
-    on `stream` or that device's current one, and raise TsqError where the call refuses its arguments."""
-
-    def __init__(self, dtype: torch.dtype, k_codes: torch.Tensor, v_codes: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
-        lib()
-        for name, t in (("k_codes", k_codes), ("v_codes", v_codes)):
-            assert t.is_cuda and t.is_contiguous() and t.dtype == torch.int8 and t.dim() == 4 and t.shape == k_codes.shape and t.device == k_codes.device, \
-                "%s must be a contiguous int8 CUDA tensor [pages, kv_heads, page_tokens, head_dim]" % name
-        pages, kv_heads, page_tokens, head_dim = k_codes.shape
-        for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
-            assert t.is_cuda and t.is_contiguous() and t.dtype == torch.float32 and tuple(t.shape) == (pages, kv_heads) and t.device == k_codes.device, \
-                "%s must be a contiguous float32 CUDA tensor [pages, kv_heads] on the codes' device" % name
-        self.dtype, self.pages, self.kv_heads, self.page_tokens, self.head_dim = dtype, pages, kv_heads, page_tokens, head_dim
-        self.k_codes, self.v_codes, self.k_scale, self.v_scale = k_codes, v_codes, k_scale, v_scale
-        self.device = k_codes.device.index
-        self._c = _CacheStruct(dtype_code(dtype), kv_heads, head_dim, page_tokens, pages, k_codes.data_ptr(), v_codes.data_ptr(),
-                               k_scale.data_ptr(), v_scale.data_ptr())
-        self._addr = C.addressof(self._c)
-        self._scale = head_dim ** -0.5 if head_dim else 1.0
-
-    @classmethod
-    def alloc(cls, dtype: torch.dtype, kv_heads: int, head_dim: int, pages: int, page_tokens: int = 64, device: int = 0) -> "Cache":
-        """A cache over tensors of its own, every code and scale 0."""
-        dev = torch.device("cuda", device)
-        codes = [torch.zeros((pages, kv_heads, page_tokens, head_dim), dtype=torch.int8, device=dev) for _ in range(2)]
-        scales = [torch.zeros((pages, kv_heads), dtype=torch.float32, device=dev) for _ in range(2)]
-        return cls(dtype, *codes, *scales)
+class _Paged:
+    """What the paged caches of either width have in common.  Methods are the C calls with pointers filled in; they run on the tensors' device, on `stream` or
+    that device's current one, and raise TsqError where the call refuses its arguments."""
+    _names = ("", "", "", "")         # the C calls: store, load, workspace, attention
 
     def store(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
-        st = _calls.cache_store(self._addr, self.device, k, v, slots, stream)
+        st = self._store(self._addr, self.device, k, v, slots, stream)
         if st != 0:
-            raise TsqError(st, "tsq_cache_store")
+            raise TsqError(st, self._names[0])
 
     def load(self, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
-        st = _calls.cache_load(self._addr, self.device, slots, k, v, stream)
+        st = self._load(self._addr, self.device, slots, k, v, stream)
         if st != 0:
-            raise TsqError(st, "tsq_cache_load")
+            raise TsqError(st, self._names[1])
 
     def workspace_bytes(self, tokens: int, q_heads: int, requests: int, max_query: int) -> int:
         out = C.c_size_t(0)
         with torch.cuda.device(self.device):
-            _check(lib().tsq_cache_workspace(C.byref(self._c), tokens, q_heads, requests, max_query, C.byref(out)), "tsq_cache_workspace")
+            _check(getattr(lib(), self._names[2])(C.byref(self._c), tokens, q_heads, requests, max_query, C.byref(out)), self._names[2])
         return int(out.value)
 
     def workspace(self, tokens: int, q_heads: int, requests: int, max_query: int) -> torch.Tensor:
@@ -304,13 +289,85 @@ class Cache:
             _check(lib().tsq_cache_workspace_status(ws.data_ptr(), C.byref(out), _stream(stream)), "tsq_cache_workspace_status")
         return int(out.value)
 
+
+class Cache(_Paged):
+    """The paged 8-bit key/value cache (tsq_cache_t) over four tensors of the caller's: codes int8 [pages, kv_heads, page_tokens, head_dim] and scales
+    float32 [pages, kv_heads], for keys and for values."""
+    _names = ("tsq_cache_store", "tsq_cache_load", "tsq_cache_workspace", "tsq_cache_attention")
+
+    def __init__(self, dtype: torch.dtype, k_codes: torch.Tensor, v_codes: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        lib()
+        for name, t in (("k_codes", k_codes), ("v_codes", v_codes)):
+            assert t.is_cuda and t.is_contiguous() and t.dtype == torch.int8 and t.dim() == 4 and t.shape == k_codes.shape and t.device == k_codes.device, \
+                "%s must be a contiguous int8 CUDA tensor [pages, kv_heads, page_tokens, head_dim]" % name
+        pages, kv_heads, page_tokens, head_dim = k_codes.shape
+        for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+            assert t.is_cuda and t.is_contiguous() and t.dtype == torch.float32 and tuple(t.shape) == (pages, kv_heads) and t.device == k_codes.device, \
+                "%s must be a contiguous float32 CUDA tensor [pages, kv_heads] on the codes' device" % name
+        self.dtype, self.pages, self.kv_heads, self.page_tokens, self.head_dim = dtype, pages, kv_heads, page_tokens, head_dim
+        self.k_codes, self.v_codes, self.k_scale, self.v_scale = k_codes, v_codes, k_scale, v_scale
+        self.device = k_codes.device.index
+        self._c = _CacheStruct(dtype_code(dtype), kv_heads, head_dim, page_tokens, pages, k_codes.data_ptr(), v_codes.data_ptr(),
+                               k_scale.data_ptr(), v_scale.data_ptr())
+        self._addr = C.addressof(self._c)
+        self._scale = head_dim ** -0.5 if head_dim else 1.0
+        self._store, self._load, self._attention = _calls.cache_store, _calls.cache_load, _calls.cache_attention
+
+    @classmethod
+    def alloc(cls, dtype: torch.dtype, kv_heads: int, head_dim: int, pages: int, page_tokens: int = 64, device: int = 0) -> "Cache":
+        """A cache over tensors of its own, every code and scale 0."""
+        dev = torch.device("cuda", device)
+        codes = [torch.zeros((pages, kv_heads, page_tokens, head_dim), dtype=torch.int8, device=dev) for _ in range(2)]
+        scales = [torch.zeros((pages, kv_heads), dtype=torch.float32, device=dev) for _ in range(2)]
+        return cls(dtype, *codes, *scales)
+
     def attention(self, q: torch.Tensor, query_start: torch.Tensor, lengths: torch.Tensor, block_table: torch.Tensor, out: torch.Tensor,
                   ws: torch.Tensor, max_query: int, scale: Optional[float] = None, stream=None) -> None:
         """scale: 1 / sqrt(head_dim) unless given."""
-        st = _calls.cache_attention(self._addr, self.device, q, query_start, lengths, block_table, out, ws, max_query,
-                                    self._scale if scale is None else scale, stream)
+        st = self._attention(self._addr, self.device, q, query_start, lengths, block_table, out, ws, max_query,
+                             self._scale if scale is None else scale, stream)
         if st != 0:
-            raise TsqError(st, "tsq_cache_attention")
+            raise TsqError(st, self._names[3])
+
+
+class Cache4(_Paged):
+    """The paged 4-bit key/value cache (tsq_cache4_t) over four tensors of the caller's: codes uint8 [pages, kv_heads, page_tokens, head_dim / 2], two to a byte, and a
+    word int32 [pages, kv_heads, page_tokens] with each token's scale and zero-point, for keys and for values."""
+    _names = ("tsq_cache4_store", "tsq_cache4_load", "tsq_cache4_workspace", "tsq_cache4_attention")
+
+    def __init__(self, dtype: torch.dtype, k_codes: torch.Tensor, v_codes: torch.Tensor, k_grid: torch.Tensor, v_grid: torch.Tensor):
+        lib()
+        for name, t in (("k_codes", k_codes), ("v_codes", v_codes)):
+            assert t.is_cuda and t.is_contiguous() and t.dtype == torch.uint8 and t.dim() == 4 and t.shape == k_codes.shape and t.device == k_codes.device, \
+                "%s must be a contiguous uint8 CUDA tensor [pages, kv_heads, page_tokens, head_dim / 2]" % name
+        pages, kv_heads, page_tokens, half = k_codes.shape
+        for name, t in (("k_grid", k_grid), ("v_grid", v_grid)):
+            assert t.is_cuda and t.is_contiguous() and t.dtype == torch.int32 and tuple(t.shape) == (pages, kv_heads, page_tokens) and t.device == k_codes.device, \
+                "%s must be a contiguous int32 CUDA tensor [pages, kv_heads, page_tokens] on the codes' device" % name
+        self.dtype, self.pages, self.kv_heads, self.page_tokens, self.head_dim = dtype, pages, kv_heads, page_tokens, 2 * half
+        self.k_codes, self.v_codes, self.k_grid, self.v_grid = k_codes, v_codes, k_grid, v_grid
+        self.device = k_codes.device.index
+        self._c = _Cache4Struct(dtype_code(dtype), kv_heads, 2 * half, page_tokens, pages, k_codes.data_ptr(), v_codes.data_ptr(),
+                                k_grid.data_ptr(), v_grid.data_ptr())
+        self._addr = C.addressof(self._c)
+        self._scale = (2 * half) ** -0.5 if half else 1.0
+        self._store, self._load, self._attention = _calls.cache4_store, _calls.cache4_load, _calls.cache4_attention
+
+    @classmethod
+    def alloc(cls, dtype: torch.dtype, kv_heads: int, head_dim: int, pages: int, page_tokens: int = 64, device: int = 0) -> "Cache4":
+        """A cache over tensors of its own, every code, scale and zero-point 0."""
+        dev = torch.device("cuda", device)
+        codes = [torch.zeros((pages, kv_heads, page_tokens, head_dim // 2), dtype=torch.uint8, device=dev) for _ in range(2)]
+        grids = [torch.zeros((pages, kv_heads, page_tokens), dtype=torch.int32, device=dev) for _ in range(2)]
+        return cls(dtype, *codes, *grids)
+
+    def attention(self, q: torch.Tensor, query_start: torch.Tensor, lengths: torch.Tensor, block_table: torch.Tensor, out: torch.Tensor,
+                  ws: torch.Tensor, max_query: int, scale: Optional[float] = None, causal: bool = True, stream=None) -> None:
+        """scale: 1 / sqrt(head_dim) unless given.  causal: False lets every row of a request see all of its lengths[i] tokens (cross attention)."""
+        st = self._attention(self._addr, self.device, q, query_start, lengths, block_table, out, ws, max_query,
+                             self._scale if scale is None else scale, causal, stream)
+        if st != 0:
+            raise TsqError(st, self._names[3])
 
 
 def cache_slots(page_tokens: int, held: torch.Tensor, added: torch.Tensor, free_pages: torch.Tensor, query_start: torch.Tensor,

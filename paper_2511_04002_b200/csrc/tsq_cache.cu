@@ -11,6 +11,91 @@
 #include "tsq_internal.h"
 
 namespace tsq {
+
+// ---- host side, shared with the 4-bit cache ------------------------------------------------------
+
+bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+int page_shift(int32_t page_tokens) {
+  for (int s = 4; s <= 7; ++s) {
+    if (page_tokens == 1 << s) return s;
+  }
+  return -1;
+}
+
+bool rows_fit(const void* x, long long stride, long long tokens, long long heads, int head_dim) {
+  return tokens == 0 || (x && aligned(x, 16) && stride % 8 == 0 && stride >= heads * head_dim);
+}
+
+int current_sms() {
+  static std::atomic<int> known[kMaxDevices];
+  int device = 0;
+  if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= kMaxDevices) return 0;
+  int n = known[device].load(std::memory_order_relaxed);
+  if (n == 0) {
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return 0;
+    known[device].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
+tsq_status_t launched(cudaError_t e) {
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    return TSQ_ERR_CUDA;
+  }
+  count_launch();
+  return TSQ_OK;
+}
+
+// Workspace: 16 bytes with the status, the counters of either kernel, the slots of sums.
+static size_t workspace_head(int sms) { return static_cast<size_t>(align16(16ull + 4ull * sms * std::max(kRowsCtasPerSm * kRowsCounters, kTilesCounters))); }
+size_t attention_workspace_size(int sms, int head_dim, bool few) {
+  const unsigned long long rows = few ? 1ull * kRowsCtasPerSm * kRowsSlots * kRowsTile : 128ull * kTilesSlots;
+  return workspace_head(sms) + static_cast<size_t>(align16(4ull * rows * sms * (head_dim + 2)));
+}
+
+tsq_status_t check_attention_sizes(int32_t kv_heads, int64_t tokens, int32_t q_heads, int32_t requests, int32_t max_query) {
+  if (tokens < 0 || tokens > kMaxSlots || requests < 0 || max_query < 1 || q_heads < 1 || q_heads % kv_heads != 0) return TSQ_ERR_INVALID_ARG;
+  const int group = q_heads / kv_heads;
+  return group > 64 || requests > kMaxRequests || tokens * group > kMaxSlots ? TSQ_ERR_UNSUPPORTED : TSQ_OK;
+}
+
+constexpr float kMostScale = 2.0e38f;  // times log2(e) still finite
+
+// The arguments beside the cache, whose sizes check_attention_sizes has passed; TSQ_OK with 0 requests or tokens leaves nothing to do.
+tsq_status_t check_attention(const AttentionCall& a, int head_dim) {
+  if (a.table_pages < 0 || !(std::fabs(a.scale) <= kMostScale) || !a.ws_dev || !aligned(a.ws_dev, 16)) return TSQ_ERR_INVALID_ARG;
+  if (a.requests > 0 && (!a.query_start || !a.lengths || (a.table_pages > 0 && !a.block_table))) return TSQ_ERR_INVALID_ARG;
+  if (!aligned(a.query_start, 4) || !aligned(a.lengths, 4) || !aligned(a.block_table, 4)) return TSQ_ERR_INVALID_ARG;
+  if (!rows_fit(a.q, a.q_stride, a.tokens, a.q_heads, head_dim) || !rows_fit(a.out, a.out_stride, a.tokens, a.q_heads, head_dim)) return TSQ_ERR_INVALID_ARG;
+  return TSQ_OK;
+}
+
+void fill_attention(const AttentionCall& a, int32_t kv_heads, int64_t pages, int page_tokens, int sms, AttentionParams& p) {
+  std::memset(&p, 0, sizeof p);
+  p.q = a.q;
+  p.out = a.out;
+  p.query_start = a.query_start;
+  p.lengths = a.lengths;
+  p.table = a.block_table;
+  p.q_stride = a.q_stride;
+  p.out_stride = a.out_stride;
+  p.tokens = a.tokens;
+  p.requests = a.requests;
+  p.pages = static_cast<int32_t>(pages);
+  p.page_shift = page_shift(page_tokens);
+  p.table_pages = a.table_pages;
+  p.kv_heads = kv_heads;
+  p.group = a.q_heads / kv_heads;
+  p.max_query = a.max_query;
+  p.causal = -1;
+  p.scale_log2 = a.scale * 1.4426950408889634f;
+  p.status = static_cast<unsigned int*>(a.ws_dev);
+  p.counters = p.status + 4;
+  p.partials = reinterpret_cast<float*>(static_cast<unsigned char*>(a.ws_dev) + workspace_head(sms));
+}
+
 namespace {
 
 // ---- block tables and slots ----------------------------------------------------------------------
@@ -423,18 +508,6 @@ __global__ void __launch_bounds__(kLoadThreads) load_kernel(const LoadParams p) 
 
 // ---- host side -----------------------------------------------------------------------------------
 
-constexpr int kMaxSlots = 0x7fffffff;
-constexpr float kMostScale = 2.0e38f;  // times log2(e) still finite
-
-bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-
-int page_shift(int32_t page_tokens) {
-  for (int s = 4; s <= 7; ++s) {
-    if (page_tokens == 1 << s) return s;
-  }
-  return -1;
-}
-
 tsq_status_t check_cache(const tsq_cache_t* c) {
   if (!c || (c->dtype != TSQ_F16 && c->dtype != TSQ_BF16) || c->kv_heads < 1 || c->head_dim < 1 || c->page_tokens < 1 || c->pages < 1)
     return TSQ_ERR_INVALID_ARG;
@@ -443,34 +516,6 @@ tsq_status_t check_cache(const tsq_cache_t* c) {
   if ((c->head_dim != 64 && c->head_dim != 128) || page_shift(c->page_tokens) < 0) return TSQ_ERR_UNSUPPORTED;
   if (c->kv_heads > 1024) return TSQ_ERR_UNSUPPORTED;
   if (c->pages > kMaxSlots / c->page_tokens) return TSQ_ERR_INVALID_ARG;
-  return TSQ_OK;
-}
-
-// Rows of `heads` heads with `stride` elements between tokens.
-bool rows_fit(const void* x, long long stride, long long tokens, long long heads, int head_dim) {
-  return tokens == 0 || (x && aligned(x, 16) && stride % 8 == 0 && stride >= heads * head_dim);
-}
-
-// SMs of the current device, asked for once per device.
-int current_sms() {
-  static std::atomic<int> known[kMaxDevices];
-  int device = 0;
-  if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= kMaxDevices) return 0;
-  int n = known[device].load(std::memory_order_relaxed);
-  if (n == 0) {
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return 0;
-    known[device].store(n, std::memory_order_relaxed);
-  }
-  return n;
-}
-
-// The result of a launch; a failed one leaves nothing behind for the caller's own error checks.
-tsq_status_t launched(cudaError_t e) {
-  if (e != cudaSuccess) {
-    cudaGetLastError();
-    return TSQ_ERR_CUDA;
-  }
-  count_launch();
   return TSQ_OK;
 }
 
@@ -484,17 +529,11 @@ cudaError_t launch_store(const StoreParams& p, int shift, int grid, cudaStream_t
   }
 }
 
-// Workspace: 16 bytes with the status, the counters of either kernel, the slots of sums.
 // Which kernel: by the query rows that a key head's codes serve at most.  The row kernel reads the codes again for every 16 rows; the tile kernel takes
 // 256 at once, at a step's price whether they are there or not.  us, rows / tiles (bf16, heads of 128, codes in HBM): 16 requests of 8000 keys, 8 key heads,
 // 24 and 32 rows 119 / 158, 48 rows 170 / 158, 64 rows 213 / 158; 64 of 2000 keys 24 rows 123 / 176, 48 rows 176 / 178; 1 of 100000 keys 32 rows 113 / 158, 64 rows 180 / 160;
 // 16 of 3000 keys, 40 key heads, 20 rows 209 / 285, 40 rows 301 / 291.
 bool few_query_rows(long long max_query, int group) { return max_query * group <= kFewQueryRows; }
-size_t workspace_head(int sms) { return static_cast<size_t>(align16(16ull + 4ull * sms * std::max(kRowsCtasPerSm * kRowsCounters, kTilesCounters))); }
-size_t workspace_size(int sms, int head_dim, bool few) {
-  const unsigned long long rows = few ? 1ull * kRowsCtasPerSm * kRowsSlots * kRowsTile : 128ull * kTilesSlots;
-  return workspace_head(sms) + static_cast<size_t>(align16(4ull * rows * sms * (head_dim + 2)));
-}
 
 }  // namespace
 }  // namespace tsq
@@ -619,21 +658,14 @@ tsq_status_t tsq_cache_load(const tsq_cache_t* cache, const int32_t* slots, int6
   return launched(e);
 }
 
-static tsq_status_t check_attention_sizes(const tsq_cache_t* cache, int64_t tokens, int32_t q_heads, int32_t requests, int32_t max_query) {
-  const tsq_status_t fine = check_cache(cache);
-  if (fine != TSQ_OK) return fine;
-  if (tokens < 0 || tokens > kMaxSlots || requests < 0 || max_query < 1 || q_heads < 1 || q_heads % cache->kv_heads != 0) return TSQ_ERR_INVALID_ARG;
-  const int group = q_heads / cache->kv_heads;
-  return group > 64 || requests > kMaxRequests || tokens * group > kMaxSlots ? TSQ_ERR_UNSUPPORTED : TSQ_OK;
-}
-
 tsq_status_t tsq_cache_workspace(const tsq_cache_t* cache, int64_t tokens, int32_t q_heads, int32_t requests, int32_t max_query, size_t* workspace_bytes) {
   if (!workspace_bytes) return TSQ_ERR_INVALID_ARG;
-  const tsq_status_t fine = check_attention_sizes(cache, tokens, q_heads, requests, max_query);
+  tsq_status_t fine = check_cache(cache);
+  if (fine == TSQ_OK) fine = check_attention_sizes(cache->kv_heads, tokens, q_heads, requests, max_query);
   if (fine != TSQ_OK) return fine;
   const int sms = current_sms();
   if (sms < 1) return launched(cudaErrorInvalidDevice);
-  *workspace_bytes = workspace_size(sms, cache->head_dim, few_query_rows(max_query, q_heads / cache->kv_heads));
+  *workspace_bytes = attention_workspace_size(sms, cache->head_dim, few_query_rows(max_query, q_heads / cache->kv_heads));
   return TSQ_OK;
 }
 
@@ -652,42 +684,22 @@ tsq_status_t tsq_cache_workspace_init(void* ws_dev, size_t ws_bytes, void* cuda_
 tsq_status_t tsq_cache_attention(const tsq_cache_t* cache, const void* q, int64_t q_stride, int32_t q_heads, int64_t tokens, const int32_t* query_start,
                                  const int32_t* lengths, int32_t requests, int32_t max_query, const int32_t* block_table, int32_t table_pages, float scale,
                                  void* out, int64_t out_stride, void* ws_dev, size_t ws_bytes, void* cuda_stream) {
-  const tsq_status_t fine = check_attention_sizes(cache, tokens, q_heads, requests, max_query);
+  const AttentionCall a = {q, q_stride, tokens, q_heads, query_start, lengths, requests, max_query, block_table, table_pages, scale, out, out_stride, ws_dev, ws_bytes};
+  tsq_status_t fine = check_cache(cache);
+  if (fine == TSQ_OK) fine = check_attention_sizes(cache->kv_heads, tokens, q_heads, requests, max_query);
+  if (fine == TSQ_OK) fine = check_attention(a, cache->head_dim);
   if (fine != TSQ_OK) return fine;
-  if (table_pages < 0 || !(std::fabs(scale) <= kMostScale) || !ws_dev || !aligned(ws_dev, 16)) return TSQ_ERR_INVALID_ARG;
-  if (requests > 0 && (!query_start || !lengths || (table_pages > 0 && !block_table))) return TSQ_ERR_INVALID_ARG;
-  if (!aligned(query_start, 4) || !aligned(lengths, 4) || !aligned(block_table, 4)) return TSQ_ERR_INVALID_ARG;
-  if (!rows_fit(q, q_stride, tokens, q_heads, cache->head_dim) || !rows_fit(out, out_stride, tokens, q_heads, cache->head_dim)) return TSQ_ERR_INVALID_ARG;
   const int sms = current_sms();
   if (sms < 1) return launched(cudaErrorInvalidDevice);
   const bool few = few_query_rows(max_query, q_heads / cache->kv_heads);
-  if (ws_bytes < workspace_size(sms, cache->head_dim, few)) return TSQ_ERR_BUFFER_TOO_SMALL;
+  if (ws_bytes < attention_workspace_size(sms, cache->head_dim, few)) return TSQ_ERR_BUFFER_TOO_SMALL;
   if (requests == 0 || tokens == 0) return TSQ_OK;
   AttentionParams p;
-  std::memset(&p, 0, sizeof p);
-  p.q = q;
-  p.out = out;
-  p.query_start = query_start;
-  p.lengths = lengths;
-  p.table = block_table;
+  fill_attention(a, cache->kv_heads, cache->pages, cache->page_tokens, sms, p);
   p.k_codes = cache->k_codes;
   p.v_codes = cache->v_codes;
   p.k_scale = cache->k_scale;
   p.v_scale = cache->v_scale;
-  p.q_stride = q_stride;
-  p.out_stride = out_stride;
-  p.tokens = tokens;
-  p.requests = requests;
-  p.pages = static_cast<int32_t>(cache->pages);
-  p.page_shift = page_shift(cache->page_tokens);
-  p.table_pages = table_pages;
-  p.kv_heads = cache->kv_heads;
-  p.group = q_heads / cache->kv_heads;
-  p.max_query = max_query;
-  p.scale_log2 = scale * 1.4426950408889634f;
-  p.status = static_cast<unsigned int*>(ws_dev);
-  p.counters = p.status + 4;
-  p.partials = reinterpret_cast<float*>(static_cast<unsigned char*>(ws_dev) + workspace_head(sms));
   const bool bf16 = cache->dtype == TSQ_BF16;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   return launched(few ? launch_attention_rows(p, bf16, cache->head_dim, sms, st) : launch_attention_tiles(p, bf16, cache->head_dim, sms, st));

@@ -1,4 +1,4 @@
-// Device-side parts that the kernels of attention over the paged 8-bit cache share.
+// Device-side parts that the kernels of attention over the paged caches share.
 #ifndef TSQ_CACHE_DEVICE_CUH_
 #define TSQ_CACHE_DEVICE_CUH_
 
@@ -15,12 +15,22 @@ constexpr float kLeastScale = 8.673617379884035e-19f;  // 2^-60
 __device__ __forceinline__ float log2_of_scale(float s) { return s != s ? s : __log2f(fmaxf(s, kLeastScale)); }
 __device__ __forceinline__ float inverse_of_scale(float s) { return 1.0f / fmaxf(s, kLeastScale); }
 
+// A word of the 4-bit cache's grids: the scale, a bfloat16 number, in the lower half, the zero-point, signed, in the upper one.
+__device__ __forceinline__ float grid_scale(uint32_t word) { return __uint_as_float(word << 16); }
+__device__ __forceinline__ float grid_zero(uint32_t word) { return static_cast<float>(static_cast<int32_t>(word) >> 16); }
+__device__ __forceinline__ bool grid_is_number(uint32_t word) { return (word & 0x7f80u) != 0x7f80u; }
+// The largest magnitude that a code of the token may stand for; 0 where the scale is no number.
+__device__ __forceinline__ float grid_top(uint32_t word) {
+  const float zero = grid_zero(word);
+  return grid_is_number(word) ? fabsf(grid_scale(word)) * fmaxf(fabsf(zero), fabsf(zero + 15.0f)) : 0.0f;
+}
+
 // A request as the kernels read it: every number is brought into the range of the arrays first.
 struct Request {
   long long start;   // first row
   int rows;          // rows that are written
   int keys;          // keys that can be seen: within the table
-  long long before;  // position of row 0 (negative: rows that see nothing)
+  long long before;  // position of row 0 (negative: rows that see nothing); the length, where every row sees all keys
 
   __device__ __forceinline__ int tiles(int tile, const AttentionParams& p) const {
     return static_cast<int>((static_cast<long long>(rows) * p.group + tile - 1) / tile);
@@ -42,7 +52,7 @@ __device__ __forceinline__ Request request_of(const AttentionParams& p, int i) {
   r.start = begin;
   r.rows = static_cast<int>(min(end - begin, static_cast<long long>(p.max_query)));
   r.keys = static_cast<int>(min(min(length, static_cast<long long>(p.table_pages) << p.page_shift), 0x7ffff000ll));  // a step further stays an int
-  r.before = length - (end - begin);
+  r.before = length - ((end - begin) & p.causal);
   return r;
 }
 

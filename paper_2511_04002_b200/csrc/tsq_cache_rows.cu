@@ -2,63 +2,17 @@
 
 #include "tsq_cache.h"
 #include "tsq_cache_device.cuh"
+#include "tsq_cache_rows.cuh"
 #include "tsq_device.cuh"
 #include "tsq_internal.h"
 
 namespace tsq {
 namespace {
 
-constexpr int kWarps = 4;
-constexpr int kThreads = 32 * kWarps;
+constexpr int kWarps = kRowsWarps, kThreads = kRowsThreads;
 constexpr int kStepTokens = 16;              // tokens of a warp's step: within one page
 constexpr int kUnitTokens = kWarps * kStepTokens;
-constexpr int kFanIn = 16;                   // parts of a tile that are added up at once
 constexpr int kTileUnits = 2;                // what beginning and ending a tile costs, in units
-
-// One m16n8k16 product, binary16 in, binary32 sums.
-__device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint4 lds128(uint32_t at) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
-  return v;
-}
-__device__ __forceinline__ float4 lds128f(uint32_t at) {
-  float4 v;
-  asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at));
-  return v;
-}
-// An 8 x 8 block of binary16 numbers, a row's two neighbours in each thread, transposed.
-__device__ __forceinline__ uint32_t transposed(uint32_t v) {
-  uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
-  return r;
-}
-// Over the eight threads that have the same columns.
-__device__ __forceinline__ float column_max(float v) {
-  v = fmaxf(v, __shfl_xor_sync(kFull, v, 4));
-  v = fmaxf(v, __shfl_xor_sync(kFull, v, 8));
-  return fmaxf(v, __shfl_xor_sync(kFull, v, 16));
-}
-__device__ __forceinline__ float column_sum(float v) {
-  v += __shfl_xor_sync(kFull, v, 4);
-  v += __shfl_xor_sync(kFull, v, 8);
-  return v + __shfl_xor_sync(kFull, v, 16);
-}
-__device__ __forceinline__ uint2 lds64(uint32_t at) {
-  uint2 v;
-  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
-  return v;
-}
-__device__ __forceinline__ void copy16(uint32_t smem, const void* gmem) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(gmem) : "memory");
-}
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // Where the 16-byte chunk `c` of token row `t` lies in a stage: chunks change places by row, so that the four rows and two chunks that eight
 // lanes read at once lie in different banks.
@@ -67,19 +21,6 @@ __device__ __forceinline__ int placed(int t, int c) {
   return D == 128 ? t * 128 + ((c ^ (t & 7)) << 4) : t * 64 + ((c ^ ((t >> 1) & 3)) << 4);
 }
 
-// The B operands of the products with the keys: thread (g, c) has of the rows row0 + 8 t + g of the tile (zeros past its `rows`) the dimensions
-// c * D / 4 ... in order, four per product step.  As they lie in memory:
-template <int D, int NT>
-__device__ __forceinline__ void read_queries(const AttentionParams& p, const Request& r, int head, int row0, int rows, int g, int c, uint4 (&raw)[NT][D / 32]) {
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int row = 8 * t + g, at = row0 + row;
-    const uint16_t* const from = static_cast<const uint16_t*>(p.q) + (r.start + at / p.group) * p.q_stride +
-                                 (static_cast<long long>(head) * p.group + at % p.group) * D + c * (D / 4);
-#pragma unroll
-    for (int k = 0; k < D / 32; ++k) raw[t][k] = row < rows ? reinterpret_cast<const uint4*>(from)[k] : make_uint4(0u, 0u, 0u, 0u);
-  }
-}
 // brought to binary16 by a power of two per row.  factor: the inverses for the rows 8 t + 2 c and 8 t + 2 c + 1.
 template <bool BF16, int D, int NT>
 __device__ __forceinline__ void scale_queries(const uint4 (&raw)[NT][D / 32], int c, uint32_t (&q)[NT][D / 16][2], float (&factor)[NT][2]) {
@@ -115,9 +56,7 @@ struct Layout {
   static constexpr int kHalf = kStepTokens * D;          // bytes of a stage's keys, and of its values
   static constexpr int kStage = 2 * kHalf;
   static constexpr int kRing = kStages * kStage;         // of a warp
-  static constexpr int kRowFloats = D + 36;              // a row of a warp's sums: four floats more behind each eighth, and four at the end
-  static constexpr int kSums = kWarps * kRows * kRowFloats * 4;
-  static constexpr int kMerge = kSums + kWarps * kRows * 8;
+  static constexpr int kMerge = RowsSums<D, NT>::kBytes;
   static constexpr int kScales = kWarps * kRing > kMerge ? kWarps * kRing : kMerge;  // 64 steps' factors for each warp
   static constexpr int kBytes = kScales + kWarps * 64 * 16;
 };
@@ -142,77 +81,23 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
   constexpr int kSteps = D / 16;                          // of the products with the keys
   constexpr int kTiles = D / 16;                          // of the sums, 16 dimensions each
   extern __shared__ __align__(128) unsigned char smem[];
-  __shared__ unsigned long long s_scan[kWarps];
-  __shared__ int s_found;
-  __shared__ unsigned int s_status;
-  __shared__ unsigned long long s_begin;
-  __shared__ unsigned int s_last;
   launch_dependents();
   wait_for_prior_grids();
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, c = lane % 4;
-  const unsigned int status = *static_cast<volatile unsigned int*>(p.status);  // one thread's is used, behind a barrier: on its way with the requests
-
-  // the CTA's share, and the request that has its first unit: every thread sums its requests' units, and the one whose sums reach past the first unit tells the others
-  unsigned long long total, unit, unit_end;
-  unsigned int ctas;
-  {
-    const int per = (p.requests + kThreads - 1) / kThreads;
-    const int i0 = min(tid * per, p.requests), i1 = min(i0 + per, p.requests);
-    unsigned long long mine = 0, n = 0;
-    for (int i = i0; i < i1; ++i) {
-      n = request_of(p, i).units(L::kRows, kUnitTokens, kTileUnits, p);
-      mine += n;
-    }
-    unsigned long long in = mine;
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-      const unsigned long long up = __shfl_up_sync(kFull, in, d);
-      if (lane >= d) in += up;
-    }
-    if (lane == 31) s_scan[warp] = in;
-    if (tid == 0) {
-      s_found = 0;
-      s_status = status;
-      s_begin = 0;
-    }
-    __syncthreads();
-    unsigned long long at = in - mine;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      if (w < warp) at += s_scan[w];
-      total += s_scan[w];
-    }
-    ctas = total < gridDim.x ? static_cast<unsigned int>(total) : gridDim.x;
-    if (blockIdx.x >= ctas || s_status != TSQ_OK) return;
-    unit = scaled(blockIdx.x, total, ctas);
-    unit_end = scaled(blockIdx.x + 1, total, ctas);
-    if (at <= unit && unit < at + mine) {
-      for (int i = i0; i < i1; ++i) {
-        if (per > 1) n = request_of(p, i).units(L::kRows, kUnitTokens, kTileUnits, p);
-        if (unit < at + n) {
-          s_found = i;
-          s_begin = at;
-          break;
-        }
-        at += n;
-      }
-    }
-    __syncthreads();
-  }
-  int i = s_found;
-  unsigned long long rest = unit - s_begin;               // units of request i in front of `unit`
+  Share work;
+  if (!share_of<L::kRows, kUnitTokens, kTileUnits>(p, work)) return;
+  int i = work.request;
   Request r = request_of(p, i);
   const uint32_t ring = smem_addr(smem) + warp * L::kRing, scales = smem_addr(smem) + L::kScales + warp * (64 * 16);
 
-  while (unit < unit_end) {
+  while (work.unit < work.end) {
     const int tiles = r.tiles(L::kRows, p), keys = r.key_units(kUnitTokens), span = keys + kTileUnits;
-    const int head_tile = static_cast<int>(scaled(1, rest, span)), head = head_tile / tiles, tile = head_tile % tiles;
-    const int from = static_cast<int>(rest - static_cast<unsigned long long>(head_tile) * span), upto = static_cast<int>(min(static_cast<unsigned long long>(span), from + (unit_end - unit)));
+    const int head_tile = static_cast<int>(scaled(1, work.rest, span)), head = head_tile / tiles, tile = head_tile % tiles;
+    const int from = static_cast<int>(work.rest - static_cast<unsigned long long>(head_tile) * span), upto = static_cast<int>(min(static_cast<unsigned long long>(span), from + (work.end - work.unit)));
     const int k0 = max(0, from - kTileUnits), k1 = max(0, upto - kTileUnits);
-    const unsigned long long tile_begin = unit - from;
-    unit += upto - from;
-    rest += upto - from;
+    const unsigned long long tile_begin = work.unit - from;
+    work.unit += upto - from;
+    work.rest += upto - from;
     if (k1 > k0) {
       const int row0 = tile * L::kRows, rows = min(L::kRows, r.rows * p.group - row0);
       // keys that the tile's first and last rows see
@@ -412,127 +297,14 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
         }
       }
 
-      // ---- the four warps' sums ----
-      copies_wait<0>();
-      __syncthreads();                                      // every warp has read its stages
-      float* const sums = reinterpret_cast<float*>(smem);
-      float2* const stats = reinterpret_cast<float2*>(smem + L::kSums);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int row = warp * L::kRows + 8 * t + 2 * c + h;
-          const float all = column_sum(l[t][h]);
-          if (g == 0) stats[row] = make_float2(m[t][h], all);
-          float* const at = sums + row * L::kRowFloats + g * (D / 8 + 4);
-#pragma unroll
-          for (int d = 0; d < kTiles; d += 2) *reinterpret_cast<float4*>(at + 2 * d) = make_float4(acc[t][d][h], acc[t][d][2 + h], acc[t][d + 1][h], acc[t][d + 1][2 + h]);
-        }
-      }
-      __syncthreads();
-      constexpr int kParts = kThreads / L::kRows, kDims = D / kParts;  // threads of a row, and what each has of it
-      const int row = tid / kParts, d0 = tid % kParts * kDims, padded = d0 + d0 / (D / 8) * 4;
-      float o[kDims], top = -INFINITY, all = 0.0f;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, stats[w * L::kRows + row].x);
-#pragma unroll
-      for (int d = 0; d < kDims; ++d) o[d] = 0.0f;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float2 st = stats[w * L::kRows + row];
-        const float by = st.x == -INFINITY ? 0.0f : exp2_fast(st.x - top);
-        all += st.y * by;
-        const float* const at = sums + (w * L::kRows + row) * L::kRowFloats + padded;
-#pragma unroll
-        for (int d = 0; d < kDims; d += 4) {
-          const float4 f4 = *reinterpret_cast<const float4*>(at + d);
-          o[d] += f4.x * by;
-          o[d + 1] += f4.y * by;
-          o[d + 2] += f4.z * by;
-          o[d + 3] += f4.w * by;
-        }
-      }
-      bool write = true;
-      if (k0 > 0 || k1 < keys) {                            // other CTAs have units of this tile
-        // Parts are added up sixteen at a time by the CTA that comes last of the sixteen, their sums likewise: the order does not depend on who comes when.
-        const int first = owner_of(tile_begin + kTileUnits, total, ctas), parts = owner_of(tile_begin + span - 1, total, ctas) - first + 1;
-        constexpr int kSlot = L::kRows * (D + 2);
-        const auto slot_of = [&](int n) { return p.partials + (2ll * (first + n) + (n == 0 ? 1 : 0)) * kSlot; };
-        int part = static_cast<int>(blockIdx.x) - first;
-        unsigned int* counters = p.counters;
-        for (int stride = 1; stride < parts && write; stride *= kFanIn, counters += gridDim.x) {
-          const int begin = part / (kFanIn * stride) * (kFanIn * stride), members = min(kFanIn, (parts - begin + stride - 1) / stride);
-          if (members > 1) {
-            float* const mine = slot_of(part);
-            if (row < rows) {
-#pragma unroll
-              for (int d = 0; d < kDims; d += 4) *reinterpret_cast<float4*>(mine + row * D + d0 + d) = make_float4(o[d], o[d + 1], o[d + 2], o[d + 3]);
-              if (d0 == 0) *reinterpret_cast<float2*>(mine + L::kRows * D + 2 * row) = make_float2(top, all);
-            }
-            __syncthreads();
-            if (tid == 0) s_last = count_arrival(counters + first + begin, static_cast<unsigned>(members - 1)) == static_cast<unsigned>(members - 1);
-            __syncthreads();
-            write = s_last != 0u;
-            if (write && row < rows) {
-              // loads without a branch between them, so that many are on their way: past the last part its data again, with weight 0
-              const auto part_at = [&](int n) { return slot_of(begin + min(n, members - 1) * stride); };
-              float2 st[kFanIn];
-#pragma unroll
-              for (int n = 0; n < kFanIn; ++n) st[n] = __ldcg(reinterpret_cast<const float2*>(part_at(n) + L::kRows * D) + row);
-              top = -INFINITY;
-#pragma unroll
-              for (int n = 0; n < kFanIn; ++n) {
-                if (n >= members) st[n] = make_float2(-INFINITY, 0.0f);
-                top = fmaxf(top, st[n].x);
-              }
-              all = 0.0f;
-#pragma unroll
-              for (int d = 0; d < kDims; ++d) o[d] = 0.0f;
-              constexpr int kBatch = 64 / kDims < kFanIn ? 64 / kDims : kFanIn;
-#pragma unroll
-              for (int n0 = 0; n0 < kFanIn; n0 += kBatch) {
-                if (n0 >= members) break;
-                float4 x[kBatch][kDims / 4];
-#pragma unroll
-                for (int n = 0; n < kBatch; ++n) {
-#pragma unroll
-                  for (int d = 0; d < kDims / 4; ++d) x[n][d] = __ldcg(reinterpret_cast<const float4*>(part_at(n0 + n) + row * D + d0) + d);
-                }
-#pragma unroll
-                for (int n = 0; n < kBatch; ++n) {
-                  const float by = st[n0 + n].x == -INFINITY ? 0.0f : exp2_fast(st[n0 + n].x - top);
-                  all = __fmaf_rn(st[n0 + n].y, by, all);
-#pragma unroll
-                  for (int d = 0; d < kDims / 4; ++d) {
-                    o[4 * d] = __fmaf_rn(x[n][d].x, by, o[4 * d]);
-                    o[4 * d + 1] = __fmaf_rn(x[n][d].y, by, o[4 * d + 1]);
-                    o[4 * d + 2] = __fmaf_rn(x[n][d].z, by, o[4 * d + 2]);
-                    o[4 * d + 3] = __fmaf_rn(x[n][d].w, by, o[4 * d + 3]);
-                  }
-                }
-              }
-            }
-            __syncthreads();                                // every thread has read what the next level writes over
-          }
-          part = begin;
-        }
-      }
-      write = write && row < rows;
-      if (write) {
-        const float by = all == 0.0f ? 0.0f : 1.0f / all;
-        const int at = row0 + row;
-        uint16_t* const to = static_cast<uint16_t*>(p.out) + (r.start + at / p.group) * p.out_stride + (static_cast<long long>(head) * p.group + at % p.group) * D + d0;
-#pragma unroll
-        for (int d = 0; d < kDims; d += 4)
-          *reinterpret_cast<uint2*>(to + d) = make_uint2(Elem<BF16>::pack_rn(o[d] * by, o[d + 1] * by), Elem<BF16>::pack_rn(o[d + 2] * by, o[d + 3] * by));
-      }
+      finish_tile<BF16, D, NT>(p, work, r, head, row0, rows, k0 > 0 || k1 < keys, tile_begin + kTileUnits, tile_begin + span - 1, smem, m, l, acc);
     }
-    if (unit < unit_end && rest == r.units(L::kRows, kUnitTokens, kTileUnits, p)) {
+    if (work.unit < work.end && work.rest == r.units(L::kRows, kUnitTokens, kTileUnits, p)) {
       do {
         r = request_of(p, ++i);
       } while (r.rows == 0 && i + 1 < p.requests);
       if (r.rows == 0) break;                             // not reached while units are left
-      rest = 0;
+      work.rest = 0;
     }
   }
 }

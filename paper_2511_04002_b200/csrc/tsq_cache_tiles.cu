@@ -1,4 +1,4 @@
-// Attention over the paged 8-bit cache for many query rows per request (prompts, chunks of prompts), on the tensor cores' asynchronous products.
+// Attention over the paged caches, of 8 or 4 bits, for many query rows per request (prompts, chunks of prompts), on the tensor cores' asynchronous products.
 
 #include "tsq_cache.h"
 #include "tsq_cache_device.cuh"
@@ -195,6 +195,20 @@ __device__ __forceinline__ void store_sector(void* at, const uint32_t (&w)[8], b
   }
 }
 
+// The column of an operand in which a dimension lies.  8 bits: its own.  4 bits: the nibbles of a word come out in pairs (0, 4), (1, 5), (2, 6), (3, 7), and stay there: keys and queries
+// have the same order, and the sums' columns are put back when a row is written.
+template <int BITS>
+__host__ __device__ constexpr int nibble_column(int d) { return BITS == 8 ? d : (d & ~7) | (d & 3) << 1 | (d >> 2 & 1); }
+
+// The eight codes of a word plus their token's zero-point, exact in binary16, times its scale (in both halves): 0x6400 | nibble is 1024 + code, or 1024 + 16 code = 16 (64 + code).
+__device__ __forceinline__ uint4 widen_nibbles(uint32_t w, __half2 less_even, __half2 less_odd, __half2 scale) {
+  const auto even = [&](uint32_t u) { return Elem<false>::bits(__hmul2(__hadd2(Elem<false>::as2((u & 0x000f000fu) | 0x64006400u), less_even), scale)); };
+  const auto odd = [&](uint32_t u) {
+    return Elem<false>::bits(__hmul2(__hfma2(Elem<false>::as2((u & 0x00f000f0u) | 0x64006400u), __float2half2_rn(0.0625f), less_odd), scale));
+  };
+  return make_uint4(even(w), odd(w), even(w >> 8), odd(w >> 8));
+}
+
 // Shared-memory descriptors of 128-byte swizzled operands: rows of 128 bytes, eight rows to a 1024-byte atom.
 // K-major (queries, keys): atoms follow one another down the rows.  MN-major (values: a row is a token, its 64 dimensions contiguous): atoms follow
 // one another along the tokens, the second 64 dimensions lie kHalf bytes behind.
@@ -310,7 +324,11 @@ __host__ __device__ constexpr uint32_t arrivals_of(int bar) {  // a group's warp
 // order of the steps.
 // Bound by the chain scores -> weights -> sums -> scores of each group: about 4400 clocks a step where the products take 2050 and the exponentials, 16 per SM and clock, as many.
 // 8192 tokens, 32 query heads on 8 key heads: 600 to 634 us, 865 to 910 TFLOP/s (bf16 or fp16, heads of 128), at the 1.55 GHz that the power cap leaves.
-template <bool BF16, int D>
+//
+// BITS = 4: a token has a scale and a zero-point of its own, which the widening groups apply: (code + zero-point) * scale is a whole number of at most 11 bits as long as the
+// range of the token reaches 0, and so exact in binary16 (otherwise rounded once, 2^-12).  Scales are taken relative to a granule's largest number, a power of two that takes the place of the
+// page's scale: what the softmax and product warps do is the same for both widths.
+template <bool BF16, int D, int BITS>
 __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const AttentionParams p) {
   using Sh = Shared<D>;
   extern __shared__ unsigned char smem_raw[];
@@ -488,8 +506,16 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
       for (int k = 0; k < D / 8; ++k) {
         const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
         uint32_t h[4];
+        if constexpr (BITS == 8) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) h[e] = pack_half2(Elem<BF16>::lo_f32(w[e]) * sign, Elem<BF16>::hi_f32(w[e]) * sign);
+          for (int e = 0; e < 4; ++e) h[e] = pack_half2(Elem<BF16>::lo_f32(w[e]) * sign, Elem<BF16>::hi_f32(w[e]) * sign);
+        } else {                                           // in the order of nibble_column
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            h[2 * e] = pack_half2(Elem<BF16>::lo_f32(w[e]) * sign, Elem<BF16>::lo_f32(w[e + 2]) * sign);
+            h[2 * e + 1] = pack_half2(Elem<BF16>::hi_f32(w[e]) * sign, Elem<BF16>::hi_f32(w[e + 2]) * sign);
+          }
+        }
         *reinterpret_cast<uint4*>(q_at + (k / 8) * kHalf + (((k % 8) ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
       }
       fence_proxy_async_smem();
@@ -590,7 +616,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
             for (int e = 0; e < 32; e += 16) {
               uint32_t w[8];
 #pragma unroll
-              for (int k = 0; k < 8; ++k) w[k] = Elem<BF16>::pack_rn(__uint_as_float(o[e + 2 * k]) * by, __uint_as_float(o[e + 2 * k + 1]) * by);
+              for (int k = 0; k < 8; ++k)
+                w[k] = Elem<BF16>::pack_rn(__uint_as_float(o[e + nibble_column<BITS>(2 * k)]) * by, __uint_as_float(o[e + nibble_column<BITS>(2 * k + 1)]) * by);
               store_sector(to + d + e, w, out_sectors);
             }
           }
@@ -655,7 +682,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
             for (int e = 0; e < 32; e += 16) {
               uint32_t w[8];
 #pragma unroll
-              for (int k = 0; k < 8; ++k) w[k] = Elem<BF16>::pack_rn(o[e + 2 * k] * by, o[e + 2 * k + 1] * by);
+              for (int k = 0; k < 8; ++k) w[k] = Elem<BF16>::pack_rn(o[e + nibble_column<BITS>(2 * k)] * by, o[e + nibble_column<BITS>(2 * k + 1)] * by);
               store_sector(to + d + e, w, out_sectors);
             }
           }
@@ -666,77 +693,165 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
   } else if (warp < 16) {
     // ---- codes to binary16: a warpgroup for the keys, one for the values ----
     regs_down<kWidenRegs>();
-    constexpr int kChunks = D / 16;                        // 16-byte chunks of a token's codes
-    constexpr int kItems = kKeys * kChunks / 128;          // per thread and step
     const bool values = warp >= 12;
     const int w = warp % 4, in_group = tid % 128;
     const int8_t* const codes = values ? p.v_codes : p.k_codes;
     const int full = values ? kVFull : kKFull, free = values ? kVFree : kKFree;
-    // eight neighbouring lanes write four chunks of two neighbouring tokens: the swizzle puts those in different banks
-    const int token0 = D == 128 ? w * 4 + (lane >> 4) * 2 + ((lane >> 2) & 1) : w * 8 + (lane >> 2);
-    const int chunk = D == 128 ? (lane & 3) | ((lane >> 3) & 1) << 2 : lane & 3;
-    unsigned char* const to = smem_at + (values ? Sh::kV : Sh::kK) + (chunk / 4) * kHalf;
-    const bool has_scale = !values && in_group < kGranules;  // the keys' group leaves the scales too, a thread for each granule
     uint32_t n = 0;                                        // steps so far
-    uint4 raw[kItems];
-    float4 scale = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    // pages of the next step's granules, -1 where there is none: every thread reads those of its own tokens (one lane for each granule and shuffles: 16 requests of 8000 tokens,
-    // 64 rows 150 -> 217 us, 5 requests in chunks 366 -> 420, although fewer instructions)
-    int pages[kItems], scale_page = -1;
     auto page_at = [&](int j, int granule) {
       const int token = j * kKeys + 16 * granule;
       if (token >= place.r.keys) return -1;
       return p.table[static_cast<long long>(place.request) * p.table_pages + (token >> p.page_shift)];
     };
-    auto fetch_pages = [&](int j) {
+    if constexpr (BITS == 8) {
+      constexpr int kChunks = D / 16;                        // 16-byte chunks of a token's codes
+      constexpr int kItems = kKeys * kChunks / 128;          // per thread and step
+      // eight neighbouring lanes write four chunks of two neighbouring tokens: the swizzle puts those in different banks
+      const int token0 = D == 128 ? w * 4 + (lane >> 4) * 2 + ((lane >> 2) & 1) : w * 8 + (lane >> 2);
+      const int chunk = D == 128 ? (lane & 3) | ((lane >> 3) & 1) << 2 : lane & 3;
+      unsigned char* const to = smem_at + (values ? Sh::kV : Sh::kK) + (chunk / 4) * kHalf;
+      const bool has_scale = !values && in_group < kGranules;  // the keys' group leaves the scales too, a thread for each granule
+      uint4 raw[kItems];
+      float4 scale = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      // pages of the next step's granules, -1 where there is none: every thread reads those of its own tokens (one lane for each granule and shuffles: 16 requests of 8000 tokens,
+      // 64 rows 150 -> 217 us, 5 requests in chunks 366 -> 420, although fewer instructions)
+      int pages[kItems], scale_page = -1;
+      auto fetch_pages = [&](int j) {
 #pragma unroll
-      for (int it = 0; it < kItems; ++it) pages[it] = page_at(j, (token0 + it * (128 / kChunks)) / 16);
-      if (has_scale) scale_page = page_at(j, in_group);
-    };
-    auto fetch = [&](int j) {
+        for (int it = 0; it < kItems; ++it) pages[it] = page_at(j, (token0 + it * (128 / kChunks)) / 16);
+        if (has_scale) scale_page = page_at(j, in_group);
+      };
+      auto fetch = [&](int j) {
 #pragma unroll
-      for (int it = 0; it < kItems; ++it) {
-        const int token = j * kKeys + token0 + it * (128 / kChunks);
-        raw[it] = make_uint4(0u, 0u, 0u, 0u);
-        if (static_cast<unsigned>(pages[it]) < static_cast<unsigned>(p.pages))
-          raw[it] = *(reinterpret_cast<const uint4*>(codes + (((static_cast<long long>(pages[it]) * p.kv_heads + place.head) << p.page_shift) +
-                                                              (token & ((1 << p.page_shift) - 1))) * D) + chunk);
-      }
-      if (has_scale) {
-        scale = make_float4(0.0f, -INFINITY, 0.0f, 0.0f);  // nothing of a page that is not there is seen
-        if (static_cast<unsigned>(scale_page) < static_cast<unsigned>(p.pages)) {
-          const long long page_head = static_cast<long long>(scale_page) * p.kv_heads + place.head;
-          const float vs = p.v_scale[page_head];
-          scale = make_float4(p.k_scale[page_head], log2_of_scale(vs), inverse_of_scale(vs), 0.0f);
+        for (int it = 0; it < kItems; ++it) {
+          const int token = j * kKeys + token0 + it * (128 / kChunks);
+          raw[it] = make_uint4(0u, 0u, 0u, 0u);
+          if (static_cast<unsigned>(pages[it]) < static_cast<unsigned>(p.pages))
+            raw[it] = *(reinterpret_cast<const uint4*>(codes + (((static_cast<long long>(pages[it]) * p.kv_heads + place.head) << p.page_shift) +
+                                                                (token & ((1 << p.page_shift) - 1))) * D) + chunk);
         }
-      }
-    };
-    int j = place.k0;
-    bool more = true;
-    fetch_pages(j);
-    fetch(j);
-    while (more) {
-      if (++j >= place.k1) {                               // the step behind this one
-        more = place.next(p);
-        j = place.k0;
-      }
-      if (more) fetch_pages(j);
-      const uint32_t buffer = n & 1u;
-      if (!wait(free + buffer, ((n >> 1) & 1u) ^ 1u)) break;
-      if (has_scale) reinterpret_cast<float4*>(smem_at + Sh::kScales)[(n % kMeta) * kGranules + in_group] = scale;
+        if (has_scale) {
+          scale = make_float4(0.0f, -INFINITY, 0.0f, 0.0f);  // nothing of a page that is not there is seen
+          if (static_cast<unsigned>(scale_page) < static_cast<unsigned>(p.pages)) {
+            const long long page_head = static_cast<long long>(scale_page) * p.kv_heads + place.head;
+            const float vs = p.v_scale[page_head];
+            scale = make_float4(p.k_scale[page_head], log2_of_scale(vs), inverse_of_scale(vs), 0.0f);
+          }
+        }
+      };
+      int j = place.k0;
+      bool more = true;
+      fetch_pages(j);
+      fetch(j);
+      while (more) {
+        if (++j >= place.k1) {                               // the step behind this one
+          more = place.next(p);
+          j = place.k0;
+        }
+        if (more) fetch_pages(j);
+        const uint32_t buffer = n & 1u;
+        if (!wait(free + buffer, ((n >> 1) & 1u) ^ 1u)) break;
+        if (has_scale) reinterpret_cast<float4*>(smem_at + Sh::kScales)[(n % kMeta) * kGranules + in_group] = scale;
 #pragma unroll
-      for (int it = 0; it < kItems; ++it) {
-        const int token = token0 + it * (128 / kChunks);
-        const uint32_t u[4] = {raw[it].x ^ 0x80808080u, raw[it].y ^ 0x80808080u, raw[it].z ^ 0x80808080u, raw[it].w ^ 0x80808080u};
-        unsigned char* const at = to + buffer * Sh::kOperand + token * 128;
-        const int c = 2 * (chunk % 4), x = token & 7;
-        *reinterpret_cast<uint4*>(at + ((c ^ x) << 4)) = make_uint4(widen_lo(u[0]), widen_hi(u[0]), widen_lo(u[1]), widen_hi(u[1]));
-        *reinterpret_cast<uint4*>(at + (((c + 1) ^ x) << 4)) = make_uint4(widen_lo(u[2]), widen_hi(u[2]), widen_lo(u[3]), widen_hi(u[3]));
+        for (int it = 0; it < kItems; ++it) {
+          const int token = token0 + it * (128 / kChunks);
+          const uint32_t u[4] = {raw[it].x ^ 0x80808080u, raw[it].y ^ 0x80808080u, raw[it].z ^ 0x80808080u, raw[it].w ^ 0x80808080u};
+          unsigned char* const at = to + buffer * Sh::kOperand + token * 128;
+          const int c = 2 * (chunk % 4), x = token & 7;
+          *reinterpret_cast<uint4*>(at + ((c ^ x) << 4)) = make_uint4(widen_lo(u[0]), widen_hi(u[0]), widen_lo(u[1]), widen_hi(u[1]));
+          *reinterpret_cast<uint4*>(at + (((c + 1) ^ x) << 4)) = make_uint4(widen_lo(u[2]), widen_hi(u[2]), widen_lo(u[3]), widen_hi(u[3]));
+        }
+        fence_proxy_async_smem();
+        bar_arrive(bars + 8 * (full + buffer));
+        if (more) fetch(j);
+        ++n;
       }
-      fence_proxy_async_smem();
-      bar_arrive(bars + 8 * (full + buffer));
-      if (more) fetch(j);
-      ++n;
+    } else {
+      constexpr int kChunks = D / 32;                      // 16-byte chunks of a token's codes
+      constexpr int kItems = kKeys * kChunks / 128;        // per thread and step
+      // A warp has 32 neighbouring tokens, two granules.  Eight neighbouring lanes have two chunks of four neighbouring tokens, whose parts the swizzle puts in different banks.
+      const int token0 = D == 128 ? 32 * w + ((lane >> 1) & 3) + ((lane >> 4) << 2) : 32 * w + (lane >> 1);
+      const int chunk = D == 128 ? (lane & 1) | ((lane >> 3) & 1) << 1 : lane & 1;
+      constexpr int kItemTokens = 32 / kItems;             // from one of a thread's items to the next
+      unsigned char* const to = smem_at + (values ? Sh::kV : Sh::kK) + (chunk / 2) * kHalf;
+      uint4 raw[kItems];
+      uint32_t k_word[kItems], v_word[kItems];             // scales and zero-points; 0 where there is no token.  The values' group has no use for the keys'
+      int pages[2];                                        // of the next step's granules
+      auto fetch_pages = [&](int j) {
+        pages[0] = page_at(j, 2 * w);
+        pages[1] = page_at(j, 2 * w + 1);
+      };
+      bool there[2];                                       // of the step whose codes have been fetched: granules whose page is in the cache
+      auto fetch = [&](int j) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) there[g] = static_cast<unsigned>(pages[g]) < static_cast<unsigned>(p.pages);
+#pragma unroll
+        for (int it = 0; it < kItems; ++it) {
+          const int g = it * kItemTokens / 16, token = j * kKeys + token0 + it * kItemTokens;
+          raw[it] = make_uint4(0u, 0u, 0u, 0u);
+          k_word[it] = v_word[it] = 0u;
+          if (there[g]) {
+            const long long at = ((static_cast<long long>(pages[g]) * p.kv_heads + place.head) << p.page_shift) + (token & ((1 << p.page_shift) - 1));
+            raw[it] = *(reinterpret_cast<const uint4*>(codes + at * (D / 2)) + chunk);
+            if (token < place.r.keys) {
+              v_word[it] = p.v_grid[at];
+              if (!values) k_word[it] = p.k_grid[at];
+            }
+          }
+        }
+      };
+      int j = place.k0;
+      bool more = true;
+      fetch_pages(j);
+      fetch(j);
+      while (more) {
+        if (++j >= place.k1) {                             // the step behind this one
+          more = place.next(p);
+          j = place.k0;
+        }
+        if (more) fetch_pages(j);
+        // the granules' powers of two, and the tokens' scales relative to them
+        float k_power[2], v_power[2], k_inverse[2], v_inverse[2];
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          float k_top = 0.0f, v_top = 0.0f;
+#pragma unroll
+          for (int it = g * kItems / 2; it < (g + 1) * kItems / 2; ++it) {
+            k_top = fmaxf(k_top, grid_top(k_word[it]));
+            v_top = fmaxf(v_top, grid_top(v_word[it]));
+          }
+          // numbers that are not negative are in the order of their bits
+          if (!values) k_power[g] = row_power(__uint_as_float(__reduce_max_sync(kFull, __float_as_uint(k_top))), k_inverse[g]);
+          v_power[g] = row_power(fmaxf(__uint_as_float(__reduce_max_sync(kFull, __float_as_uint(v_top))), kLeastScale), v_inverse[g]);
+        }
+        const uint32_t buffer = n & 1u;
+        if (!wait(free + buffer, ((n >> 1) & 1u) ^ 1u)) break;
+        if (!values && lane < 2) {                         // nothing of a page that is not there is seen
+          const bool first = lane == 0, here = first ? there[0] : there[1];
+          const float v_by = first ? v_inverse[0] : v_inverse[1];
+          reinterpret_cast<float4*>(smem_at + Sh::kScales)[(n % kMeta) * kGranules + 2 * w + lane] =
+              here ? make_float4(first ? k_inverse[0] : k_inverse[1], static_cast<float>(static_cast<int>(__float_as_uint(v_by) >> 23) - 127), first ? v_power[0] : v_power[1], 0.0f)
+                   : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
+        }
+#pragma unroll
+        for (int it = 0; it < kItems; ++it) {
+          const int g = it * kItemTokens / 16, token = token0 + it * kItemTokens;
+          const uint32_t word = values ? v_word[it] : k_word[it];
+          const bool fine = grid_is_number(v_word[it]) && grid_is_number(k_word[it]);
+          // a token whose scale is no number makes the rows NaN that see it, and no others: by its scores
+          const float scale = fine ? grid_scale(word) * (values ? v_power[g] : k_power[g]) : values ? 0.0f : NAN;
+          const float zero = grid_zero(word);
+          const __half2 s2 = __float2half2_rn(scale), less_even = __float2half2_rn(zero - 1024.0f), less_odd = __float2half2_rn(zero - 64.0f);
+          unsigned char* const at = to + buffer * Sh::kOperand + token * 128;
+          const uint32_t u[4] = {raw[it].x, raw[it].y, raw[it].z, raw[it].w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(at + (((4 * (chunk % 2) + k) ^ (token & 7)) << 4)) = widen_nibbles(u[k], less_even, less_odd, s2);
+        }
+        fence_proxy_async_smem();
+        bar_arrive(bars + 8 * (full + buffer));
+        if (more) fetch(j);
+        ++n;
+      }
     }
     regs_back<kWidenRegs>(warp / 4, !ok, &s_failed);
   } else {
@@ -823,21 +938,25 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
   if (threadIdx.x == 0 && s_failed != 0u) atomicExch(p.status, static_cast<unsigned>(TSQ_ERR_TIMEOUT));
 }
 
-template <bool BF16, int D>
+template <bool BF16, int D, int BITS>
 cudaError_t launch(const AttentionParams& p, int ctas, cudaStream_t stream) {
   constexpr int bytes = Shared<D>::kBytes + 1024;
   static_assert(Shared<D>::kScales >= 8 * kMaxRequests, "the unit counts fit in front of the scales");
   static std::atomic<unsigned long long> done{0};
-  const cudaError_t e = allow_shared(attention_tiles_kernel<BF16, D>, bytes, done);
+  const cudaError_t e = allow_shared(attention_tiles_kernel<BF16, D, BITS>, bytes, done);
   if (e != cudaSuccess) return e;
-  return launch_overlapped(attention_tiles_kernel<BF16, D>, ctas, kThreads, bytes, stream, p);
+  return launch_overlapped(attention_tiles_kernel<BF16, D, BITS>, ctas, kThreads, bytes, stream, p);
+}
+
+template <int BITS>
+cudaError_t launch(const AttentionParams& p, bool bf16, int head_dim, int sms, cudaStream_t stream) {
+  if (head_dim == 128) return bf16 ? launch<true, 128, BITS>(p, sms, stream) : launch<false, 128, BITS>(p, sms, stream);
+  return bf16 ? launch<true, 64, BITS>(p, sms, stream) : launch<false, 64, BITS>(p, sms, stream);
 }
 
 }  // namespace
 
-cudaError_t launch_attention_tiles(const AttentionParams& p, bool bf16, int head_dim, int sms, cudaStream_t stream) {
-  if (head_dim == 128) return bf16 ? launch<true, 128>(p, sms, stream) : launch<false, 128>(p, sms, stream);
-  return bf16 ? launch<true, 64>(p, sms, stream) : launch<false, 64>(p, sms, stream);
-}
+cudaError_t launch_attention_tiles(const AttentionParams& p, bool bf16, int head_dim, int sms, cudaStream_t stream) { return launch<8>(p, bf16, head_dim, sms, stream); }
+cudaError_t launch_attention4_tiles(const AttentionParams& p, bool bf16, int head_dim, int sms, cudaStream_t stream) { return launch<4>(p, bf16, head_dim, sms, stream); }
 
 }  // namespace tsq

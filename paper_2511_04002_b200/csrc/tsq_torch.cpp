@@ -1,4 +1,4 @@
-// The per-step calls of the binding, tsq_encode, tsq_decode and those of the paged cache on torch tensors, as a CPython extension: argument
+// The per-step calls of the binding, tsq_encode, tsq_decode and those of the paged caches on torch tensors, as a CPython extension: argument
 // checks, pointers, sizes and the current stream are read from the tensors in C++ and the C ABI (include/tsq.h) is called
 // directly.  A decode step is a few microseconds of GPU work, so what the interpreter spends around the call counts: through
 // ctypes, with the stream object that torch.cuda.current_stream() builds, a 64 x 4096 decode took 9.1 us of host time per
@@ -12,6 +12,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <exception>
+#include <type_traits>
 
 #include "tsq.h"
 
@@ -136,8 +137,10 @@ PyObject* guarded(F&& f) {
   }
 }
 
-const tsq_cache_t* cache_of(PyObject* address, PyObject* device, int* out) {
-  const auto* cache = static_cast<const tsq_cache_t*>(PyLong_AsVoidPtr(address));
+// CacheT: tsq_cache_t or tsq_cache4_t.
+template <typename CacheT>
+const CacheT* cache_of(PyObject* address, PyObject* device, int* out) {
+  const auto* cache = static_cast<const CacheT*>(PyLong_AsVoidPtr(address));
   *out = static_cast<int>(PyLong_AsLong(device));
   if (PyErr_Occurred()) return nullptr;
   if (!cache) PyErr_SetString(PyExc_ValueError, "no cache");
@@ -178,11 +181,25 @@ PyObject* cache_slots(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// cache_store(cache, device, k, v, slots, stream) -> status; cache_load(cache, device, slots, k, v, stream) -> status
+tsq_status_t store_rows(const tsq_cache_t* c, const void* k, int64_t ks, const void* v, int64_t vs, int64_t tokens, const int32_t* slots, void* stream) {
+  return tsq_cache_store(c, k, ks, v, vs, tokens, slots, stream);
+}
+tsq_status_t store_rows(const tsq_cache4_t* c, const void* k, int64_t ks, const void* v, int64_t vs, int64_t tokens, const int32_t* slots, void* stream) {
+  return tsq_cache4_store(c, k, ks, v, vs, tokens, slots, stream);
+}
+tsq_status_t load_rows(const tsq_cache_t* c, const int32_t* slots, int64_t tokens, void* k, int64_t ks, void* v, int64_t vs, void* stream) {
+  return tsq_cache_load(c, slots, tokens, k, ks, v, vs, stream);
+}
+tsq_status_t load_rows(const tsq_cache4_t* c, const int32_t* slots, int64_t tokens, void* k, int64_t ks, void* v, int64_t vs, void* stream) {
+  return tsq_cache4_load(c, slots, tokens, k, ks, v, vs, stream);
+}
+
+// cache_store(cache, device, k, v, slots, stream) -> status; cache_load(cache, device, slots, k, v, stream) -> status; cache4_store, cache4_load the same
+template <typename CacheT>
 PyObject* move_rows(PyObject* const* a, bool store) {
   return guarded([&]() -> PyObject* {
     int device = 0;
-    const tsq_cache_t* const cache = cache_of(a[0], a[1], &device);
+    const CacheT* const cache = cache_of<CacheT>(a[0], a[1], &device);
     if (!cache) return nullptr;
     const at::Tensor *k = tensor(a[store ? 2 : 3], "k"), *v = k ? tensor(a[store ? 3 : 4], "v") : nullptr, *slots = v ? tensor(a[store ? 4 : 2], "slots") : nullptr;
     if (!check_ints(slots, device, 1, -1, -1, "slots")) return nullptr;
@@ -197,24 +214,34 @@ PyObject* move_rows(PyObject* const* a, bool store) {
     const int64_t ks = token_stride(*k), vs = token_stride(*v);
     tsq_status_t st;
     Py_BEGIN_ALLOW_THREADS;
-    st = store ? tsq_cache_store(cache, kp, ks, vp, vs, tokens, sp, on.stream) : tsq_cache_load(cache, sp, tokens, kp, ks, vp, vs, on.stream);
+    st = store ? store_rows(cache, kp, ks, vp, vs, tokens, sp, on.stream) : load_rows(cache, sp, tokens, kp, ks, vp, vs, on.stream);
     Py_END_ALLOW_THREADS;
     return PyLong_FromLong(st);
   });
 }
-PyObject* cache_store(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return n == 6 ? move_rows(a, true) : PyErr_Format(PyExc_TypeError, "cache_store takes 6 arguments");
-}
-PyObject* cache_load(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return n == 6 ? move_rows(a, false) : PyErr_Format(PyExc_TypeError, "cache_load takes 6 arguments");
+template <typename CacheT, bool STORE>
+PyObject* move_call(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return n == 6 ? move_rows<CacheT>(a, STORE) : PyErr_Format(PyExc_TypeError, "a call that moves rows takes 6 arguments");
 }
 
-// cache_attention(cache, device, q, query_start, lengths, block_table, out, ws, max_query, scale, stream) -> status
-PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 11) return PyErr_Format(PyExc_TypeError, "cache_attention takes 11 arguments");
+tsq_status_t attend(const tsq_cache_t* c, const void* q, int64_t qs, int32_t heads, int64_t tokens, const int32_t* start, const int32_t* lengths, int32_t requests, int32_t most,
+                    const int32_t* table, int32_t width, float scale, int32_t, void* out, int64_t os, void* ws, size_t ws_bytes, void* stream) {
+  return tsq_cache_attention(c, q, qs, heads, tokens, start, lengths, requests, most, table, width, scale, out, os, ws, ws_bytes, stream);
+}
+tsq_status_t attend(const tsq_cache4_t* c, const void* q, int64_t qs, int32_t heads, int64_t tokens, const int32_t* start, const int32_t* lengths, int32_t requests, int32_t most,
+                    const int32_t* table, int32_t width, float scale, int32_t causal, void* out, int64_t os, void* ws, size_t ws_bytes, void* stream) {
+  return tsq_cache4_attention(c, q, qs, heads, tokens, start, lengths, requests, most, table, width, scale, causal, out, os, ws, ws_bytes, stream);
+}
+
+// cache_attention(cache, device, q, query_start, lengths, block_table, out, ws, max_query, scale, stream) -> status; cache4_attention the same with `causal` in front of the stream
+template <typename CacheT>
+PyObject* attention_call(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  constexpr bool kMayBeWhole = std::is_same<CacheT, tsq_cache4_t>::value;
+  constexpr Py_ssize_t kArguments = kMayBeWhole ? 12 : 11;
+  if (n != kArguments) return PyErr_Format(PyExc_TypeError, "this call of attention takes %zd arguments", kArguments);
   return guarded([&]() -> PyObject* {
     int device = 0;
-    const tsq_cache_t* const cache = cache_of(a[0], a[1], &device);
+    const CacheT* const cache = cache_of<CacheT>(a[0], a[1], &device);
     if (!cache) return nullptr;
     const at::Tensor* t[6];
     static const char* const names[6] = {"q", "query_start", "lengths", "block_table", "out", "ws"};
@@ -223,6 +250,7 @@ PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     const long long max_query = PyLong_AsLongLong(a[8]);
     const double scale = PyFloat_AsDouble(a[9]);
+    const int causal = kMayBeWhole ? PyObject_IsTrue(a[10]) : 1;
     if (PyErr_Occurred()) return nullptr;
     if (!check_ints(t[2], device, 1, -1, -1, names[2])) return nullptr;
     const int64_t requests = t[2]->size(0);
@@ -232,7 +260,7 @@ PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
       return nullptr;
     if (!t[5]->is_cuda() || t[5]->get_device() != device || t[5]->scalar_type() != at::kByte || !t[5]->is_contiguous())
       return PyErr_Format(PyExc_AssertionError, "ws must be a contiguous uint8 CUDA tensor on the cache's device");
-    OnDevice on(device, a[10]);
+    OnDevice on(device, a[kArguments - 1]);
     if (!on.ok) return nullptr;
     const int64_t most = 0x7fffffff;
     if (max_query < 1 || max_query > most || t[0]->size(1) > most || requests > most || t[3]->size(1) > most) return PyLong_FromLong(TSQ_ERR_INVALID_ARG);
@@ -241,9 +269,9 @@ PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void *const op = t[4]->data_ptr(), *const wp = t[5]->data_ptr();
     tsq_status_t st;
     Py_BEGIN_ALLOW_THREADS;
-    st = tsq_cache_attention(cache, qp, token_stride(*t[0]), static_cast<int32_t>(t[0]->size(1)), t[0]->size(0), ints(1), ints(2), static_cast<int32_t>(requests),
-                             static_cast<int32_t>(max_query), ints(3), static_cast<int32_t>(t[3]->size(1)), static_cast<float>(scale), op, token_stride(*t[4]), wp,
-                             static_cast<size_t>(t[5]->numel()), on.stream);
+    st = attend(cache, qp, token_stride(*t[0]), static_cast<int32_t>(t[0]->size(1)), t[0]->size(0), ints(1), ints(2), static_cast<int32_t>(requests),
+                static_cast<int32_t>(max_query), ints(3), static_cast<int32_t>(t[3]->size(1)), static_cast<float>(scale), causal, op, token_stride(*t[4]), wp,
+                static_cast<size_t>(t[5]->numel()), on.stream);
     Py_END_ALLOW_THREADS;
     return PyLong_FromLong(st);
   });
@@ -256,9 +284,12 @@ PyMethodDef methods[] = {
     {"encode", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(encode)), METH_FASTCALL, nullptr},
     {"decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(decode)), METH_FASTCALL, nullptr},
     {"cache_slots", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(cache_slots)), METH_FASTCALL, nullptr},
-    {"cache_store", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(cache_store)), METH_FASTCALL, nullptr},
-    {"cache_load", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(cache_load)), METH_FASTCALL, nullptr},
-    {"cache_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(cache_attention)), METH_FASTCALL, nullptr},
+    {"cache_store", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(move_call<tsq_cache_t, true>)), METH_FASTCALL, nullptr},
+    {"cache_load", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(move_call<tsq_cache_t, false>)), METH_FASTCALL, nullptr},
+    {"cache_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(attention_call<tsq_cache_t>)), METH_FASTCALL, nullptr},
+    {"cache4_store", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(move_call<tsq_cache4_t, true>)), METH_FASTCALL, nullptr},
+    {"cache4_load", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(move_call<tsq_cache4_t, false>)), METH_FASTCALL, nullptr},
+    {"cache4_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(attention_call<tsq_cache4_t>)), METH_FASTCALL, nullptr},
     {"current_stream", current_stream, METH_NOARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tsq_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
