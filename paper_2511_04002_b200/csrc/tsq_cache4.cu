@@ -63,12 +63,6 @@ __device__ __forceinline__ void store32(void* at, const uint32_t (&w)[8], bool w
   }
 }
 
-__device__ __forceinline__ float reciprocal(float x) {
-  float y;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 // ---- quantising into the cache -------------------------------------------------------------------
 
 constexpr float kMagic = 12582912.0f;     // 1.5 * 2^23: a sum with it is a whole number, which its low bits hold
@@ -296,7 +290,11 @@ tsq_status_t move_rows(const tsq_cache4_t* cache, void* k, int64_t k_stride, voi
   return launched(launch_overlapped(kernel, ctas, kMoveThreads, 0, st, p));
 }
 
-bool few_query_rows(long long max_query, int group) { return max_query * group <= kFewQueryRows; }
+// Which kernel: by the query rows that a key head's codes serve at most.  The row kernel takes the codes again for every 16 rows, the tile kernel 256 at once, at a step's price whether they
+// are there or not.  us, rows / tiles (bf16, heads of 128): 16 requests of 8000 keys, 8 key heads, 16 rows 59 / 149, 32 rows 98 / 148, 48 rows 136 / 148, 64 rows 174 / 151; 64 of 2000 keys 48 rows
+// 151 / 161, 64 rows 195 / 161; 1 of 100000 keys 48 rows 116 / 153, 64 rows 140 / 153; 16 of 3000 keys, 40 key heads, 32 rows 180 / 264, 40 rows 255 / 265.
+constexpr int kFewRows = 48;
+bool few_query_rows(long long max_query, int group) { return max_query * group <= kFewRows; }
 
 }  // namespace
 }  // namespace tsq

@@ -12,12 +12,22 @@ namespace {
 constexpr int kWarps = kRowsWarps, kThreads = kRowsThreads;
 constexpr int kStepTokens = 32;              // tokens of a warp's step, a lane each; two granules of 16, which lie in a page each
 constexpr int kUnitTokens = kWarps * kStepTokens;
-constexpr int kTileUnits = 1;                // what beginning and ending a tile costs, in units
+constexpr int kTileUnits = 2;                // what beginning and ending a tile costs, in units
+
+constexpr uint32_t kNoToken = 0xff80u;       // the word of a token without a page: no scale is negative
 
 __device__ __forceinline__ uint32_t lds32(uint32_t at) {
   uint32_t v;
   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at));
   return v;
+}
+
+__device__ __forceinline__ void lds2x64(uint64_t& a, uint64_t& b, uint32_t at) { asm volatile("ld.shared.v2.u64 {%0,%1}, [%2];" : "=l"(a), "=l"(b) : "r"(at)); }
+// The first of a row of products.
+__device__ __forceinline__ void mma_16816_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
 }
 
 // Where the 16-byte chunk `c` of token row `t` lies in a stage: chunks change places within their 128 bytes, so that the eight chunks that lanes read at once of every second
@@ -28,14 +38,17 @@ __device__ __forceinline__ int placed(int t, int c) {
   return (at ^ (D == 128 ? ((at >> 3) & 3) << 1 : ((at >> 3) & 1) << 1)) << 4;
 }
 
-// Nibbles in bits 0 .. 3 and in bits 4 .. 7 of both halves as binary16 numbers code * 2^-20: below the normal range, but exact.  (The products take such a number at the exponent 2^-14 and cut
-// what is below 2^-24 of the largest product in their sum: 2^-18 of a code here, and 2^-14 without the multiplication by 16.)
-__device__ __forceinline__ uint32_t low_nibbles(uint32_t u) { return Elem<false>::bits(__hmul2(Elem<false>::as2(u & 0x000f000fu), __float2half2_rn(16.0f))); }
-__device__ __forceinline__ uint32_t high_nibbles(uint32_t u) { return u & 0x00f000f0u; }
+// Four codes from 16 bits, in both halves of a word: the first two of them or, with `upper`, the others, shifted to bits 3 .. 6 and 7 .. 10.  There a nibble is the binary16 number code * 2^-21 or
+// code * 2^-17: numbers with an exponent of 0 and of 1 have the same unit 2^-24, so eleven bits are linear.  (The products take a number below the normal range at the exponent 2^-14 and cut
+// what is below 2^-24 of the largest product in their sum: 2^-17 of a code here, where nibbles in bits 0 .. 3 would lose 2^-14.)
+__device__ __forceinline__ uint32_t to_linear_bits(uint32_t u, bool upper) { return upper ? u >> 5 : mad_u32(u, 8u, 0u); }
+__device__ __forceinline__ uint32_t low_nibbles(uint32_t u) { return u & 0x00780078u; }
+__device__ __forceinline__ uint32_t high_nibbles(uint32_t u) { return u & 0x07800780u; }
 
-// The queries as the products with nibbles take them, brought to binary16 by a power of two per row.  Of eight dimensions the pairs (0, 4), (1, 5), (2, 6), (3, 7) go together.  factor, sum: of the rows 8 t + 2 c and 8 t + 2 c + 1, what turns sums of products into <q, code>, and the row's sum in their measure.
+// The queries as the products with nibbles take them, brought to binary16 by a power of two per row.  Of eight dimensions the pairs (0, 4), (1, 5), (2, 6), (3, 7) go together;
+// odd ones meet codes that count sixteen times.  factor, sum: of the rows 8 t + 2 c and 8 t + 2 c + 1, what turns sums of products into <q, code>, and the row's sum in their measure.
 template <bool BF16, int D, int NT>
-__device__ __forceinline__ void scale_queries(const uint4 (&raw)[NT][D / 32], int c, uint32_t (&q)[NT][D / 16][2], float (&factor)[NT][2], float (&sum)[NT][2]) {
+__device__ __forceinline__ void scale_queries(const uint4 (&raw)[NT][D / 32], int c, uint32_t (&q)[NT][D / 16][2], uint64_t (&factor)[NT], uint64_t (&sum)[NT]) {
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     uint32_t w[D / 8];
@@ -48,7 +61,7 @@ __device__ __forceinline__ void scale_queries(const uint4 (&raw)[NT][D / 32], in
     top = max(top, __shfl_xor_sync(kFull, top, 1));
     top = max(top, __shfl_xor_sync(kFull, top, 2));
     float inverse;
-    const float power = row_power(Elem<BF16>::pattern_f32(top), inverse);
+    const float power = row_power<126>(Elem<BF16>::pattern_f32(top), inverse);  // a sixteenth of the least numbers is to be one, too
 #pragma unroll
     for (int k = 0; k < D / 32; ++k) {
 #pragma unroll
@@ -56,18 +69,16 @@ __device__ __forceinline__ void scale_queries(const uint4 (&raw)[NT][D / 32], in
         const uint32_t u = w[4 * k + h], v = w[4 * k + 2 + h];
         const float u0 = Elem<BF16>::lo_f32(u) * power, v0 = Elem<BF16>::lo_f32(v) * power, u1 = Elem<BF16>::hi_f32(u) * power, v1 = Elem<BF16>::hi_f32(v) * power;
         q[t][2 * k + h][0] = pack_half2(u0, v0);
-        q[t][2 * k + h][1] = pack_half2(u1, v1);
+        q[t][2 * k + h][1] = pack_half2(u1 * 0.0625f, v1 * 0.0625f);
         all += (u0 + v0) + (u1 + v1);
       }
     }
     all += __shfl_xor_sync(kFull, all, 1);
     all += __shfl_xor_sync(kFull, all, 2);
-    all *= 9.5367431640625e-7f;                            // 2^-20
-    inverse *= 1048576.0f;                                 // the 2^20 that a code lacks
-    factor[t][0] = __shfl_sync(kFull, inverse, 8 * c);     // of the thread with g = 2 c
-    factor[t][1] = __shfl_sync(kFull, inverse, 8 * c + 4);
-    sum[t][0] = __shfl_sync(kFull, all, 8 * c);
-    sum[t][1] = __shfl_sync(kFull, all, 8 * c + 4);
+    all *= 4.76837158203125e-7f;                           // 2^-21
+    inverse *= 2097152.0f;                                 // the 2^21 that a code lacks
+    factor[t] = pack2f(__shfl_sync(kFull, inverse, 8 * c), __shfl_sync(kFull, inverse, 8 * c + 4));  // of the threads with g = 2 c and 2 c + 1
+    sum[t] = pack2f(__shfl_sync(kFull, all, 8 * c), __shfl_sync(kFull, all, 8 * c + 4));
   }
 }
 
@@ -75,27 +86,28 @@ __device__ __forceinline__ void scale_queries(const uint4 (&raw)[NT][D / 32], in
 template <int D, int NT>
 struct Layout {
   static constexpr int kRows = 8 * NT;
-  static constexpr int kCtasPerSm = NT == 1 ? kRowsCtasPerSm : 3;
-  static constexpr int kStages = NT == 1 ? 3 : 4;        // of a warp's ring
+  // heads of 128, 8 rows: 4 CTAs of 128 registers 70.5 us for 64 requests, 3 of 168 68.2, 2 73; 131072 tokens 46.0, 40.5, 42.6
+  static constexpr int kCtasPerSm = NT == 1 && D == 64 ? 4 : 3;
+  static constexpr int kStages = 3;                      // of a warp's ring
   static constexpr int kHalf = kStepTokens * D / 2;      // bytes of a stage's keys, and of its values
   static constexpr int kWords = 2 * kHalf;               // behind them: the keys' words, the values'
   static constexpr int kStage = kWords + 2 * kStepTokens * 4;
   static constexpr int kRing = kStages * kStage;         // of a warp
   static constexpr int kMerge = RowsSums<D, NT>::kBytes;
-  static constexpr int kTokens = kWarps * kRing > kMerge ? kWarps * kRing : kMerge;  // a step's factors for each warp: four numbers a token, then the values' zero-points in binary16
-  static constexpr int kTokenBytes = kStepTokens * 18;
+  static constexpr int kTokens = kWarps * kRing > kMerge ? kWarps * kRing : kMerge;  // a step's factors for each warp: four numbers a token, each twice, the values' zero-points in binary16, as many zeros
+  static constexpr int kTokenBytes = kStepTokens * 36;
   static constexpr int kBytes = kTokens + kWarps * kTokenBytes;
 };
 
 // As over the 8-bit cache (tsq_cache_rows.cu): units of neighbouring tokens of one (request, key head, tile of query rows), the same number for every CTA; the four warps have 32
 // tokens of a unit each, a ring of stages and sums of their own; codes are the 16-row operand of both products.  What 4 bits change:
 //
-// A nibble alone in bits 4 .. 7 of a 16-bit field is the binary16 number code * 2^-20, and one in bits 0 .. 3 that by a multiplication by 16.  So a word becomes four operand registers by four
-// masks, a shift and two packed products: (0, 4) and (1, 5) of its eight codes, then (2, 6) and (3, 7).  What that leaves is put right outside of the products:
+// A nibble alone in the right bits of a 16-bit field is a binary16 number (to_linear_bits).  So a word becomes four operand registers by two shifts and four masks: (0, 4) and (1, 5) of its
+// eight codes, then (2, 6) and (3, 7).  What that leaves is put right outside of the products:
 //   score  = s_k (sum q c + z_k sum q)          by two operations per score, the keys' scale and zero-point by token
 //   out    = (sum w c + sum w z_v) / sum p      w = p s_v rounded to binary16, as over the 8-bit cache: 2^(score + log2 s_v - m), relative to the row's largest;
 //                                               the second sum is one more product, whose operand is the zero-points, whole numbers, so both have the same rounded weights
-// The factor 2^20 comes in at a tile's end.
+// The factors 2^21 and 2^17 come in at a tile's end.
 template <bool BF16, int D, int NT>
 __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention4_rows_kernel(const AttentionParams p) {
   using L = Layout<D, NT>;
@@ -110,7 +122,16 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
   if (!share_of<L::kRows, kUnitTokens, kTileUnits>(p, work)) return;
   int i = work.request;
   Request r = request_of(p, i);
-  const uint32_t ring = smem_addr(smem) + warp * L::kRing, factors = smem_addr(smem) + L::kTokens + warp * L::kTokenBytes, zeros = factors + kStepTokens * 16;
+  const uint32_t ring = smem_addr(smem) + warp * L::kRing, factors = smem_addr(smem) + L::kTokens + warp * L::kTokenBytes, zeros = factors + kStepTokens * 32;
+  // where the lane's parts lie in a stage (placed), for tokens in front of which a whole number of eight lies: rows of eight are kHalf / 4 apart
+  constexpr int kEight = L::kHalf / 4;
+  const uint32_t copy_to = placed<D>(lane / kChunks, lane % kChunks);
+  const uint32_t k_at = D == 128 ? placed<D>(g, c) : placed<D>(g, c / 2) + 8 * (c % 2);
+  const uint32_t v_at = L::kHalf + (D == 128 ? placed<D>(2 * c, g / 2) + 8 * (g % 2) : placed<D>(2 * c, g / 4) + 4 * (g % 4));
+  constexpr uint32_t kNeighbour = D == 128 ? 64 : 32;      // token 2 c + 1: that bit of the address the other way round
+  // zero-points are one row of their operand; the other rows' threads read zeros behind them
+  const uint32_t z_at = zeros + (g == 0 ? 4 * c : 2 * kStepTokens);
+  if (lane < 16) asm volatile("st.shared.u32 [%0], %1;" ::"r"(zeros + 2 * kStepTokens + 4 * lane), "r"(0u) : "memory");
 
   while (work.unit < work.end) {
     const int tiles = r.tiles(L::kRows, p), keys = r.key_units(kUnitTokens), span = keys + kTileUnits;
@@ -140,48 +161,55 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
       };
       // for the batch of 16 steps that is being worked off and the one behind it, and what is read ahead for the next
       int page_0 = page_of(0), page_1 = n_steps > 16 ? page_of(1) : -1, page_ahead = -1;
-      auto pages_of = [&](int step, int (&id)[2]) {
-        const int batch = (step >> 4) & 1 ? page_1 : page_0;
-        id[0] = __shfl_sync(kFull, batch, 2 * step & 31);
-        id[1] = __shfl_sync(kFull, batch, (2 * step & 31) + 1);
-      };
-      // the slot of a page's head and place, for the token `token` in page `id`
-      auto row_of = [&](int id, int token) {
-        return ((static_cast<long long>(id) * p.kv_heads + head) << p.page_shift) + (token & ((1 << p.page_shift) - 1));
-      };
+      // A step's places in its pages are those of every other step.  Addresses in page 0; what a page has of all heads lies `page_rows` rows behind.
+      const int place = base & ((1 << p.page_shift) - 1);
+      const bool one_page = p.page_shift > 4;               // a step's second granule lies behind the first
+      const long long row = (static_cast<long long>(head) << p.page_shift) + place;
+      const uint32_t page_rows = static_cast<uint32_t>(p.kv_heads) << p.page_shift, page_bytes = page_rows * (D / 2);
+      const int8_t *const k_from = p.k_codes + row * (D / 2) + lane * 16, *const v_from = p.v_codes + row * (D / 2) + lane * 16;
+      // lanes 0 .. 15: four tokens' words each, the keys', then the values'
+      const uint32_t* const words_from = (lane & 8 ? p.v_grid : p.k_grid) + row + (lane & 3) * 4 + (lane & 4 && one_page ? 16 : 0);
+      uint32_t stage_in = ring;
       auto issue = [&](int step) {
         if (step < n_steps) {
-          int id[2];
-          pages_of(step, id);
-          const int token = base + step * kUnitTokens;
-          const uint32_t stage = ring + (step % L::kStages) * L::kStage;
+          const int batch = (step >> 4) & 1 ? page_1 : page_0;
+          const int id0 = __shfl_sync(kFull, batch, 2 * step & 31), id1 = __shfl_sync(kFull, batch, (2 * step & 31) + 1);
           constexpr int kCopies = kStepTokens * kChunks / 64;   // of a granule's keys, and of its values, by the warp
+          const auto copy_granules = [&](int id, int first, int n_granules) {
+            const int8_t* const k_page = k_from + static_cast<unsigned long long>(static_cast<uint32_t>(id)) * page_bytes;
+            const int8_t* const v_page = v_from + static_cast<unsigned long long>(static_cast<uint32_t>(id)) * page_bytes;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if (id[h] < 0) continue;
-            const long long at = row_of(id[h], token + 16 * h) * (D / 2) + lane * 16;
-            const int8_t *const k_from = p.k_codes + at, *const v_from = p.v_codes + at;
-#pragma unroll
-            for (int n = 0; n < kCopies; ++n) {
-              const int item = (h * kCopies + n) * 32 + lane;
-              const int to = placed<D>(item / kChunks, item % kChunks);
-              copy16(stage + to, k_from + n * 512);
-              copy16(stage + L::kHalf + to, v_from + n * 512);
+            for (int n = 0; n < n_granules * kCopies; ++n) {
+              const uint32_t to = stage_in + copy_to + (first * kCopies + n) * 512;
+              copy16(to, k_page + n * 512);
+              copy16(to + L::kHalf, v_page + n * 512);
             }
+          };
+          if (one_page && (id0 | id1) >= 0) {               // the second granule of the last step may have no token
+            copy_granules(id0, 0, 2);
+          } else {                                          // one_page: the second one is then not there
+            if (id0 >= 0) copy_granules(id0, 0, 1);
+            if (id1 >= 0) copy_granules(id1, 1, 1);
           }
-          if (lane < 16) {                                 // four tokens' words each: the keys', then the values'
-            const int mine = lane & 4 ? id[1] : id[0];
-            if (mine >= 0) copy16(stage + L::kWords + lane * 16, (lane < 8 ? p.k_grid : p.v_grid) + row_of(mine, token + 4 * (lane & 7)));
+          const int mine = lane & 4 ? id1 : id0;
+          if (lane < 16) {
+            const uint32_t to = stage_in + L::kWords + lane * 16;
+            if (mine >= 0) {
+              copy16(to, words_from + static_cast<unsigned long long>(static_cast<uint32_t>(mine)) * page_rows);
+            } else {
+              asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(to), "r"(kNoToken) : "memory");
+            }
           }
         }
         copies_commit();
+        stage_in = stage_in + L::kStage == ring + L::kRing ? ring : stage_in + L::kStage;
       };
       __syncthreads();                                      // the shared memory is free of the last tile's sums
 #pragma unroll
       for (int s = 0; s < L::kStages - 1; ++s) issue(s);
 
       uint32_t q[NT][kSteps][2];
-      float factor[NT][2], sum_q[NT][2];                    // of the rows 8 t + 2 c and 8 t + 2 c + 1, whose scores this thread has
+      uint64_t factor[NT], sum_q[NT];                       // of the rows 8 t + 2 c and 8 t + 2 c + 1, whose scores this thread has
       scale_queries<BF16, D, NT>(raw, c, q, factor, sum_q);
       int seen[NT][2];
 #pragma unroll
@@ -191,22 +219,22 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
       }
 
       float acc[NT][kTiles][4], acc_zero[NT][4];
-      float m[NT][2], l[NT][2];
+      float m[NT][2], limit[NT][2];
+      uint64_t l[NT], less[NT];                             // sums; the references negated, 0 as long as there is none
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
 #pragma unroll
         for (int d = 0; d < kTiles; ++d) acc[t][d][0] = acc[t][d][1] = acc[t][d][2] = acc[t][d][3] = 0.0f;
         acc_zero[t][0] = acc_zero[t][1] = acc_zero[t][2] = acc_zero[t][3] = 0.0f;
-        m[t][0] = m[t][1] = -INFINITY;
-        l[t][0] = l[t][1] = 0.0f;
+        m[t][0] = m[t][1] = limit[t][0] = limit[t][1] = -INFINITY;
+        l[t] = less[t] = 0ull;
       }
 
+      uint32_t stage_out = ring;
       for (int step = 0; step < n_steps; ++step) {
         copies_wait<L::kStages - 2>();
         __syncwarp();
         issue(step + L::kStages - 1);
-        int id[2];
-        pages_of(step, id);
         // the batch after the next takes this one's place: its pages are read while this one's last steps are worked off
         if ((step & 15) == 7 && (step | 15) + 17 < n_steps) page_ahead = page_of((step >> 4) + 2);
         if ((step & 15) == 15) {
@@ -217,20 +245,23 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
           }
           page_ahead = -1;
         }
-        if (id[0] < 0 && id[1] < 0) continue;
-        const uint32_t stage = ring + (step % L::kStages) * L::kStage;
+        const uint32_t stage = stage_out;
+        stage_out = stage + L::kStage == ring + L::kRing ? ring : stage + L::kStage;
         const int token0 = base + step * kUnitTokens;
 
         // factors of the lane's token: of its scores, their addend (log2 s_v), of the softmax's sum; a token that is not there has weight 0
         {
-          const uint32_t k_word = lds32(stage + L::kWords + lane * 4), v_word = lds32(stage + L::kWords + (kStepTokens + lane) * 4);
-          const bool here = (lane < 16 ? id[0] : id[1]) >= 0 && token0 + lane < seen_last;
-          const float vs = grid_scale(v_word);
-          const float ks = grid_is_number(k_word) && grid_is_number(v_word) ? grid_scale(k_word) * p.scale_log2 : NAN;
-          asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(factors + lane * 16), "f"(here ? ks : 0.0f), "f"(here ? grid_zero(k_word) : 0.0f),
-                       "f"(here ? log2_of_scale(vs) : -INFINITY), "f"(here ? inverse_of_scale(vs) : 0.0f)
-                       : "memory");
-          const __half z = __float2half_rn(here ? grid_zero(v_word) : 0.0f);
+          uint32_t k_word = lds32(stage + L::kWords + lane * 4), v_word = lds32(stage + L::kWords + (kStepTokens + lane) * 4);
+          const bool here = v_word != kNoToken && token0 + lane < seen_last;
+          k_word = here ? k_word : 0u;
+          v_word = here ? v_word : 0u;
+          const float ks = grid_scale(k_word), vs = grid_scale(v_word), least = fmaxf(vs, kLeastScale), kz = grid_zero(k_word);
+          const float by = __fmaf_rn(ks, p.scale_log2, __fmaf_rn(ks, 0.0f, vs * 0.0f));  // NaN where one of the scales is not finite
+          const float a = here ? log2_approx(least) : -INFINITY, inverse = reciprocal(least);
+          // each twice, for the products of pairs of rows
+          asm volatile("st.shared.v4.f32 [%0], {%1,%1,%2,%2};" ::"r"(factors + lane * 32), "f"(by), "f"(kz) : "memory");
+          asm volatile("st.shared.v4.f32 [%0], {%1,%1,%2,%2};" ::"r"(factors + lane * 32 + 16), "f"(a), "f"(inverse) : "memory");
+          const __half z = __float2half_rn(grid_zero(v_word));
           asm volatile("st.shared.u16 [%0], %1;" ::"r"(zeros + lane * 2), "h"(__half_as_ushort(z)) : "memory");
         }
         __syncwarp();
@@ -239,15 +270,13 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
         float s[2][NT][4];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-#pragma unroll
-          for (int t = 0; t < NT; ++t) s[u][t][0] = s[u][t][1] = s[u][t][2] = s[u][t][3] = 0.0f;
           uint32_t w0[kChunks], w1[kChunks];                // of the tokens g and g + 8: D / 4 dimensions from c * D / 4 on
           if constexpr (D == 128) {
-            const uint4 x0 = lds128(stage + placed<D>(16 * u + g, c)), x1 = lds128(stage + placed<D>(16 * u + g + 8, c));
+            const uint4 x0 = lds128(stage + k_at + 2 * u * kEight), x1 = lds128(stage + k_at + (2 * u + 1) * kEight);
             w0[0] = x0.x, w0[1] = x0.y, w0[2] = x0.z, w0[3] = x0.w;
             w1[0] = x1.x, w1[1] = x1.y, w1[2] = x1.z, w1[3] = x1.w;
           } else {
-            const uint2 x0 = lds64(stage + placed<D>(16 * u + g, c / 2) + 8 * (c % 2)), x1 = lds64(stage + placed<D>(16 * u + g + 8, c / 2) + 8 * (c % 2));
+            const uint2 x0 = lds64(stage + k_at + 2 * u * kEight), x1 = lds64(stage + k_at + (2 * u + 1) * kEight);
             w0[0] = x0.x, w0[1] = x0.y;
             w1[0] = x1.x, w1[1] = x1.y;
           }
@@ -255,25 +284,31 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
           for (int k = 0; k < kChunks; ++k) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const uint32_t u0 = w0[k] >> (8 * h), u1 = w1[k] >> (8 * h);
+              const uint32_t u0 = to_linear_bits(w0[k], h != 0), u1 = to_linear_bits(w1[k], h != 0);
               const uint32_t a[4] = {low_nibbles(u0), low_nibbles(u1), high_nibbles(u0), high_nibbles(u1)};
 #pragma unroll
-              for (int t = 0; t < NT; ++t) mma_16816(s[u][t], a, q[t][2 * k + h][0], q[t][2 * k + h][1]);
+              for (int t = 0; t < NT; ++t) {
+                if (k + h == 0) {
+                  mma_16816_first(s[u][t], a, q[t][0][0], q[t][0][1]);
+                } else {
+                  mma_16816(s[u][t], a, q[t][2 * k + h][0], q[t][2 * k + h][1]);
+                }
+              }
             }
           }
         }
-        float inverse_v[2][2];
-        bool over = false;
+        uint64_t inverse_v[2][2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const float4 f0 = lds128f(factors + (16 * u + g) * 16), f1 = lds128f(factors + (16 * u + g + 8) * 16);
-          inverse_v[u][0] = f0.w, inverse_v[u][1] = f1.w;
 #pragma unroll
-          for (int t = 0; t < NT; ++t) {
+          for (int e = 0; e < 2; ++e) {                     // tokens g and g + 8
+            uint64_t by, kz, a;
+            lds2x64(by, kz, factors + (16 * u + 8 * e + g) * 32);
+            lds2x64(a, inverse_v[u][e], factors + (16 * u + 8 * e + g) * 32 + 16);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              s[u][t][h] = __fmaf_rn(__fmaf_rn(f0.y, sum_q[t][h], s[u][t][h]), f0.x * factor[t][h], f0.z);
-              s[u][t][2 + h] = __fmaf_rn(__fmaf_rn(f1.y, sum_q[t][h], s[u][t][2 + h]), f1.x * factor[t][h], f1.z);
+            for (int t = 0; t < NT; ++t) {
+              const uint64_t x = fma2(fma2(kz, sum_q[t], pack2f(s[u][t][2 * e], s[u][t][2 * e + 1])), mul2(by, factor[t]), a);
+              unpack2f(x, s[u][t][2 * e], s[u][t][2 * e + 1]);
             }
           }
         }
@@ -291,12 +326,13 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
           }
         }
         float top[NT][2];
+        bool over = false;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             top[t][h] = fmaxf(fmaxf(s[0][t][h], s[0][t][2 + h]), fmaxf(s[1][t][h], s[1][t][2 + h]));
-            over = over || top[t][h] > m[t][h] + 8.0f;
+            over = over || top[t][h] > limit[t][h];
           }
         }
         // m is a reference, not the maximum: it follows only when a score is more than 2^8 above it (a weight stays below 2^9 in binary16)
@@ -309,9 +345,11 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
               const float now = fmaxf(m[t][h], column_max(top[t][h]));
               by[h] = m[t][h] == -INFINITY ? 0.0f : exp2_fast(m[t][h] - now);
               m[t][h] = now;
-              l[t][h] *= by[h];
+              limit[t][h] = now + 8.0f;
               acc_zero[t][h] *= by[h];
             }
+            l[t] = mul2(l[t], pack2f(by[0], by[1]));
+            less[t] = pack2f(m[t][0] == -INFINITY ? 0.0f : -m[t][0], m[t][1] == -INFINITY ? 0.0f : -m[t][1]);
 #pragma unroll
             for (int d = 0; d < kTiles; ++d) {
               acc[t][d][0] *= by[0];
@@ -324,14 +362,17 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
         uint32_t w[2][NT][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          const float ref0 = m[t][0] == -INFINITY ? 0.0f : m[t][0], ref1 = m[t][1] == -INFINITY ? 0.0f : m[t][1];
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            const float x0 = exp2_fast(s[u][t][0] - ref0), x1 = exp2_fast(s[u][t][1] - ref1), x2 = exp2_fast(s[u][t][2] - ref0), x3 = exp2_fast(s[u][t][3] - ref1);
-            l[t][0] = __fmaf_rn(x0, inverse_v[u][0], __fmaf_rn(x2, inverse_v[u][1], l[t][0]));
-            l[t][1] = __fmaf_rn(x1, inverse_v[u][0], __fmaf_rn(x3, inverse_v[u][1], l[t][1]));
-            w[u][t][0] = transposed(pack_half2(x0, x1));
-            w[u][t][1] = transposed(pack_half2(x2, x3));
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float x0, x1;
+              unpack2f(add2(pack2f(s[u][t][2 * e], s[u][t][2 * e + 1]), less[t]), x0, x1);
+              x0 = exp2_fast(x0);
+              x1 = exp2_fast(x1);
+              l[t] = fma2(pack2f(x0, x1), inverse_v[u][e], l[t]);
+              w[u][t][e] = transposed(pack_half2(x0, x1));
+            }
           }
         }
 
@@ -341,12 +382,12 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
           uint32_t v[4][D / 64];
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
-            const int token = 16 * u + 2 * c + (t & 1) + 8 * (t >> 1);
+            const uint32_t at = (stage + (t & 1 ? v_at ^ kNeighbour : v_at)) + (2 * u + (t >> 1)) * kEight;
             if constexpr (D == 128) {
-              const uint2 x = lds64(stage + L::kHalf + placed<D>(token, g / 2) + 8 * (g % 2));
+              const uint2 x = lds64(at);
               v[t][0] = x.x, v[t][1] = x.y;
             } else {
-              v[t][0] = lds32(stage + L::kHalf + placed<D>(token, g / 4) + 4 * (g % 4));
+              v[t][0] = lds32(at);
             }
           }
 #pragma unroll
@@ -356,33 +397,35 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
               const uint32_t x = __byte_perm(v[0][k], v[1][k], half ? 0x7632 : 0x5410), y = __byte_perm(v[2][k], v[3][k], half ? 0x7632 : 0x5410);
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
-                const uint32_t u0 = x >> (8 * h), u1 = y >> (8 * h);
+                const uint32_t u0 = to_linear_bits(x, h != 0), u1 = to_linear_bits(y, h != 0);
                 const uint32_t a[4] = {low_nibbles(u0), high_nibbles(u0), low_nibbles(u1), high_nibbles(u1)};
 #pragma unroll
                 for (int t = 0; t < NT; ++t) mma_16816(acc[t][4 * k + 2 * half + h], a, w[u][t][0], w[u][t][1]);
               }
             }
           }
-          const uint32_t z0 = lds32(zeros + (16 * u + 2 * c) * 2), z1 = lds32(zeros + (16 * u + 2 * c + 8) * 2);
-          const uint32_t a[4] = {g == 0 ? z0 : 0u, 0u, g == 0 ? z1 : 0u, 0u};
+          const uint32_t a[4] = {lds32(z_at + 32 * u), 0u, lds32(z_at + 32 * u + 16), 0u};
 #pragma unroll
           for (int t = 0; t < NT; ++t) mma_16816(acc_zero[t], a, w[u][t][0], w[u][t][1]);
         }
       }
 
+      float sums[NT][2];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) unpack2f(l[t], sums[t][0], sums[t][1]);
       // codes' sums and zero-points' sum in one measure: the latter are with the threads of g = 0
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         const float zero0 = __shfl_sync(kFull, acc_zero[t][0], c), zero1 = __shfl_sync(kFull, acc_zero[t][1], c);
 #pragma unroll
         for (int d = 0; d < kTiles; ++d) {
-          acc[t][d][0] = __fmaf_rn(acc[t][d][0], 1048576.0f, zero0);
-          acc[t][d][1] = __fmaf_rn(acc[t][d][1], 1048576.0f, zero1);
-          acc[t][d][2] = __fmaf_rn(acc[t][d][2], 1048576.0f, zero0);
-          acc[t][d][3] = __fmaf_rn(acc[t][d][3], 1048576.0f, zero1);
+          acc[t][d][0] = __fmaf_rn(acc[t][d][0], 2097152.0f, zero0);
+          acc[t][d][1] = __fmaf_rn(acc[t][d][1], 2097152.0f, zero1);
+          acc[t][d][2] = __fmaf_rn(acc[t][d][2], 131072.0f, zero0);
+          acc[t][d][3] = __fmaf_rn(acc[t][d][3], 131072.0f, zero1);
         }
       }
-      finish_tile<BF16, D, NT>(p, work, r, head, row0, rows, k0 > 0 || k1 < keys, tile_begin + kTileUnits, tile_begin + span - 1, smem, m, l, acc);
+      finish_tile<BF16, D, NT>(p, work, r, head, row0, rows, k0 > 0 || k1 < keys, tile_begin + kTileUnits, tile_begin + span - 1, smem, m, sums, acc);
     }
     if (work.unit < work.end && work.rest == r.units(L::kRows, kUnitTokens, kTileUnits, p)) {
       do {

@@ -79,6 +79,17 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// Of numbers in the normal range.
+__device__ __forceinline__ float log2_approx(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float reciprocal(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   uint32_t u;
@@ -94,11 +105,12 @@ __device__ __forceinline__ uint32_t less_1152(uint32_t pair) {
 __device__ __forceinline__ uint32_t widen_lo(uint32_t u) { return less_1152(__byte_perm(u, 0x64646464u, 0x4140)); }
 __device__ __forceinline__ uint32_t widen_hi(uint32_t u) { return less_1152(__byte_perm(u, 0x64646464u, 0x4342)); }
 
-// Power of two that brings a row whose largest magnitude is `top` to just below 2^15 (2^112 at most, which brings the least bfloat16 numbers to 2^-21, a binary16 number), and the
+// Power of two that brings a row whose largest magnitude is `top` to just below 2^15 (2^MOST at most: 2^112 brings the least bfloat16 numbers to 2^-21, a binary16 number), and the
 // inverse.  Both stay in binary32's normal range; a row that is not finite is left alone.
+template <int MOST = 112>
 __device__ __forceinline__ float row_power(float top, float& inverse) {
   const int e = static_cast<int>(__float_as_uint(top) >> 23);              // biased exponent; 0: below the normal range
-  const int up = e < 255 ? min(14 - (e - 127), 112) : 0;
+  const int up = e < 255 ? min(14 - (e - 127), MOST) : 0;
   inverse = __uint_as_float(static_cast<uint32_t>(127 - up) << 23);
   return __uint_as_float(static_cast<uint32_t>(127 + up) << 23);
 }
