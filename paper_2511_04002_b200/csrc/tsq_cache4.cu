@@ -12,7 +12,7 @@
 namespace tsq {
 namespace {
 
-constexpr int kMoveThreads = 256;
+constexpr int kMoveThreads = 128;
 constexpr int kLaneNumbers = 16;          // of a row, by one thread: 32 bytes of it, 8 bytes of codes
 
 struct Move4Params {
@@ -227,15 +227,27 @@ __global__ void __launch_bounds__(kMoveThreads) load4_kernel(const Move4Params p
     const long long t = mine.first + n * M::kTogether;
     if (t >= p.tokens) break;
     const float zero = grid_zero(word[n]), scale = grid_scale(word[n]);
-    const uint64_t by = pack2f(scale, scale), less = pack2f(zero - 8388608.0f, zero - 8388608.0f);
+    const uint64_t by = pack2f(scale, scale);
+    // 0x6400 | nibble is 1024 + code, or 1024 + 16 code = 16 (64 + code) in the next four bits: the sums with the zero-point are exact in binary16
+    const __half2 less_even = __float2half2_rn(zero - 1024.0f), less_odd = __float2half2_rn(zero - 64.0f), sixteenth = __float2half2_rn(0.0625f);
     uint32_t out[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const uint32_t u = (k < 4 ? code[n].x : code[n].y) >> (8 * (k % 4));
-      float a, b;                                              // 2^23 + code less 2^23 - zero-point: exact
-      unpack2f(mul2(add2(pack2u((u & 15u) | 0x4b000000u, ((u >> 4) & 15u) | 0x4b000000u), less), by), a, b);
-      const uint32_t r = Elem<BF16>::pack_rn(a, b);
-      out[k] = Elem<BF16>::bits(__hmax2_nan(__hmin2_nan(Elem<BF16>::as2(r), Elem<BF16>::as2(limit)), Elem<BF16>::as2(limit | 0x80008000u)));
+    for (int k = 0; k < 2; ++k) {
+      const uint32_t w = k ? code[n].y : code[n].x;
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {                            // the codes e and e + 4
+        const uint32_t u = e < 2 ? w : w >> 8;
+        const float2 c = __half22float2(e & 1 ? __hfma2(Elem<false>::as2((u & 0x00f000f0u) | 0x64006400u), sixteenth, less_odd)
+                                              : __hadd2(Elem<false>::as2((u & 0x000f000fu) | 0x64006400u), less_even));
+        unpack2f(mul2(pack2f(c.x, c.y), by), x[e], x[e + 4]);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) out[4 * k + e] = Elem<BF16>::pack_rn(x[2 * e], x[2 * e + 1]);
+    }
+    if (!(grid_top(word[n]) <= (BF16 ? 3.0e38f : 65504.0f))) {  // a code may stand for more than the type holds
+#pragma unroll
+      for (int k = 0; k < 8; ++k) out[k] = Elem<BF16>::bits(__hmax2_nan(__hmin2_nan(Elem<BF16>::as2(out[k]), Elem<BF16>::as2(limit)), Elem<BF16>::as2(limit | 0x80008000u)));
     }
     store32(to + t * stride, out, whole);
   }
