@@ -391,10 +391,12 @@ tsq_status_t tsq_cache4_load(const tsq_cache4_t *cache, const int32_t *slots, in
  *   causal   1: row j of request i is the token at position lengths[i] - n_i + j and sees the positions up to its own.  0: every row of request i sees all of its lengths[i] tokens, whatever
  *            n_i is (a decoder's queries over an encoder's states, which were stored once).  Anything else is TSQ_ERR_INVALID_ARG
  * A value scale below 2^-60 counts as 2^-60 in the weights' scaling and as what it is in the value; the scales of the values that a row sees may differ by a factor of 2^80.  A token whose key or
- * value scale is NaN or infinite makes the rows NaN that see it, and no others.  With up to 32 query rows (max_query times q_heads / kv_heads) products with codes are exact and scales
- * come in in binary32.  With more, values and keys are brought to binary16 relative to the largest number that 16 neighbouring tokens can stand for, exactly as long as a token's codes reach down
- * to 0 or across it and its scale has seven significant bits and is no less than 2^-32 of that number; otherwise they are rounded once, or lose bits below 2^-35 of it.  The ranges that tsq_cache_attention
- * asks of scale, key scales and queries hold for the tokens' key scales; queries lie within +-2^120.
+ * value scale is NaN or infinite makes the rows NaN that see it, and no others.  Codes, scales and zero-points come in as follows.
+ *   up to 48 query rows (max_query times q_heads / kv_heads)  products with codes are exact, scales and zero-points come in in binary32
+ *   more   keys and values are formed in binary16, relative to the largest scale of 16 neighbouring tokens, which has to be below 2^120: exactly as long as the zero-point lies in -15 .. 0 and
+ *          the scale has seven significant bits and is no less than 2^-12 of that largest; otherwise zero-point times scale is rounded to binary16, and its sum with code times scale, and what lies
+ *          below 2^-19 of the largest scale is lost
+ * The ranges that tsq_cache_attention asks of scale, key scales and queries hold for the tokens' key scales; queries lie within +-2^120.
  * The workspace is of tsq_cache4_workspace's size or larger; one may be shared with calls over an 8-bit cache that it is large enough for.
  */
 tsq_status_t tsq_cache4_workspace(const tsq_cache4_t *cache, int64_t tokens, int32_t q_heads, int32_t requests, int32_t max_query,

@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(kMoveThreads) load4_kernel(const Move4Params p
 #pragma unroll
       for (int e = 0; e < 4; ++e) out[4 * k + e] = Elem<BF16>::pack_rn(x[2 * e], x[2 * e + 1]);
     }
-    if (!(grid_top(word[n]) <= (BF16 ? 3.0e38f : 65504.0f))) {  // a code may stand for more than the type holds
+    if (!(scale * fmaxf(fabsf(zero), fabsf(zero + 15.0f)) <= (BF16 ? 3.0e38f : 65504.0f))) {  // a code may stand for more than the type holds
 #pragma unroll
       for (int k = 0; k < 8; ++k) out[k] = Elem<BF16>::bits(__hmax2_nan(__hmin2_nan(Elem<BF16>::as2(out[k]), Elem<BF16>::as2(limit)), Elem<BF16>::as2(limit | 0x80008000u)));
     }

@@ -38,13 +38,6 @@ __device__ __forceinline__ int placed(int t, int c) {
   return (at ^ (D == 128 ? ((at >> 3) & 3) << 1 : ((at >> 3) & 1) << 1)) << 4;
 }
 
-// Four codes from 16 bits, in both halves of a word: the first two of them or, with `upper`, the others, shifted to bits 3 .. 6 and 7 .. 10.  There a nibble is the binary16 number code * 2^-21 or
-// code * 2^-17: numbers with an exponent of 0 and of 1 have the same unit 2^-24, so eleven bits are linear.  (The products take a number below the normal range at the exponent 2^-14 and cut
-// what is below 2^-24 of the largest product in their sum: 2^-17 of a code here, where nibbles in bits 0 .. 3 would lose 2^-14.)
-__device__ __forceinline__ uint32_t to_linear_bits(uint32_t u, bool upper) { return upper ? u >> 5 : mad_u32(u, 8u, 0u); }
-__device__ __forceinline__ uint32_t low_nibbles(uint32_t u) { return u & 0x00780078u; }
-__device__ __forceinline__ uint32_t high_nibbles(uint32_t u) { return u & 0x07800780u; }
-
 // The queries as the products with nibbles take them, brought to binary16 by a power of two per row.  Of eight dimensions the pairs (0, 4), (1, 5), (2, 6), (3, 7) go together;
 // odd ones meet codes that count sixteen times.  factor, sum: of the rows 8 t + 2 c and 8 t + 2 c + 1, what turns sums of products into <q, code>, and the row's sum in their measure.
 template <bool BF16, int D, int NT>

@@ -200,13 +200,12 @@ __device__ __forceinline__ void store_sector(void* at, const uint32_t (&w)[8], b
 template <int BITS>
 __host__ __device__ constexpr int nibble_column(int d) { return BITS == 8 ? d : (d & ~7) | (d & 3) << 1 | (d >> 2 & 1); }
 
-// The eight codes of a word plus their token's zero-point, exact in binary16, times its scale (in both halves): 0x6400 | nibble is 1024 + code, or 1024 + 16 code = 16 (64 + code).
-__device__ __forceinline__ uint4 widen_nibbles(uint32_t w, __half2 less_even, __half2 less_odd, __half2 scale) {
-  const auto even = [&](uint32_t u) { return Elem<false>::bits(__hmul2(__hadd2(Elem<false>::as2((u & 0x000f000fu) | 0x64006400u), less_even), scale)); };
-  const auto odd = [&](uint32_t u) {
-    return Elem<false>::bits(__hmul2(__hfma2(Elem<false>::as2((u & 0x00f000f0u) | 0x64006400u), __float2half2_rn(0.0625f), less_odd), scale));
-  };
-  return make_uint4(even(w), odd(w), even(w >> 8), odd(w >> 8));
+// The eight codes of a word as numbers in binary16, by one fused operation for two of them: nibbles * 2^-21 and 2^-17 (to_linear_bits) times scale * 2^21 and 2^17, plus zero-point * scale.
+__device__ __forceinline__ uint4 widen_nibbles(uint32_t w, __half2 by_low, __half2 by_high, __half2 zero) {
+  const auto low = [&](uint32_t u) { return Elem<false>::bits(__hfma2(Elem<false>::as2(low_nibbles(u)), by_low, zero)); };
+  const auto high = [&](uint32_t u) { return Elem<false>::bits(__hfma2(Elem<false>::as2(high_nibbles(u)), by_high, zero)); };
+  const uint32_t first = to_linear_bits(w, false), last = to_linear_bits(w, true);
+  return make_uint4(low(first), high(first), low(last), high(last));
 }
 
 // Shared-memory descriptors of 128-byte swizzled operands: rows of 128 bytes, eight rows to a 1024-byte atom.
@@ -325,9 +324,9 @@ __host__ __device__ constexpr uint32_t arrivals_of(int bar) {  // a group's warp
 // Bound by the chain scores -> weights -> sums -> scores of each group: about 4400 clocks a step where the products take 2050 and the exponentials, 16 per SM and clock, as many.
 // 8192 tokens, 32 query heads on 8 key heads: 600 to 634 us, 865 to 910 TFLOP/s (bf16 or fp16, heads of 128), at the 1.55 GHz that the power cap leaves.
 //
-// BITS = 4: a token has a scale and a zero-point of its own, which the widening groups apply: (code + zero-point) * scale is a whole number of at most 11 bits as long as the
-// range of the token reaches 0, and so exact in binary16 (otherwise rounded once, 2^-12).  Scales are taken relative to a granule's largest number, a power of two that takes the place of the
-// page's scale: what the softmax and product warps do is the same for both widths.
+// BITS = 4: a token has a scale and a zero-point of its own, which the widening groups apply: with a scale of seven significant bits and a range of the token that reaches 0, (code + zero-point) * scale
+// has at most 11 bits and is exact in binary16 (otherwise the product of the last two is rounded, and the sum).  Scales are taken relative to a power of two above a granule's largest, which takes the
+// place of the page's scale: what the softmax and product warps do is the same for both widths.
 template <bool BF16, int D, int BITS>
 __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const AttentionParams p) {
   using Sh = Shared<D>;
@@ -768,12 +767,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
       }
     } else {
       constexpr int kChunks = D / 32;                      // 16-byte chunks of a token's codes
-      constexpr int kItems = kKeys * kChunks / 128;        // per thread and step
-      // A warp has 32 neighbouring tokens, two granules.  Eight neighbouring lanes have two chunks of four neighbouring tokens, whose parts the swizzle puts in different banks.
-      const int token0 = D == 128 ? 32 * w + ((lane >> 1) & 3) + ((lane >> 4) << 2) : 32 * w + (lane >> 1);
-      const int chunk = D == 128 ? (lane & 1) | ((lane >> 3) & 1) << 1 : lane & 1;
+      constexpr int kItems = kKeys * kChunks / 128;        // per thread and step, half of them in each of the warp's two granules
       constexpr int kItemTokens = 32 / kItems;             // from one of a thread's items to the next
-      unsigned char* const to = smem_at + (values ? Sh::kV : Sh::kK) + (chunk / 2) * kHalf;
+      // Eight neighbouring lanes have two chunks of four neighbouring tokens, whose parts the swizzle puts in different banks.
+      const int token0 = D == 128 ? ((lane >> 1) & 3) + ((lane >> 4) << 2) : lane >> 1;  // of the first item in its granule
+      const int chunk = D == 128 ? (lane & 1) | ((lane >> 3) & 1) << 1 : lane & 1;
+      unsigned char* const to = smem_at + (values ? Sh::kV : Sh::kK) + (chunk / 2) * kHalf + (32 * w + token0) * 128;
+      const uint32_t page_rows = static_cast<uint32_t>(p.kv_heads) << p.page_shift, mask = (1u << p.page_shift) - 1u;
       uint4 raw[kItems];
       uint32_t k_word[kItems], v_word[kItems];             // scales and zero-points; 0 where there is no token.  The values' group has no use for the keys'
       int pages[2];                                        // of the next step's granules
@@ -784,22 +784,41 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
       bool there[2];                                       // of the step whose codes have been fetched: granules whose page is in the cache
       auto fetch = [&](int j) {
 #pragma unroll
-        for (int g = 0; g < 2; ++g) there[g] = static_cast<unsigned>(pages[g]) < static_cast<unsigned>(p.pages);
+        for (int g = 0; g < 2; ++g) {
+          const int first = j * kKeys + 32 * w + 16 * g;
+          there[g] = static_cast<unsigned>(pages[g]) < static_cast<unsigned>(p.pages);
+          const unsigned long long at = static_cast<unsigned long long>(static_cast<uint32_t>(pages[g])) * page_rows +
+                                        ((static_cast<uint32_t>(place.head) << p.page_shift) + (static_cast<uint32_t>(first) & mask) + token0);
+          const int8_t* const from = codes + at * (D / 2) + chunk * 16;
+          const uint32_t *const k_from = p.k_grid + at, *const v_from = p.v_grid + at;
+          const int left = place.r.keys - first - token0;
 #pragma unroll
-        for (int it = 0; it < kItems; ++it) {
-          const int g = it * kItemTokens / 16, token = j * kKeys + token0 + it * kItemTokens;
-          raw[it] = make_uint4(0u, 0u, 0u, 0u);
-          k_word[it] = v_word[it] = 0u;
-          if (there[g]) {
-            const long long at = ((static_cast<long long>(pages[g]) * p.kv_heads + place.head) << p.page_shift) + (token & ((1 << p.page_shift) - 1));
-            raw[it] = *(reinterpret_cast<const uint4*>(codes + at * (D / 2)) + chunk);
-            if (token < place.r.keys) {
-              v_word[it] = p.v_grid[at];
-              if (!values) k_word[it] = p.k_grid[at];
+          for (int n = 0; n < kItems / 2; ++n) {
+            const int it = g * (kItems / 2) + n;
+            raw[it] = make_uint4(0u, 0u, 0u, 0u);
+            k_word[it] = v_word[it] = 0u;
+            if (there[g]) {
+              raw[it] = *reinterpret_cast<const uint4*>(from + n * (kItemTokens * D / 2));
+              if (n * kItemTokens < left) {
+                v_word[it] = v_from[n * kItemTokens];
+                if (!values) k_word[it] = k_from[n * kItemTokens];
+              }
             }
           }
         }
       };
+      // Scales are taken relative to a power of two above the granule's largest: they come to below 2^-5, so that times 2^21 they stay in binary16.  e: that one's biased exponent.
+      auto exponent_of = [&](const uint32_t (&word)[kItems], int g) {
+        uint32_t most = 0u;
+#pragma unroll
+        for (int n = 0; n < kItems / 2; ++n) {
+          const uint32_t e = word[g * (kItems / 2) + n] & 0x7f80u;
+          most = max(most, e == 0x7f80u ? 0u : e);
+        }
+        return __reduce_max_sync(kFull, most) >> 7;
+      };
+      auto power = [](uint32_t e) { return __uint_as_float((e < 248u ? 248u - e : 1u) << 23); };
+      auto inverse_power = [](uint32_t e) { return __uint_as_float((e + 6u) << 23); };
       int j = place.k0;
       bool more = true;
       fetch_pages(j);
@@ -810,42 +829,37 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
           j = place.k0;
         }
         if (more) fetch_pages(j);
-        // the granules' powers of two, and the tokens' scales relative to them
-        float k_power[2], v_power[2], k_inverse[2], v_inverse[2];
+        uint32_t k_e[2] = {0u, 0u}, v_e[2];
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-          float k_top = 0.0f, v_top = 0.0f;
-#pragma unroll
-          for (int it = g * kItems / 2; it < (g + 1) * kItems / 2; ++it) {
-            k_top = fmaxf(k_top, grid_top(k_word[it]));
-            v_top = fmaxf(v_top, grid_top(v_word[it]));
-          }
-          // numbers that are not negative are in the order of their bits
-          if (!values) k_power[g] = row_power(__uint_as_float(__reduce_max_sync(kFull, __float_as_uint(k_top))), k_inverse[g]);
-          v_power[g] = row_power(fmaxf(__uint_as_float(__reduce_max_sync(kFull, __float_as_uint(v_top))), kLeastScale), v_inverse[g]);
+          if (!values) k_e[g] = exponent_of(k_word, g);
+          v_e[g] = max(exponent_of(v_word, g), 67u);       // kLeastScale
         }
         const uint32_t buffer = n & 1u;
         if (!wait(free + buffer, ((n >> 1) & 1u) ^ 1u)) break;
         if (!values && lane < 2) {                         // nothing of a page that is not there is seen
-          const bool first = lane == 0, here = first ? there[0] : there[1];
-          const float v_by = first ? v_inverse[0] : v_inverse[1];
+          const bool here = lane == 0 ? there[0] : there[1];
+          const uint32_t ke = lane == 0 ? k_e[0] : k_e[1], ve = lane == 0 ? v_e[0] : v_e[1];
           reinterpret_cast<float4*>(smem_at + Sh::kScales)[(n % kMeta) * kGranules + 2 * w + lane] =
-              here ? make_float4(first ? k_inverse[0] : k_inverse[1], static_cast<float>(static_cast<int>(__float_as_uint(v_by) >> 23) - 127), first ? v_power[0] : v_power[1], 0.0f)
-                   : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
+              here ? make_float4(inverse_power(ke), static_cast<float>(static_cast<int>(ve) - 121), power(ve), 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
         }
 #pragma unroll
         for (int it = 0; it < kItems; ++it) {
-          const int g = it * kItemTokens / 16, token = token0 + it * kItemTokens;
-          const uint32_t word = values ? v_word[it] : k_word[it];
-          const bool fine = grid_is_number(v_word[it]) && grid_is_number(k_word[it]);
-          // a token whose scale is no number makes the rows NaN that see it, and no others: by its scores
-          const float scale = fine ? grid_scale(word) * (values ? v_power[g] : k_power[g]) : values ? 0.0f : NAN;
-          const float zero = grid_zero(word);
-          const __half2 s2 = __float2half2_rn(scale), less_even = __float2half2_rn(zero - 1024.0f), less_odd = __float2half2_rn(zero - 64.0f);
+          const int g = it / (kItems / 2), token = 16 * g + it % (kItems / 2) * kItemTokens;
+          float scale;
+          if (values) {
+            scale = grid_is_number(v_word[it]) ? grid_scale(v_word[it]) * power(v_e[g]) : 0.0f;
+          } else {                                         // a token of which a scale is no number makes the rows NaN that see it, and no others: by its scores
+            const float ks = grid_scale(k_word[it]);
+            scale = __fmaf_rn(ks, power(k_e[g]), __fmaf_rn(ks, 0.0f, grid_scale(v_word[it]) * 0.0f));
+          }
+          const float zero = grid_zero(values ? v_word[it] : k_word[it]);
+          const __half2 by_low = __float2half2_rn(scale * 2097152.0f), by_high = __float2half2_rn(scale * 131072.0f), add = __float2half2_rn(zero * scale);
           unsigned char* const at = to + buffer * Sh::kOperand + token * 128;
           const uint32_t u[4] = {raw[it].x, raw[it].y, raw[it].z, raw[it].w};
+          // eight tokens further the swizzle is the same
 #pragma unroll
-          for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(at + (((4 * (chunk % 2) + k) ^ (token & 7)) << 4)) = widen_nibbles(u[k], less_even, less_odd, s2);
+          for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(at + (((4 * (chunk % 2) + k) ^ (token0 & 7)) << 4)) = widen_nibbles(u[k], by_low, by_high, add);
         }
         fence_proxy_async_smem();
         bar_arrive(bars + 8 * (full + buffer));

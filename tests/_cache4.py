@@ -67,7 +67,7 @@ class Setup4(Setup):
 def attention_ref(s, q, starts, lengths, scale, causal=True, table=None):
     """Rows in 64 bits, and how far a kernel may be off that rounds weights to binary16 relative to the largest of the row times its token's scale, sums in binary32 and
     rounds the row once: weights half a step (2^-11) and 2^-25 at the small end; each score's binary32 sum D + 8 roundings of its terms' magnitudes, which are those of code times query and of
-    zero-point times query apart; keys and values that are rounded to binary16 half a step; the sums over the tokens one rounding of 2^-23 for each 16 of them and for each part; 2^-20 for the exponential
+    zero-point times query apart; keys and values that are rounded to binary16 half a step of themselves and of their zero-point times the scale; the sums over the tokens one rounding of 2^-23 for each 16 of them and for each part; 2^-20 for the exponential
     and the quotient."""
     table = (s.table if table is None else table).cpu()
     out, tol = torch.full(q.shape, math.nan, dtype=torch.float64), torch.zeros(q.shape, dtype=torch.float64)
@@ -82,9 +82,10 @@ def attention_ref(s, q, starts, lengths, scale, causal=True, table=None):
         for h in range(s.H):
             def rows(codes, grid):
                 x = numbers(codes[safe, h], grid[safe, h]).reshape(-1, s.D)[:L].cpu()
-                size = (scales(grid[safe, h]).double() * (15 + zeros(grid[safe, h]).abs())).reshape(-1)[:L].cpu()   # of a term
-                return torch.where(ok[:, None], x, 0.0), torch.where(ok, size, 0.0)
-            (k, k_size), (v, v_size) = rows(s.k_codes, s.k_grid), rows(s.v_codes, s.v_grid)
+                step, zero = (f(grid[safe, h]).double().reshape(-1)[:L].cpu() for f in (scales, zeros))
+                # the numbers, the size of a term of their sums, what two roundings to binary16 go by
+                return torch.where(ok[:, None], x, 0.0), torch.where(ok, step * (15 + zero.abs()), 0.0), torch.where(ok[:, None], x.abs() + (step * zero.abs())[:, None], 0.0)
+            (k, k_size, k_round), (v, v_size, v_round) = rows(s.k_codes, s.k_grid), rows(s.v_codes, s.v_grid)
             k_half = 0.0 if exact(s.k_grid[safe, h].reshape(-1)[:L]) else 2.0 ** -11
             v_half = 0.0 if exact(s.v_grid[safe, h].reshape(-1)[:L]) else 2.0 ** -11
             for j in range(n):
@@ -98,8 +99,8 @@ def attention_ref(s, q, starts, lengths, scale, causal=True, table=None):
                 w = torch.softmax(score, -1)
                 o = w @ v[:see]
                 sums = x.abs().sum(-1, keepdim=True) * k_size[:see]
-                off = ((sums * (s.D + 8) * 2.0 ** -24 + (x.abs() @ k[:see].abs().t()) * k_half) * abs(scale)).amax(-1, keepdim=True)
-                near = w @ v[:see].abs() * (2.0 ** -11 + 2 * off + 2.0 ** -20 + v_half) + (w @ v_size[:see])[:, None] * (see / 16 + 8) * 2.0 ** -23
+                off = ((sums * (s.D + 8) * 2.0 ** -24 + (x.abs() @ k_round[:see].t()) * k_half) * abs(scale)).amax(-1, keepdim=True)
+                near = w @ v[:see].abs() * (2.0 ** -11 + 2 * off + 2.0 ** -20) + w @ v_round[:see] * v_half + (w @ v_size[:see])[:, None] * (see / 16 + 8) * 2.0 ** -23
                 near = near + see * 2.0 ** -25 * v_size[:see].max()
                 out[starts[i] + j, h * G:(h + 1) * G] = o
                 tol[starts[i] + j, h * G:(h + 1) * G] = near + HALF_STEP[s.dtype] * (o.abs() + near) + 2.0 ** -25
