@@ -55,7 +55,7 @@ struct AttentionParams {
 };
 
 constexpr int kFewQueryRows = 32;
-// Up to so many query rows (query heads of a key head times max_query): tiles of 8 rows, four CTAs per SM, or of 16 rows, three.  A CTA has a counter for each level of
+// Up to so many query rows (query heads of a key head times max_query; the 4-bit cache has a limit of its own): tiles of 8 rows, four CTAs per SM, or of 16 rows, three.  A CTA has a counter for each level of
 // the sums of parts and two slots of a tile's accumulators, maxima and sums in the workspace.
 constexpr int kRowsCtasPerSm = 4;            // the more of the two
 constexpr int kRowsTile = 16;                // likewise

@@ -33,3 +33,14 @@ def test_every_quotient(fmt, ulp):
             halves += int((quotient[quotient <= 128] % 1 == 0.5).sum())
             assert np.array_equal(rounded(use, inverse), want) and np.array_equal(rounded(-use, inverse), -want)
     assert halves > 1000
+
+
+def test_nibbles_are_numbers_where_they_stand():
+    """to_linear_bits (csrc/tsq_cache_device.cuh): the lower eleven bits of a binary16 number count in one unit, 2^-24, whether the eleventh is set or not."""
+    n = np.arange(2048, dtype=np.uint16)
+    assert np.array_equal(n.view(np.float16).astype(np.float64), n * 2.0 ** -24)
+    words = np.arange(65536, dtype=np.uint32)
+    for shifted, first in ((words << 3, 0), (words >> 5, 2)):
+        for mask, unit, k in ((0x0078, 2.0 ** -21, first), (0x0780, 2.0 ** -17, first + 1)):
+            got = (shifted & mask).astype(np.uint16).view(np.float16).astype(np.float64)
+            assert np.array_equal(got, (words >> (4 * k) & 15) * unit)
