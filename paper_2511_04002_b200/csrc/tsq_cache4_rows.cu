@@ -104,8 +104,8 @@ struct Layout {
 // The factors 2^21 and 2^17 come in at a tile's end.
 //
 // Bound by the ALU pipe (half a pass per clock; 5.5 of its operations for 8 codes) and HBM together where the cache is long: 5.6 TB/s from 16000 tokens a request on (64 requests), 4.3 TB/s with what it
-// costs to begin and to end for 64 requests of 500 to 8000 tokens (297 MB, 68 to 73 us); by the chain lengths -> table -> codes -> sums where it is short (one of 1001 tokens: 8.5 us).  Steps of 16 tokens'
-// codes were 32-token ones from the start: what a step costs besides its codes is shared by twice as many.  Tried and not kept: products of e4m3 with the queries in parts (these instructions come
+// costs to begin and to end for 64 requests of 500 to 8000 tokens (297 MB, 68 to 73 us); by the chain lengths -> table -> codes -> sums where it is short (one of 1001 tokens: 8.5 us).  A step has 32
+// tokens, twice as many as over the 8-bit cache: what it costs besides its codes is shared by as many bytes.  Tried and not kept: products of e4m3 with the queries in parts (these instructions come
 // out as conversions and products in binary16: 83 us); the next step's scores formed during this one's sums (70.8); the next tile's first codes fetched before a tile's end (68.3, and 28.4 -> 29.5 for many
 // short tiles); shares by how early a CTA is launched (70.5).
 template <bool BF16, int D, int NT>

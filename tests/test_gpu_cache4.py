@@ -175,6 +175,14 @@ def test_attention_of_drafted_tokens(causal, dtype, D, P, H, group, added):
     check_attention(Setup4(dtype, [16, 700, 33, 129, 2100], H, D, P, seed=group), added, group, causal=causal)
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("D,P,H,group,added", [(128, 64, 2, 8, [6, 5, 1, 3, 6]), (64, 16, 1, 16, [3, 2, 1, 0, 3]), (128, 16, 1, 3, [16, 9, 13, 11, 7]), (64, 128, 2, 1, [16, 33, 48, 17, 1]),
+                                               (128, 32, 2, 7, [7, 7, 1, 2, 7]), (64, 64, 1, 49, [1, 1, 1, 1, 1])])
+def test_attention_around_the_most_rows_of_the_row_kernel(dtype, D, P, H, group, added):
+    # 48 rows in tiles of 16, the last one full or not; 49
+    check_attention(Setup4(dtype, [16, 700, 50, 129, 2100], H, D, P, seed=group), added, group)
+
+
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("D,P,H,group,held,added", [
@@ -270,6 +278,33 @@ def test_large_and_small_queries_scales_and_a_negative_factor(dtype, added):
 def test_zero_points_anywhere(dtype, added, zero):
     # ranges that do not reach 0: codes' sums and the zero-points' cancel, operands are rounded
     check_attention(Setup4(dtype, [130, 77, 260], 2, 64, 16, seed=14, zero=zero), [added] * 3, 2, scale=0.125 / (1 + max(abs(z) for z in zero)))
+
+
+@pytest.mark.parametrize("added", [1, 5, 60])
+def test_tokens_of_zeros_and_of_one_number(added):
+    # stored: pages of zeros, tokens of one number throughout, tokens of tiny and of large numbers side by side
+    s = Setup4(BF16, [200, 90], 2, 64, 16, seed=15)
+    slots = s.slots_of(0, 0, 200) + s.slots_of(1, 0, 90)
+    k, v = s.rows(290, 2), s.rows(290, 2)
+    k[16:48], v[32:64] = 0.0, 0.0
+    v[70], v[71], k[72], v[200], k[201] = 5.0, -0.001, 3.0, 0.0, 0.0
+    v[80:90] *= 2.0 ** -12
+    v[85] *= 2.0 ** 16
+    check_store(s, k, v, slots)
+    check_attention(s, [added, added], 3)
+    check_attention(s, [added, added], 3, causal=False)
+
+
+@pytest.mark.parametrize("added", [1, 33])
+@pytest.mark.parametrize("log2_k,log2_v", [(-30, 100), (20, -38), (60, 60), (-20, -20)])
+def test_scales_far_from_one(added, log2_k, log2_v):
+    s = Setup4(BF16, [300, 77], 2, 128, 32, seed=16)
+    used = s.table[0, :10].long()
+    s.k_grid[used], s.v_grid[used] = word_of(scales(s.k_grid[used]) * 2.0 ** log2_k, zeros(s.k_grid[used])), word_of(scales(s.v_grid[used]) * 2.0 ** log2_v, zeros(s.v_grid[used]))
+    tail = int(s.table[0, 9])                                           # its places behind the request stay rubbish
+    s.k_grid[tail, :, 300 % 32:] = int(word_of(torch.tensor([math.nan]), torch.tensor([5])))
+    s.v_grid[tail, :, 300 % 32:] = int(word_of(torch.tensor([math.inf]), torch.tensor([5])))
+    check_attention(s, [added, added], 2, scale=128 ** -0.5 * 2.0 ** -max(log2_k, 0))
 
 
 @pytest.mark.parametrize("added", [1, 33])
@@ -396,7 +431,7 @@ def check_parts(dtype, held, added, D, P, H, group, causal=True):
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16])
-@pytest.mark.parametrize("added,group", [(1, 1), (4, 5)])
+@pytest.mark.parametrize("added,group", [(1, 1), (4, 5), (3, 16)])
 @pytest.mark.parametrize("keys", [128 * n + more for n, more in ((6, 1), (13, 128), (14, 3), (15, 17), (252, 64), (253, 1), (254, 95), (255, 128), (470, 2), (625, 0), (1700, 9))])
 def test_parts_of_one_tile_of_few_rows(dtype, added, group, keys):
     check_parts(dtype, [keys], [added], 128 if keys % 2 else 64, 64, 1, group)
