@@ -628,26 +628,74 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
       // a slot holds columns of 128 rows: maxima, sums, then the dimensions
       constexpr long long kSlot = 128ll * (D + 2);
       float* const slot = p.partials + (4ll * blockIdx.x + 2 * t + (place.k0 > 0 ? 0 : 1)) * kSlot + row;
-      slot[0] = l != 0.0f ? m : -INFINITY;                  // a row whose scores are no numbers has a sum that is none
-      slot[128] = l;
-      if (any) {
+      const unsigned long long tile_begin = place.unit - place.from + kTileSteps;  // its first step
+      const int first = owner_of(tile_begin, total, ctas), last = owner_of(tile_begin + place.steps - 1, total, ctas);
+      unsigned int* const counter = p.counters + 8 * first + warp;  // a warp's rows by themselves
+      const float m_part = l != 0.0f ? m : -INFINITY;       // a row whose scores are no numbers has a sum that is none
+      // One of two parts that comes last adds the other's to its own where it stands; whether it does so is mostly known before its own is written.
+      const bool two = last == first + 1;
+      unsigned int done = 0u;
+      if (two) {
+        if (lane == 0) asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(done) : "l"(counter) : "memory");
+        done = __shfl_sync(kFull, done, 0);
+      }
+      if (done != 0u) {
+        if (lane == 0) *counter = 0u;                       // as the last arrival leaves it
+      } else {
+        slot[0] = m_part;
+        slot[128] = l;
+        if (any) {
+#pragma unroll 1
+          for (int d = 0; d < D; d += 32) {
+            uint32_t o[32];
+            tm_load32(o, o_at + d);
+            tm_wait_ld(o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) slot[128 * (2 + d + e)] = __uint_as_float(o[e]);
+          }
+          tm_fence_before();
+        }
+        __threadfence();
+        __syncwarp();
+        if (lane == 0) done = atomicInc(counter, static_cast<unsigned>(last - first));
+        done = __shfl_sync(kFull, done, 0);
+      }
+      if (two && done != 0u) {
+        __threadfence();
+        const int other = static_cast<int>(blockIdx.x) == first ? last : first;
+        const float* const part = p.partials + (4ll * other + 2 * t + (other == first ? 1 : 0)) * kSlot + row;
+        const float m_other = __ldcg(part), l_other = __ldcg(part + 128), top = fmaxf(m_part, m_other);
+        const float w_own = m_part == -INFINITY ? 0.0f : exp2_fast(m_part - top), w_other = m_other == -INFINITY ? 0.0f : exp2_fast(m_other - top);
+        const float all = (m_part == -INFINITY ? 0.0f : l * w_own) + (m_other == -INFINITY ? 0.0f : l_other * w_other);
+        const float by = all == 0.0f ? 0.0f : 1.0f / all;
+        float x[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) x[e] = __ldcg(part + 128 * (2 + e));
 #pragma unroll 1
         for (int d = 0; d < D; d += 32) {
           uint32_t o[32];
-          tm_load32(o, o_at + d);
+          tm_load32(o, o_at + d);                          // nothing of it counts where the group had no step
           tm_wait_ld(o);
+          // a part of maximum -Inf has seen nothing: what stands in its place does not count, whatever it is
 #pragma unroll
-          for (int e = 0; e < 32; ++e) slot[128 * (2 + d + e)] = __uint_as_float(o[e]);
+          for (int e = 0; e < 32; ++e)
+            x[e] = (0.0f + ((m_part == -INFINITY ? 0.0f : __uint_as_float(o[e]) * w_own) + (m_other == -INFINITY ? 0.0f : x[e] * w_other))) * by;  // as sums of more parts begin
+          if (live) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 16) {
+              uint32_t w[8];
+#pragma unroll
+              for (int k = 0; k < 8; ++k) w[k] = Elem<BF16>::pack_rn(x[e + nibble_column<BITS>(2 * k)], x[e + nibble_column<BITS>(2 * k + 1)]);
+              store_sector(to + d + e, w, out_sectors);
+            }
+          }
+          if (d + 32 < D) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) x[e] = __ldcg(part + 128 * (2 + d + 32 + e));
+          }
         }
         tm_fence_before();
-      }
-      const unsigned long long tile_begin = place.unit - place.from + kTileSteps;  // its first step
-      const int first = owner_of(tile_begin, total, ctas), last = owner_of(tile_begin + place.steps - 1, total, ctas);
-      __threadfence();
-      __syncwarp();
-      unsigned int done = 0u;                              // a warp's rows by themselves
-      if (lane == 0) done = atomicInc(p.counters + 8 * first + warp, static_cast<unsigned>(last - first));
-      if (__shfl_sync(kFull, done, 0) == static_cast<unsigned>(last - first)) {
+      } else if (!two && done == static_cast<unsigned>(last - first)) {
         __threadfence();
         // two parts and 32 dimensions at a time, without a branch between the loads, so that all of them are on their way; behind the last part its data again, not counted
         const auto part_at = [&](int n) { return p.partials + (4ll * min(n, last) + 2 * t + (min(n, last) == first ? 1 : 0)) * kSlot + row; };
