@@ -326,7 +326,7 @@ __host__ __device__ constexpr uint32_t arrivals_of(int bar) {  // a group's warp
 //
 // BITS = 4: a token has a scale and a zero-point of its own, which the widening groups apply: with a scale of seven significant bits and a range of the token that reaches 0, (code + zero-point) * scale
 // has at most 11 bits and is exact in binary16 (otherwise the product of the last two is rounded, and the sum).  Scales are taken relative to a power of two above a granule's largest, which takes the
-// place of the page's scale: what the softmax and product warps do is the same for both widths.  8192 tokens as above 569 to 621 us from box to box, 5 requests in chunks 345 to 368; with a sum and a
+// place of the page's scale: what the softmax and product warps do is the same for both widths.  8192 tokens as above 541 to 621 us from box to box, 5 requests in chunks 345 to 368; with a sum and a
 // product for two codes instead of one fused operation 577 and 365.
 template <bool BF16, int D, int BITS>
 __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const AttentionParams p) {
@@ -660,6 +660,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
         if (lane == 0) done = atomicInc(counter, static_cast<unsigned>(last - first));
         done = __shfl_sync(kFull, done, 0);
       }
+      __syncwarp();                                         // what lane 0 has seen of the other parts, every lane sees
       if (two && done != 0u) {
         __threadfence();
         const int other = static_cast<int>(blockIdx.x) == first ? last : first;
