@@ -356,6 +356,7 @@ class Cache4(_Paged):
     @classmethod
     def alloc(cls, dtype: torch.dtype, kv_heads: int, head_dim: int, pages: int, page_tokens: int = 64, device: int = 0) -> "Cache4":
         """A cache over tensors of its own, every code, scale and zero-point 0."""
+        assert head_dim % 2 == 0, "two dimensions share a byte: head_dim must be even"
         dev = torch.device("cuda", device)
         codes = [torch.zeros((pages, kv_heads, page_tokens, head_dim // 2), dtype=torch.uint8, device=dev) for _ in range(2)]
         grids = [torch.zeros((pages, kv_heads, page_tokens), dtype=torch.int32, device=dev) for _ in range(2)]

@@ -89,3 +89,9 @@ def test_tensors_on_the_host():
     codes, grid = torch.zeros((2, 1, 16, 32), dtype=torch.uint8), torch.zeros((2, 1, 16), dtype=torch.int32)
     with pytest.raises(AssertionError):
         B.Cache4(torch.float16, codes, codes, grid, grid)
+
+
+def test_a_cache_of_half_bytes():
+    import torch
+    with pytest.raises(AssertionError, match="even"):
+        B.Cache4.alloc(torch.float16, 2, 129, 4)
