@@ -70,8 +70,9 @@ constexpr int kStoreItems = 2;
 template <bool BF16>
 constexpr uint32_t kPlainPattern = BF16 ? 0x7e81u : 0x7c00u;  // below it: within 2^126, and finite
 
-// Scale, zero-point and what the codes are formed with.  Halves are rounded away from zero by the product with an inverse that is 2^-20 too large: x / s that is a half (and only that
-// can be within 2^-11 of one in proportion: x has 11 significant bits, s seven) comes out beyond it, everything else stays on its side of the next half, |x / s| being 128 at most.
+// Scale, zero-point and what the codes are formed with.  Halves are rounded away from zero by the product with an inverse that is 2^-20 too large, give or take the reciprocal's unit and the product's
+// half one: 2^-21 to 2^-19.  x / s that is a half comes out beyond it.  Everything else stays on its side of the next half h / 2: x = X 2^a has 11 significant bits and s = S 2^b seven, so the two differ
+// by 1 / (h S) of the half at least, and that is above 2^-15 as long as |x / s| <= 128 (h <= 255, S <= 127; the nearest is 127.496 beside 127.5).
 struct Grid4 {
   float inverse, zero;
   uint32_t word;
