@@ -393,9 +393,10 @@ tsq_status_t tsq_cache4_load(const tsq_cache4_t *cache, const int32_t *slots, in
  * A value scale below 2^-60 counts as 2^-60 in the weights' scaling and as what it is in the value; the scales of the values that a row sees may differ by a factor of 2^80.  A token whose key or
  * value scale is NaN or infinite makes the rows NaN that see it, and no others.  Codes, scales and zero-points come in as follows.
  *   up to 48 query rows (max_query times q_heads / kv_heads)  products with codes are exact, scales and zero-points come in in binary32
- *   more   keys and values are formed in binary16, relative to the largest scale of 16 neighbouring tokens, which has to be below 2^120: exactly as long as the zero-point lies in -15 .. 0 and
- *          the scale has seven significant bits and is no less than 2^-12 of that largest; otherwise zero-point times scale is rounded to binary16, and its sum with code times scale, and what lies
- *          below 2^-19 of the largest scale is lost
+ *   more   keys and values are formed in binary16, each relative to its own scale or, where 16 neighbouring tokens' scales lie within a factor of 2^4, to the largest of theirs: exactly as long as
+ *          the zero-point lies in -15 .. 0 and the scale has seven significant bits; otherwise zero-point times scale is rounded to binary16, and its sum with code times scale.  Weights are rounded
+ *          relative to up to 2^5 times the largest of their row times its token's scale: 2^-20 of it at the small end instead of 2^-25.  A scale of 2^120 or more counts as infinite; what a value scale
+ *          is below 2^-79 is lost
  * The ranges that tsq_cache_attention asks of scale, key scales and queries hold for the tokens' key scales; queries lie within +-2^120.
  * The workspace is of tsq_cache4_workspace's size or larger; one may be shared with calls over an 8-bit cache that it is large enough for.
  */

@@ -18,7 +18,6 @@ __device__ __forceinline__ float inverse_of_scale(float s) { return 1.0f / fmaxf
 // A word of the 4-bit cache's grids: the scale, a bfloat16 number, in the lower half, the zero-point, signed, in the upper one.
 __device__ __forceinline__ float grid_scale(uint32_t word) { return __uint_as_float(word << 16); }
 __device__ __forceinline__ float grid_zero(uint32_t word) { return static_cast<float>(static_cast<int32_t>(word) >> 16); }
-__device__ __forceinline__ bool grid_is_number(uint32_t word) { return (word & 0x7f80u) != 0x7f80u; }
 // Four codes from 16 bits, in both halves of a word: the first two of them or, with `upper`, the others, shifted to bits 3 .. 6 and 7 .. 10.  There a nibble is the binary16 number code * 2^-21 or
 // code * 2^-17: numbers with an exponent of 0 and of 1 have the same unit 2^-24, so eleven bits are linear.  (The products take a number below the normal range at the exponent 2^-14 and cut
 // what is below 2^-24 of the largest product in their sum: 2^-17 of a code here, where nibbles in bits 0 .. 3 would lose 2^-14.)

@@ -16,7 +16,15 @@ constexpr int kSoftmaxRegs = 136, kWidenRegs = 80, kProductRegs = 48, kLaunchReg
 constexpr int kTileSteps = 4;                // what beginning and ending a tile costs, in steps
 // Most parts of a tile, on the average: adding a part up takes 1.7 us, a step 2.3 us (one tile of 235 steps in 148 parts 300 us, in 16 80 us).
 constexpr unsigned long long kMostParts = 16;
-constexpr int kMeta = 4;                     // steps whose scales are kept
+// 4 bits: powers of two by which a token's scale may be below the largest of its granule and its weights and numbers still go relative to that one.  Up to 12 numbers would come out the same;
+// weights lose as many bits at the small end as the granule's scale is above those that count.
+constexpr uint32_t kNearScales = 4;
+constexpr uint32_t kMostExponent = 247;      // of a scale, biased: 2^120 and more counts as infinite
+constexpr uint32_t kLeastExponent = 67;      // of a value's scale: kLeastScale
+// What a scale with the biased exponent e is taken relative to, 2^(e - 121): it comes to 2^-6 to 2^-5, so that times 2^21 it stays in binary16.  Its inverse and logarithm.
+__device__ __forceinline__ float scale_of_exponent(uint32_t e) { return __uint_as_float((e + 6u) << 23); }
+__device__ __forceinline__ float inverse_of_exponent(uint32_t e) { return __uint_as_float((248u - e) << 23); }
+__device__ __forceinline__ float log2_of_exponent(uint32_t e) { return static_cast<float>(static_cast<int>(e) - 121); }
 constexpr uint32_t kPolls = 1u << 20;        // of a wait inside the CTA: tens of milliseconds at least, where a sound one takes microseconds
 
 // ---- barriers, tensor memory, products -----------------------------------------------------------
@@ -93,6 +101,11 @@ __device__ __forceinline__ void tm_store32(uint32_t at, const uint32_t (&v)[32])
 }
 __device__ __forceinline__ void tm_store16(uint32_t at, const uint32_t (&v)[16]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at), TSQ_W8(v, 0), TSQ_W8(v, 8) : "memory");
+}
+__device__ __forceinline__ float shared_float(uint32_t at) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at));
+  return v;
 }
 __device__ __forceinline__ float4 shared_float4(uint32_t at) {
   float4 v;
@@ -177,6 +190,49 @@ __device__ __forceinline__ float weights_of(const uint32_t (&a)[32], const uint3
   most = 0.0f;
   weights_of_32<MASK, FAR>(a, w, scales, by_scale, m, sum, most, left);
   weights_of_32<MASK, FAR>(b, w + 16, scales + 32, by_scale, m, sum, most, left - 32);
+  return sum;
+}
+
+// The same for 32 keys by factors of their own: at `tokens` lie the biased exponents of a key's scale and a value's, two bytes a token; kNoPage in the second: nothing of it is seen.
+constexpr uint32_t kNoPage = 255;
+struct TokenFactors {
+  uint32_t e[16];
+  __device__ __forceinline__ explicit TokenFactors(uint32_t tokens) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(e[4 * k]), "=r"(e[4 * k + 1]), "=r"(e[4 * k + 2]), "=r"(e[4 * k + 3]) : "r"(tokens + 16 * k));
+  }
+  __device__ __forceinline__ uint32_t value(int n) const { return e[n / 2] >> (n % 2 * 16 + 8) & 0xffu; }
+  // score factor, log2 and inverse of the values' scale
+  __device__ __forceinline__ float score(int n) const { return scale_of_exponent(e[n / 2] >> (n % 2 * 16) & 0xffu); }
+  __device__ __forceinline__ float log2(int n) const { return value(n) == kNoPage ? -INFINITY : log2_of_exponent(value(n)); }
+  __device__ __forceinline__ float inverse(int n) const { return value(n) == kNoPage ? 0.0f : inverse_of_exponent(value(n)); }
+};
+__device__ __forceinline__ float top_by_token(const uint32_t (&s)[32], uint32_t tokens, float by_scale, int left) {
+  const TokenFactors f(tokens);
+  float most = -INFINITY;
+#pragma unroll
+  for (int n = 0; n < 32; ++n) {
+    const float v = __fmaf_rn(__uint_as_float(s[n]), f.score(n) * by_scale, f.log2(n));
+    most = fmaxf(most, n < left ? v : -INFINITY);
+  }
+  return most;
+}
+__device__ __forceinline__ float weights_by_token(const uint32_t (&s)[32], uint32_t* w, uint32_t tokens, float by_scale, float m, float sum, int left) {
+  const TokenFactors f(tokens);
+  const bool far = fabsf(m) >= kNearReference;
+  const float less = far ? m : 0.0f, near = far ? 0.0f : m;
+#pragma unroll
+  for (int n = 0; n < 32; n += 2) {
+    float x[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const float v = __fmaf_rn(__uint_as_float(s[n + k]), f.score(n + k) * by_scale, f.log2(n + k) - near) - less;
+      x[k] = exp2_fast(n + k < left ? v : -INFINITY);
+      sum = __fmaf_rn(x[k], f.inverse(n + k), sum);
+    }
+    w[n / 2] = pack_half2(x[0], x[1]);
+  }
   return sum;
 }
 
@@ -297,13 +353,17 @@ struct Place {
   }
 };
 
-template <int D>
+template <int D, int BITS>
 struct Shared {
   static constexpr int kHalves = D / 64;
   static constexpr int kOperand = kHalves * kHalf;        // 128 rows of D binary16 numbers
   static constexpr int kQ = 0, kK = 2 * kOperand, kV = 4 * kOperand;
   static constexpr int kScales = 6 * kOperand;
-  static constexpr int kBars = kScales + kMeta * kGranules * 16;
+  // Steps whose scales are kept.  Three are enough: a step's are written when the products of the last but one with the keys have ended, and those are behind the weights of the one before.
+  static constexpr int kMeta = BITS == 4 ? 3 : 4;
+  // 4 bits: exponents by token, in two bytes, so that the CTA stays within the 196 KB next to which L1 keeps 60 (with 8 KB more it keeps 28: 8192 tokens 538 -> 565 us)
+  static constexpr int kTokens = kScales + kMeta * kGranules * 16;
+  static constexpr int kBars = kTokens + (BITS == 4 ? kMeta * kKeys * 2 : 0);
   static constexpr int kBytes = kBars + 256;
 };
 // Barriers: buffers of keys and values; a half step's scores, weights and sums, by group and half; a tile's queries, by group; the end of a group's products.
@@ -326,11 +386,14 @@ __host__ __device__ constexpr uint32_t arrivals_of(int bar) {  // a group's warp
 //
 // BITS = 4: a token has a scale and a zero-point of its own, which the widening groups apply: with a scale of seven significant bits and a range of the token that reaches 0, (code + zero-point) * scale
 // has at most 11 bits and is exact in binary16 (otherwise the product of the last two is rounded, and the sum).  Scales are taken relative to a power of two above a granule's largest, which takes the
-// place of the page's scale: what the softmax and product warps do is the same for both widths.  8192 tokens as above 541 to 621 us from box to box, 5 requests in chunks 345 to 368; with a sum and a
-// product for two codes instead of one fused operation 577 and 365.
+// place of the page's scale: what the softmax and product warps do is the same for both widths.  Where a granule's scales differ by more than 2^kNearScales each of its
+// tokens has a power of two of its own: the large ones may have no weight in a row, or not be seen by it.  Such a granule's factors make every weight infinite, so that half a step takes the path for
+// large weights, which goes by token there; others pay nothing in the softmax.  A lane of the widening groups has one token's scale and zero-point and hands what widens its codes to the lanes that have
+// them.  8192 tokens as above 541 to 621 us from box to box, 5 requests in chunks 340 to 368 (the check of the scales: 538 -> 548 and 335 -> 340 on one); with a sum and a product for two codes instead of
+// one fused operation 577 and 365.
 template <bool BF16, int D, int BITS>
 __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const AttentionParams p) {
-  using Sh = Shared<D>;
+  using Sh = Shared<D, BITS>;
   extern __shared__ unsigned char smem_raw[];
   __shared__ unsigned long long s_scan[kThreads / 32], s_begin, s_tiles[kThreads / 32];
   __shared__ uint32_t s_tmem, s_failed, s_status;
@@ -537,8 +600,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
       if (any) {
         const float by_scale = factor * fabsf(p.scale_log2);
         const int seen = place.r.seen(static_cast<int>(token)), seen_first = place.r.seen(static_cast<int>(row0 / group));
-        uint32_t scales = static_cast<uint32_t>(place.before) % kMeta;
-        for (int j = place.k0; j < limit; ++j, ++count, scales = (scales + 1) % kMeta) {
+        uint32_t scales = static_cast<uint32_t>(place.before) % Sh::kMeta;
+        for (int j = place.k0; j < limit; ++j, ++count, scales = scales + 1 == Sh::kMeta ? 0u : scales + 1) {
           const bool mask = (j + 1) * kKeys > seen_first;  // as far as the group's first row sees
 #pragma unroll 1
           for (int h = 0; h < 2; ++h) {
@@ -560,8 +623,17 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
               again = __any_sync(kFull, most_weight > 4096.0f);
             }
             if (again) {
-              const float most = mask ? fmaxf(top_score<true>(a, factors, by_scale, left), top_score<true>(b, factors + 32, by_scale, left - 32))
-                                      : fmaxf(top_score<false>(a, factors, by_scale, 64), top_score<false>(b, factors + 32, by_scale, 64));
+              // whether a granule of the half has factors by token: its place among the granules' says so
+              const bool apart = BITS == 4 && __any_sync(kFull, shared_float(factors + (lane & 3) * 16 + 12) != 0.0f);
+              const uint32_t tokens = smem + Sh::kTokens + (scales * kKeys + 64 * h) * 2;
+              const int within = mask ? left : 64;
+              float most;
+              if (BITS == 4 && apart) {
+                most = fmaxf(top_by_token(a, tokens, by_scale, within), top_by_token(b, tokens + 64, by_scale, within - 32));
+              } else {
+                most = mask ? fmaxf(top_score<true>(a, factors, by_scale, left), top_score<true>(b, factors + 32, by_scale, left - 32))
+                            : fmaxf(top_score<false>(a, factors, by_scale, 64), top_score<false>(b, factors + 32, by_scale, 64));
+              }
               float by = 1.0f;
               if (have ? most > m + 8.0f : most > -INFINITY) {
                 by = have ? exp2_fast(m - most) : 0.0f;
@@ -583,7 +655,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                   tm_store16(o_at + d, o);
                 }
               }
-              sum = weights_of<true, true>(a, b, w, factors, by_scale, m, most_weight, mask ? left : 64);
+              if (BITS == 4 && apart) {
+                sum = weights_by_token(b, w + 16, tokens + 64, by_scale, m, weights_by_token(a, w, tokens, by_scale, m, 0.0f, within), within - 32);
+              } else {
+                sum = weights_of<true, true>(a, b, w, factors, by_scale, m, most_weight, within);
+              }
             }
             l += sum;
             tm_store32(at_half, w);                        // in the place of scores, which have all been read
@@ -800,7 +876,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
         if (more) fetch_pages(j);
         const uint32_t buffer = n & 1u;
         if (!wait(free + buffer, ((n >> 1) & 1u) ^ 1u)) break;
-        if (has_scale) reinterpret_cast<float4*>(smem_at + Sh::kScales)[(n % kMeta) * kGranules + in_group] = scale;
+        if (has_scale) reinterpret_cast<float4*>(smem_at + Sh::kScales)[(n % Sh::kMeta) * kGranules + in_group] = scale;
 #pragma unroll
         for (int it = 0; it < kItems; ++it) {
           const int token = token0 + it * (128 / kChunks);
@@ -825,50 +901,49 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
       unsigned char* const to = smem_at + (values ? Sh::kV : Sh::kK) + (chunk / 2) * kHalf + (32 * w + token0) * 128;
       const uint32_t page_rows = static_cast<uint32_t>(p.kv_heads) << p.page_shift, mask = (1u << p.page_shift) - 1u;
       uint4 raw[kItems];
-      uint32_t k_word[kItems], v_word[kItems];             // scales and zero-points; 0 where there is no token.  The values' group has no use for the keys'
+      constexpr uint32_t kNoToken = 0x8000u;               // the word of a token that is not there: a scale of -0, which no token has
+      uint32_t k_word = kNoToken, v_word = kNoToken;       // scale and zero-point of the lane's token.  The values' group has no use for the keys'
       int pages[2];                                        // of the next step's granules
       auto fetch_pages = [&](int j) {
         pages[0] = page_at(j, 2 * w);
         pages[1] = page_at(j, 2 * w + 1);
       };
-      bool there[2];                                       // of the step whose codes have been fetched: granules whose page is in the cache
+      const bool upper = lane >= 16;                       // the lane's token is in the second granule
+      bool there = false;                                  // of the step whose codes have been fetched: its granule's page is in the cache
       auto fetch = [&](int j) {
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
           const int first = j * kKeys + 32 * w + 16 * g;
-          there[g] = static_cast<unsigned>(pages[g]) < static_cast<unsigned>(p.pages);
+          const bool in_cache = static_cast<unsigned>(pages[g]) < static_cast<unsigned>(p.pages);
           const unsigned long long at = static_cast<unsigned long long>(static_cast<uint32_t>(pages[g])) * page_rows +
-                                        ((static_cast<uint32_t>(place.head) << p.page_shift) + (static_cast<uint32_t>(first) & mask) + token0);
-          const int8_t* const from = codes + at * (D / 2) + chunk * 16;
-          const uint32_t *const k_from = p.k_grid + at, *const v_from = p.v_grid + at;
-          const int left = place.r.keys - first - token0;
+                                        ((static_cast<uint32_t>(place.head) << p.page_shift) + (static_cast<uint32_t>(first) & mask));
+          const int8_t* const from = codes + (at + token0) * (D / 2) + chunk * 16;
 #pragma unroll
           for (int n = 0; n < kItems / 2; ++n) {
             const int it = g * (kItems / 2) + n;
             raw[it] = make_uint4(0u, 0u, 0u, 0u);
-            k_word[it] = v_word[it] = 0u;
-            if (there[g]) {
-              raw[it] = *reinterpret_cast<const uint4*>(from + n * (kItemTokens * D / 2));
-              if (n * kItemTokens < left) {
-                v_word[it] = v_from[n * kItemTokens];
-                if (!values) k_word[it] = k_from[n * kItemTokens];
-              }
+            if (in_cache) raw[it] = *reinterpret_cast<const uint4*>(from + n * (kItemTokens * D / 2));
+          }
+          if (upper == (g == 1)) {
+            there = in_cache;
+            k_word = v_word = kNoToken;
+            if (in_cache && first + (lane & 15) < place.r.keys) {
+              v_word = p.v_grid[at + (lane & 15)];
+              if (!values) k_word = p.k_grid[at + (lane & 15)];
             }
           }
         }
       };
-      // Scales are taken relative to a power of two above the granule's largest: they come to below 2^-5, so that times 2^21 they stay in binary16.  e: that one's biased exponent.
-      auto exponent_of = [&](const uint32_t (&word)[kItems], int g) {
-        uint32_t most = 0u;
-#pragma unroll
-        for (int n = 0; n < kItems / 2; ++n) {
-          const uint32_t e = word[g * (kItems / 2) + n] & 0x7f80u;
-          most = max(most, e == 0x7f80u ? 0u : e);
-        }
-        return __reduce_max_sync(kFull, most) >> 7;
+      // Biased exponents: of a scale, 0 where it counts as infinite or is NaN; the largest of the lane's granule.
+      auto is_number = [](uint32_t word) { return (word & 0x7f80u) < (kMostExponent << 7); };
+      auto largest = [&](uint32_t word) {
+        const uint32_t field = is_number(word) ? word & 0x7f80u : 0u;
+        const uint32_t lower_most = __reduce_max_sync(kFull, upper ? 0u : field), upper_most = __reduce_max_sync(kFull, upper ? field : 0u);
+        return (upper ? upper_most : lower_most) >> 7;
       };
-      auto power = [](uint32_t e) { return __uint_as_float((e < 248u ? 248u - e : 1u) << 23); };
-      auto inverse_power = [](uint32_t e) { return __uint_as_float((e + 6u) << 23); };
+      // whether the lane's scale, or 2^least if that is more, lies far below 2^e
+      auto is_far = [](uint32_t word, uint32_t e, uint32_t least) { return word != kNoToken && max(word & 0x7fffu, least << 7) + (kNearScales << 7) < (e << 7); };
+      uint32_t slot = 0;                                   // of the step's scales
       int j = place.k0;
       bool more = true;
       fetch_pages(j);
@@ -879,32 +954,50 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
           j = place.k0;
         }
         if (more) fetch_pages(j);
-        uint32_t k_e[2] = {0u, 0u}, v_e[2];
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          if (!values) k_e[g] = exponent_of(k_word, g);
-          v_e[g] = max(exponent_of(v_word, g), 67u);       // kLeastScale
+        // Scales are taken relative to a power of two above the granule's largest, or in a granule whose tokens are apart above themselves.
+        uint32_t k_e = 0u, v_e = max(largest(v_word), kLeastExponent);
+        bool far = is_far(v_word, v_e, kLeastExponent), apart = false;
+        if (!values) {
+          k_e = largest(k_word);
+          far = far || is_far(k_word, k_e, 0u);
         }
+        if (__any_sync(kFull, far)) {
+          const uint32_t half = upper ? 0xffff0000u : 0xffffu;
+          const uint32_t v_far = __ballot_sync(kFull, is_far(v_word, v_e, kLeastExponent)) & half;
+          if (v_far != 0u) v_e = max(min((v_word >> 7) & 0xffu, kMostExponent - 1u), kLeastExponent);
+          if (!values) {
+            const uint32_t k_far = __ballot_sync(kFull, is_far(k_word, k_e, 0u)) & half;
+            if (k_far != 0u) k_e = min((k_word >> 7) & 0xffu, kMostExponent - 1u);
+            apart = (v_far | k_far) != 0u;
+          }
+        }
+        // The two numbers that widen the lane's token, for the lanes that have its codes.  A token of which a scale is no number makes the rows NaN that see it, and no others: by its scores
+        const uint32_t word = values ? v_word : k_word;
+        float scale = grid_scale(word) * inverse_of_exponent(values ? v_e : k_e);
+        if (values) {
+          scale = is_number(v_word) ? scale : 0.0f;
+        } else {
+          scale = is_number(k_word) && is_number(v_word) ? scale : __uint_as_float(0x7fffffffu);
+        }
+        const uint32_t factors = pack_half2(scale * 2097152.0f, grid_zero(word) * scale);
         const uint32_t buffer = n & 1u;
         if (!wait(free + buffer, ((n >> 1) & 1u) ^ 1u)) break;
-        if (!values && lane < 2) {                         // nothing of a page that is not there is seen
-          const bool here = lane == 0 ? there[0] : there[1];
-          const uint32_t ke = lane == 0 ? k_e[0] : k_e[1], ve = lane == 0 ? v_e[0] : v_e[1];
-          reinterpret_cast<float4*>(smem_at + Sh::kScales)[(n % kMeta) * kGranules + 2 * w + lane] =
-              here ? make_float4(inverse_power(ke), static_cast<float>(static_cast<int>(ve) - 121), power(ve), 0.0f) : make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
+        if (!values) {
+          if ((lane & 15) == 0) {                          // nothing of a page that is not there is seen
+            reinterpret_cast<float4*>(smem_at + Sh::kScales)[slot * kGranules + 2 * w + (lane >> 4)] =
+                !there  ? make_float4(0.0f, -INFINITY, 0.0f, 0.0f)
+                : apart ? make_float4(0.0f, INFINITY, 0.0f, 1.0f)
+                        : make_float4(scale_of_exponent(k_e), log2_of_exponent(v_e), inverse_of_exponent(v_e), 0.0f);
+          }
+          reinterpret_cast<uint16_t*>(smem_at + Sh::kTokens)[slot * kKeys + 32 * w + lane] = static_cast<uint16_t>(k_e | (there ? v_e : kNoPage) << 8);
         }
+        slot = slot + 1 == Sh::kMeta ? 0u : slot + 1;
 #pragma unroll
         for (int it = 0; it < kItems; ++it) {
-          const int g = it / (kItems / 2), token = 16 * g + it % (kItems / 2) * kItemTokens;
-          float scale;
-          if (values) {
-            scale = grid_is_number(v_word[it]) ? grid_scale(v_word[it]) * power(v_e[g]) : 0.0f;
-          } else {                                         // a token of which a scale is no number makes the rows NaN that see it, and no others: by its scores
-            const float ks = grid_scale(k_word[it]);
-            scale = __fmaf_rn(ks, power(k_e[g]), __fmaf_rn(ks, 0.0f, grid_scale(v_word[it]) * 0.0f));
-          }
-          const float zero = grid_zero(values ? v_word[it] : k_word[it]);
-          const __half2 by_low = __float2half2_rn(scale * 2097152.0f), by_high = __float2half2_rn(scale * 131072.0f), add = __float2half2_rn(zero * scale);
+          const int token = 16 * (it / (kItems / 2)) + it % (kItems / 2) * kItemTokens;
+          const uint32_t of_token = __shfl_sync(kFull, factors, token0 + token);
+          const __half2 by_low = Elem<false>::as2(__byte_perm(of_token, 0u, 0x1010)), add = Elem<false>::as2(__byte_perm(of_token, 0u, 0x3232));
+          const __half2 by_high = __hmul2(by_low, __float2half2_rn(0.0625f));  // exact: by_low is 2^10 or more, or that of a scale far below kLeastScale
           unsigned char* const at = to + buffer * Sh::kOperand + token * 128;
           const uint32_t u[4] = {raw[it].x, raw[it].y, raw[it].z, raw[it].w};
           // eight tokens further the swizzle is the same
@@ -1004,8 +1097,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
 
 template <bool BF16, int D, int BITS>
 cudaError_t launch(const AttentionParams& p, int ctas, cudaStream_t stream) {
-  constexpr int bytes = Shared<D>::kBytes + 1024;
-  static_assert(Shared<D>::kScales >= 8 * kMaxRequests, "the unit counts fit in front of the scales");
+  constexpr int bytes = Shared<D, BITS>::kBytes + 1024;
+  static_assert(Shared<D, BITS>::kScales >= 8 * kMaxRequests, "the unit counts fit in front of the scales");
   static std::atomic<unsigned long long> done{0};
   const cudaError_t e = allow_shared(attention_tiles_kernel<BF16, D, BITS>, bytes, done);
   if (e != cudaSuccess) return e;
