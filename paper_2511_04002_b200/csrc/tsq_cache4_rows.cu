@@ -345,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
               const float now = fmaxf(m[t][h], column_max(top[t][h]));
               by[h] = m[t][h] == -INFINITY ? 0.0f : exp2_fast(m[t][h] - now);
               m[t][h] = now;
-              limit[t][h] = now + 8.0f;
+              limit[t][h] = follow_above(now);
               acc_zero[t][h] *= by[h];
             }
             l[t] = mul2(l[t], pack2f(by[0], by[1]));

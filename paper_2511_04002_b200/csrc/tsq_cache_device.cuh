@@ -74,6 +74,10 @@ __device__ __forceinline__ unsigned int count_arrival(unsigned int* counter, uns
   return before;
 }
 
+// A score above this is not weighed against the reference m but becomes it: 2^8 is what a weight may come to in binary16, with room.  Rounded down: from 2^27 on binary32's numbers lie 16 and more apart, and
+// m + 8 rounded to the next of them would let a weight of 2^16 pass, which binary16 does not hold.
+__device__ __forceinline__ float follow_above(float m) { return __fadd_rd(m, 8.0f); }
+
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(kThreads, Layout<D, NT>::kCtasPerSm) attention
             if (token0 + g + 8 >= seen[t][0]) s[t][2] = -INFINITY;
             if (token0 + g + 8 >= seen[t][1]) s[t][3] = -INFINITY;
           }
-          over = over || fmaxf(s[t][0], s[t][2]) > m[t][0] + 8.0f || fmaxf(s[t][1], s[t][3]) > m[t][1] + 8.0f;
+          over = over || fmaxf(s[t][0], s[t][2]) > follow_above(m[t][0]) || fmaxf(s[t][1], s[t][3]) > follow_above(m[t][1]);
         }
         // m is a reference, not the maximum: it follows only when a score is more than 2^8 above it (a weight stays below 2^9 in binary16)
         if (__any_sync(kFull, over)) {

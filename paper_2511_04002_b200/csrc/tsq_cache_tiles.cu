@@ -635,7 +635,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                             : fmaxf(top_score<false>(a, factors, by_scale, 64), top_score<false>(b, factors + 32, by_scale, 64));
               }
               float by = 1.0f;
-              if (have ? most > m + 8.0f : most > -INFINITY) {
+              if (have ? most > follow_above(m) : most > -INFINITY) {
                 by = have ? exp2_fast(m - most) : 0.0f;
                 m = most;
                 have = true;
