@@ -305,8 +305,9 @@ tsq_status_t move_rows(const tsq_cache4_t* cache, void* k, int64_t k_stride, voi
 }
 
 // Which kernel: by the query rows that a key head's codes serve at most.  The row kernel takes the codes again for every 16 rows, the tile kernel 256 at once, at a step's price whether they
-// are there or not.  us, rows / tiles (bf16, heads of 128): 16 requests of 8000 keys, 8 key heads, 16 rows 59 / 149, 32 rows 98 / 148, 48 rows 136 / 148, 64 rows 174 / 151; 64 of 2000 keys 48 rows
-// 151 / 161, 64 rows 195 / 161; 1 of 100000 keys 48 rows 116 / 153, 64 rows 140 / 153; 16 of 3000 keys, 40 key heads, 32 rows 180 / 264, 40 rows 255 / 265.
+// are there or not.  us, rows / tiles, 8 key heads of 128 (of 64), bf16, fp16 within 1 %: 16 requests of 8000 keys 16 rows 51 / 144 (35 / 109), 32 rows 87 / 145 (60 / 110), 48 rows 124 / 147 (84 / 110),
+// 64 rows 161 / 145 (108 / 110); 64 of 2000 keys 32 rows 96 / 150 (66 / 118), 48 rows 138 / 151 (92 / 119), 64 rows 180 / 152 (119 / 119); 1 of 100000 keys 48 rows 99 / 148 (69 / 112), 64 rows
+// 125 / 149 (84 / 113), 96 rows 179 / 149 (120 / 113); 16 of 3000 keys, 40 key heads, 48 rows 240 / 254 (158 / 198), 64 rows 315 / 253 (206 / 199).
 constexpr int kFewRows = 48;
 bool few_query_rows(long long max_query, int group) { return max_query * group <= kFewRows; }
 

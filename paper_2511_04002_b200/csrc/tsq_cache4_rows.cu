@@ -80,7 +80,7 @@ template <int D, int NT>
 struct Layout {
   static constexpr int kRows = 8 * NT;
   // heads of 128, 8 rows: 4 CTAs of 128 registers 70.5 us for 64 requests, 3 of 168 68.2, 2 of 255 73; 131072 tokens 46.0, 40.5, 42.6.  16 rows: 3 CTAs 58.9 us for 16 requests of 8000 tokens, 2
-  // (nothing spilled) 50.7; heads of 64 35.2, 35.6
+  // (nothing spilled) 50.7; heads of 64 3 CTAs 35.2 (20 bytes spilled), 2 35.6
   static constexpr int kCtasPerSm = D == 64 ? (NT == 1 ? 4 : 3) : NT == 1 ? 3 : 2;
   static constexpr int kStages = 3;                      // of a warp's ring
   static constexpr int kHalf = kStepTokens * D / 2;      // bytes of a stage's keys, and of its values

@@ -389,7 +389,7 @@ __host__ __device__ constexpr uint32_t arrivals_of(int bar) {  // a group's warp
 // place of the page's scale: what the softmax and product warps do is the same for both widths.  Where a granule's scales differ by more than 2^kNearScales each of its
 // tokens has a power of two of its own: the large ones may have no weight in a row, or not be seen by it.  Such a granule's factors make every weight infinite, so that half a step takes the path for
 // large weights, which goes by token there; others pay nothing in the softmax.  A lane of the widening groups has one token's scale and zero-point and hands what widens its codes to the lanes that have
-// them.  8192 tokens as above 541 to 621 us from box to box, 5 requests in chunks 340 to 368 (the check of the scales: 538 -> 548 and 335 -> 340 on one); with a sum and a product for two codes instead of
+// them.  8192 tokens as above 546 to 606 us from box to box, 5 requests in chunks 340 to 368 (the check of the scales: 538 -> 548 and 335 -> 340 on one); with a sum and a product for two codes instead of
 // one fused operation 577 and 365.
 template <bool BF16, int D, int BITS>
 __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const AttentionParams p) {

@@ -143,3 +143,26 @@ def test_a_token_of_zeros_that_has_nearly_all_the_weight(dtype, added, log2):
     p /= p.sum()
     want, most = p @ v, (p @ size) * (2.0 ** -11 + 2.0 ** -16 + (held / 16 + 8) * 2.0 ** -23)
     assert bool(((out.double() - want).abs() <= most + HALF_STEP[dtype] * (want.abs() + most) + (2.0 ** -25 if dtype == F16 else 0.0)).all())
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("added", [1, 40])
+@pytest.mark.parametrize("log2_scale", [0, 18, 22, 30, 60])
+def test_scores_far_from_zero_beside_small_keys(dtype, added, log2_scale):
+    """One key is 2^6 times its neighbours and its score above theirs by more than 2^8: a row is that key's value, whose weight may be off by half a step of binary16."""
+    held = 300
+    s = Setup4(dtype, [held], 2, 64, 16, seed=66)
+    every = s.table[0, :(held + 15) // 16].long()
+    s.k_grid[every] = word_of(torch.tensor([2.0 ** -5]), torch.tensor([0])).cuda()
+    s.k_codes[every] = 5 * 17
+    for where in (0, 70, held - added):                                 # every row sees them; each is 16 times the one before
+        page, place = int(s.table[0, where // 16]), where % 16
+        s.k_grid[page, :, place] = word_of(torch.tensor([2.0 * 16.0 ** (where > 0) * 16.0 ** (where > 70)]), torch.tensor([0])).cuda()
+        s.k_codes[page, :, place] = 15 * 17
+        q = (torch.rand((added, 6, 1), generator=s.g) * 3 + 2).to(dtype).expand(added, 6, 64).contiguous().cuda()
+        out = torch.full_like(q, 5.0)
+        ws = s.cache.workspace(added, 6, 1, added)
+        s.cache.attention(q, s.ints([0, added]), s.ints([held]), s.table, out, ws, added, scale=2.0 ** log2_scale)
+        want = numbers(s.v_codes[page, :, place], s.v_grid[page, :, place]).repeat_interleave(3, 0)[None]
+        size = (scales(s.v_grid[page, :, place]).double() * (15 + zeros(s.v_grid[page, :, place]).abs())).repeat_interleave(3, 0)[None, :, None]
+        assert bool(((out.double() - want).abs() <= (HALF_STEP[dtype] + 2.0 ** -16) * want.abs() + 2.0 ** -10.9 * size + 2.0 ** -24).all()), where
