@@ -16,8 +16,8 @@ constexpr int kSoftmaxRegs = 136, kWidenRegs = 80, kProductRegs = 48, kLaunchReg
 constexpr int kTileSteps = 4;                // what beginning and ending a tile costs, in steps
 // Most parts of a tile, on the average: adding a part up takes 1.7 us, a step 2.3 us (one tile of 235 steps in 148 parts 300 us, in 16 80 us).
 constexpr unsigned long long kMostParts = 16;
-// 4 bits: powers of two by which a token's scale may be below the largest of its granule and its weights and numbers still go relative to that one.  Up to 12 numbers would come out the same;
-// weights lose as many bits at the small end as the granule's scale is above those that count.
+// 4 bits: how many powers of two a token's scale may lie below the largest of its granule, so that its numbers and weights still go relative to that one.  With up to twelve the numbers would be the same,
+// but weights lose as many bits at the small end as the granule's scale is above the scales that count.
 constexpr uint32_t kNearScales = 4;
 constexpr uint32_t kMostExponent = 247;      // of a scale, biased: 2^120 and more counts as infinite
 constexpr uint32_t kLeastExponent = 67;      // of a value's scale: kLeastScale
